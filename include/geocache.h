@@ -45,7 +45,11 @@ typedef enum {
     GEOCACHE_EALIAS = -7    /* buffers overlap in a way the call does not allow */
 } geocache_status;
 
-typedef enum { GEOCACHE_F32 = 0, GEOCACHE_BF16 = 1 } geocache_dtype;
+typedef enum {
+    GEOCACHE_F32 = 0,
+    GEOCACHE_BF16 = 1,
+    GEOCACHE_F16 = 2  /* queries, keys and values of the attention block only */
+} geocache_dtype;
 
 typedef enum { GEOCACHE_DDIM = 0, GEOCACHE_FM_EULER = 1 } geocache_sampler;
 
@@ -411,6 +415,87 @@ int geocache_unpack_anchors(const void* src, void* dst, int64_t row_bytes, int B
                             int a, void* stream);
 
 /* --------------------------------------------------------------------------
+ * The attention block of the anchor-only forward (Sec. 3.2, "batch-sliced
+ * anchor forward": the denoiser runs on the packed anchor rows, which keep
+ * their structural indices and rotary slots).  The paper gives no kernels for
+ * it; the operators are the standard ones that a transformer denoiser puts
+ * between its projections.
+ * ------------------------------------------------------------------------ */
+
+/* Heads of a [tokens, heads, D] tensor: element (t, h, d) is at
+ * data + t * token_stride + h * head_stride + d (strides in elements, >= 0),
+ * so the queries, keys and values inside one projection's output need no copy. */
+typedef struct {
+    void* data;            /* device */
+    int64_t token_stride;
+    int64_t head_stride;
+} geocache_heads;
+
+typedef enum {
+    GEOCACHE_ROPE_HALF = 0,        /* pair i of a head: elements (i, i + rot/2) */
+    GEOCACHE_ROPE_INTERLEAVED = 1  /* pair i of a head: elements (2i, 2i + 1) */
+} geocache_rope_layout;
+
+/* Frequencies of the rotation for contexts longer than the trained one. */
+typedef enum {
+    GEOCACHE_ROPE_PLAIN = 0,    /* f_i = theta^(-2i/rot) */
+    GEOCACHE_ROPE_LINEAR = 1,   /* f_i / factor */
+    GEOCACHE_ROPE_BASE = 2,     /* theta' = theta * factor^(rot/(rot-2)): the slowest pair turns factor times
+                                   slower, the fastest as before */
+    GEOCACHE_ROPE_BY_PARTS = 3  /* f_i * (r + (1 - r) / factor), r = clamp((n_i - low) / (high - low), 0, 1), where
+                                   n_i = original * f_i / (2 pi) are pair i's turns over the trained context */
+} geocache_rope_scaling;
+
+typedef struct {
+    int rot;                        /* rotated elements of a head: even, 2 <= rot <= 256 */
+    double theta;                   /* > 0 */
+    geocache_rope_scaling scaling;
+    double factor;                  /* > 0; ignored for PLAIN */
+    double original, low, high;     /* BY_PARTS: trained context > 0, low < high (in turns) */
+    double magnitude;               /* cos and sin are multiplied by it; 0 means 1 */
+} geocache_rope;
+
+/* --------------------------------------------------------------------------
+ * geocache_rope_table -- cosines and sines of the rotation, made once per
+ * model: for each slot n < n_slots and pair i < rot/2
+ *     table[n][first_pair + i] = magnitude * (cos(p f_i), sin(p f_i)),
+ * with p = pos[n] (device, n_slots i32), or n where pos is NULL.  table is
+ * [n_slots][row_pairs][2] f32, 8-byte aligned; pairs outside
+ * [first_pair, first_pair + rot/2) are left as they are, so a table over
+ * several axes (views, rows, columns) is made by one call for each axis.
+ * Angles, cosines and sines are formed in double and rounded once.
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE, EALIAS, ECUDA.
+ * ------------------------------------------------------------------------ */
+int geocache_rope_table(const geocache_rope* rope, const int32_t* pos, int64_t n_slots, float* table, int row_pairs,
+                        int first_pair, void* stream);
+
+/* --------------------------------------------------------------------------
+ * geocache_qk_norm_rope -- RMS norm of each head of the queries and keys and
+ * the rotation of their positions, in one pass:
+ *     n = x * rsqrt(mean_d(x_d^2) + eps) * weight_d      (norm != 0; else n = x)
+ *     (a, b) -> (a c - b s, a s + b c) for each pair of n, (c, s) = table[slot]
+ * rounded once to `dtype` (F32, BF16 or F16); elements d >= rot are not rotated.
+ * The mean and the rotation are computed in binary32.
+ *   q, k, q_out, k_out  [T, Hq, D] and [T, Hk, D]; Hq or Hk may be 0.  An output
+ *                       equal to its input (pointer and strides) is updated in
+ *                       place; any other overlap is refused.
+ *   q_weight, k_weight  device [D] f32, or NULL (ones).
+ *   table               device [n_slots][rot/2][2] f32, 8-byte aligned; NULL iff rot = 0 (norm only).
+ *   slots               device [T] i32 (an anchor's tokens keep their slots of the
+ *                       N-view layout), or NULL: token t has slot t (T <= n_slots).
+ *                       A slot outside [0, n_slots) leaves its token unrotated and
+ *                       sets the device status word (EINVAL).
+ * Sizes: 0 <= T < 2^31, 0 <= Hq, Hk <= 65536, D % 8 == 0, 8 <= D <= 256, rot even,
+ * 0 <= rot <= D, eps >= 0.  Any alignment of the elements is accepted; rows
+ * that are 16-byte aligned are read in 16-byte words.
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE, EDTYPE, EALIAS, ECUDA.
+ * ------------------------------------------------------------------------ */
+int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, const geocache_heads* q_out,
+                          const geocache_heads* k_out, int64_t T, int Hq, int Hk, int D, geocache_dtype dtype, int norm,
+                          double eps, const float* q_weight, const float* k_weight, const float* table,
+                          int64_t n_slots, int rot, geocache_rope_layout layout, const int32_t* slots, void* stream);
+
+/* --------------------------------------------------------------------------
  * geocache_is_full_step -- 1 if `step` (0 <= step < S) is a full step under
  * `sched`, 0 if cached, a negative status on bad arguments. Host only.
  * ------------------------------------------------------------------------ */
@@ -442,10 +527,11 @@ int geocache_rotate_anchors(int N, int a, int step, int S, const geocache_schedu
  * (geocache_permute_records keeps that record), a mesh face with a vertex
  * index out of range (geocache_raster_posmaps skips it), a correspondence
  * table index outside [-1, H*W) in a TABLE-mode step (that tap is dropped),
- * and a bounded wait inside a kernel that ran out (its CTA returns without
+ * a rotary slot out of range (geocache_qk_norm_rope leaves that token
+ * unrotated), and a bounded wait inside a kernel that ran out (its CTA returns without
  * writing its outputs).
  * Returns GEOCACHE_OK, ESHAPE (record overflow), EINVAL (bad permutation
- * entry, face index or table index), ETIMEOUT (a wait gave up) or ECUDA.
+ * entry, face index, table index or slot), ETIMEOUT (a wait gave up) or ECUDA.
  * ------------------------------------------------------------------------ */
 int geocache_device_status(void* stream);
 

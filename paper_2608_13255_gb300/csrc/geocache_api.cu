@@ -86,6 +86,56 @@ int make_coef(const geocache_recon* r, geocache::ReconCoef* c) {
     return GEOCACHE_OK;
 }
 
+// bytes from a tensor's first element to the end of its last
+size_t heads_extent(const geocache_heads* x, int64_t T, int H, int D, int eb) {
+    return T && H ? ((size_t)(T - 1) * x->token_stride + (size_t)(H - 1) * x->head_stride + D) * eb : 0;
+}
+
+bool heads_overlap_bytes(const geocache_heads* x, int64_t T, int H, int D, int eb, const void* p, size_t n) {
+    return overlap(x->data, heads_extent(x, T, H, D, eb), p, n);
+}
+
+// [a, a + n) and [b, b + m) meet on a circle of `period`
+bool meet(int64_t a, int64_t n, int64_t b, int64_t m, int64_t period) {
+    const int64_t d = ((b - a) % period + period) % period;
+    return d < n || d + m > period;
+}
+
+// Two [T, H, D] tensors share an element.  Exact where both lie in rows of one
+// token stride (views of one projection's output); true where that cannot be
+// told and their extents meet.
+bool heads_overlap(const geocache_heads* a, int64_t Ta, int Ha, const geocache_heads* b, int64_t Tb, int Hb, int D, int eb) {
+    if (!overlap(a->data, heads_extent(a, Ta, Ha, D, eb), b->data, heads_extent(b, Tb, Hb, D, eb))) return false;
+    const int64_t row = a->token_stride * eb, w = (int64_t)D * eb;
+    const int64_t at = (int64_t)((uintptr_t)b->data - (uintptr_t)a->data);
+    const int64_t wa = (Ha - 1) * a->head_stride * eb + w, wb = (Hb - 1) * b->head_stride * eb + w;
+    if (row > 0 && a->token_stride == b->token_stride && wa <= row && wb <= row) {
+        if (!meet(0, wa, at, wb, row)) return false;
+        // heads of both interleaved with one stride that divides the row
+        const int64_t hs = a->head_stride * eb;
+        if (hs >= w && a->head_stride == b->head_stride && row % hs == 0) return meet(0, w, at, w, hs);
+    }
+    return true;
+}
+
+// A tensor that a call reads (strides >= 0) or writes (its rows apart from each other).
+int check_heads(const geocache_heads* x, int64_t T, int H, int D, int eb, bool write, const char* fn, const char* name) {
+    if (!x || !x->data) return fail(GEOCACHE_EINVAL, "%s: %s is required", fn, name);
+    if ((uintptr_t)x->data % eb) return fail(GEOCACHE_EINVAL, "%s: %s is not aligned to its elements", fn, name);
+    const int64_t ts = x->token_stride, hs = x->head_stride, most = (int64_t)1 << 38;
+    if (ts < 0 || hs < 0 || ts > most || hs > most)
+        return fail(GEOCACHE_ESHAPE, "%s: strides of %s (%lld, %lld) out of range", fn, name, (long long)ts, (long long)hs);
+    if ((ts && T - 1 > ((int64_t)1 << 56) / ts) || (hs && H - 1 > ((int64_t)1 << 56) / hs))
+        return fail(GEOCACHE_ESHAPE, "%s: %s spans over 2^56 elements", fn, name);
+    if (write) {
+        const bool tokens_outside = (H == 1 || hs >= D) && (T == 1 || ts >= (H - 1) * hs + D);
+        const bool heads_outside = (T == 1 || ts >= D) && (H == 1 || hs >= (T - 1) * ts + D);
+        if (!tokens_outside && !heads_outside)
+            return fail(GEOCACHE_EALIAS, "%s: rows of %s overlap each other", fn, name);
+    }
+    return GEOCACHE_OK;
+}
+
 size_t lat_bytes(int dtype) { return dtype == GEOCACHE_BF16 ? 2 : 4; }
 
 // total record count of the sparse form (synchronises the stream)
@@ -190,11 +240,12 @@ int geocache_last_launches(void) { return g_launches; }
 int geocache_abi_version(void) { return GEOCACHE_ABI_VERSION; }
 
 int geocache_device_status(void* stream) {
-    unsigned int word = 0, raster_word = 0;
+    unsigned int word = 0, raster_word = 0, rope_word = 0;
     cudaError_t e = geocache::read_device_error(&word, true, (cudaStream_t)stream);
     if (e == cudaSuccess) e = geocache::read_raster_error(&raster_word, true, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = geocache::read_rope_error(&rope_word, true, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "reading the device status word");
-    word |= raster_word;
+    word |= raster_word | rope_word;
     if (word & 2u)
         return fail(GEOCACHE_ESHAPE, "a sparse-form build had more records than max_records (status word 0x%x); "
                                      "query geocache_corr_record_count and rebuild", word);
@@ -207,6 +258,9 @@ int geocache_device_status(void* stream) {
     if (word & 16u)
         return fail(GEOCACHE_EINVAL, "a correspondence table index was outside [-1, H*W) (status word 0x%x); "
                                      "those taps were dropped", word);
+    if (word & 32u)
+        return fail(GEOCACHE_EINVAL, "a rotary slot was outside [0, n_slots) (status word 0x%x); "
+                                     "those tokens were not rotated", word);
     if (word) return fail(GEOCACHE_ETIMEOUT, "a bounded device wait gave up (status word 0x%x); outputs of that call are incomplete", word);
     return ok();
 }
@@ -520,6 +574,114 @@ int geocache_pack_anchors(const void* src, void* dst, int64_t row_bytes, int B, 
 int geocache_unpack_anchors(const void* src, void* dst, int64_t row_bytes, int B, int N, const int32_t* anchors,
                             int a, void* stream) {
     return copy_rows_entry(src, dst, row_bytes, B, N, anchors, a, false, stream);
+}
+
+int geocache_rope_table(const geocache_rope* r, const int32_t* pos, int64_t n_slots, float* table, int row_pairs,
+                        int first_pair, void* stream) {
+    const char* fn = "geocache_rope_table";
+    g_launches = 0;
+    if (!r) return fail(GEOCACHE_EINVAL, "%s: rope is NULL", fn);
+    if (r->rot < 2 || r->rot > 256 || r->rot % 2) return fail(GEOCACHE_ESHAPE, "%s: rot=%d must be even in [2, 256]", fn, r->rot);
+    if (n_slots < 0 || n_slots > 0x7fffffffLL) return fail(GEOCACHE_ESHAPE, "%s: n_slots=%lld out of range", fn, (long long)n_slots);
+    const int pairs = r->rot / 2;
+    if (row_pairs < 1 || row_pairs > 128 || first_pair < 0 || first_pair > row_pairs - pairs)
+        return fail(GEOCACHE_ESHAPE, "%s: pairs [%d, %d) outside the row of %d", fn, first_pair, first_pair + pairs, row_pairs);
+    auto positive = [](double x) { return x > 0.0 && std::isfinite(x); };
+    if (!positive(r->theta)) return fail(GEOCACHE_EINVAL, "%s: theta=%g must be positive", fn, r->theta);
+    if (r->scaling < GEOCACHE_ROPE_PLAIN || r->scaling > GEOCACHE_ROPE_BY_PARTS)
+        return fail(GEOCACHE_EINVAL, "%s: unknown scaling %d", fn, (int)r->scaling);
+    if (r->scaling != GEOCACHE_ROPE_PLAIN && !positive(r->factor))
+        return fail(GEOCACHE_EINVAL, "%s: factor=%g must be positive", fn, r->factor);
+    if (r->scaling == GEOCACHE_ROPE_BASE && r->rot < 4) return fail(GEOCACHE_EINVAL, "%s: a scaled base needs rot >= 4", fn);
+    if (r->scaling == GEOCACHE_ROPE_BY_PARTS &&
+        (!positive(r->original) || !(r->low < r->high) || !std::isfinite(r->low) || !std::isfinite(r->high)))
+        return fail(GEOCACHE_EINVAL, "%s: scaling by parts needs original > 0 and low < high", fn);
+    if (!std::isfinite(r->magnitude)) return fail(GEOCACHE_EINVAL, "%s: magnitude must be finite", fn);
+    if (n_slots > 0 && !table) return fail(GEOCACHE_EINVAL, "%s: table is required", fn);
+    if ((uintptr_t)table & 7) return fail(GEOCACHE_EINVAL, "%s: table must be 8-byte aligned", fn);
+    if ((uintptr_t)pos & 3) return fail(GEOCACHE_EINVAL, "%s: pos must be 4-byte aligned", fn);
+    if (overlap(table, (size_t)n_slots * row_pairs * 8, pos, (size_t)n_slots * 4))
+        return fail(GEOCACHE_EALIAS, "%s: table overlaps pos", fn);
+    geocache::RopeTableArgs a{};
+    a.magnitude = r->magnitude == 0.0 ? 1.0 : r->magnitude;
+    const double theta = r->scaling == GEOCACHE_ROPE_BASE ? r->theta * std::pow(r->factor, r->rot / (r->rot - 2.0)) : r->theta;
+    for (int i = 0; i < pairs; ++i) {
+        double f = std::pow(theta, -2.0 * i / r->rot);
+        if (r->scaling == GEOCACHE_ROPE_LINEAR) f /= r->factor;
+        if (r->scaling == GEOCACHE_ROPE_BY_PARTS) {
+            const double turns = r->original * f / (2.0 * 3.14159265358979323846);
+            const double part = std::fmin(1.0, std::fmax(0.0, (turns - r->low) / (r->high - r->low)));
+            f *= part + (1.0 - part) / r->factor;
+        }
+        a.freq[i] = f;
+    }
+    a.pos = pos;
+    a.table = reinterpret_cast<float2*>(table);
+    a.n_slots = n_slots;
+    a.pairs = pairs; a.row_pairs = row_pairs; a.first_pair = first_pair;
+    cudaError_t e = geocache::launch_rope_table(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, fn);
+    return ok();
+}
+
+int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, const geocache_heads* q_out,
+                          const geocache_heads* k_out, int64_t T, int Hq, int Hk, int D, geocache_dtype dtype, int norm,
+                          double eps, const float* q_weight, const float* k_weight, const float* table,
+                          int64_t n_slots, int rot, geocache_rope_layout layout, const int32_t* slots, void* stream) {
+    const char* fn = "geocache_qk_norm_rope";
+    g_launches = 0;
+    if (T < 0 || T > 0x7fffffffLL || Hq < 0 || Hq > 65536 || Hk < 0 || Hk > 65536)
+        return fail(GEOCACHE_ESHAPE, "%s: T=%lld, Hq=%d, Hk=%d out of range", fn, (long long)T, Hq, Hk);
+    if (D < 8 || D > 256 || D % 8) return fail(GEOCACHE_ESHAPE, "%s: D=%d must be a multiple of 8 in [8, 256]", fn, D);
+    if (rot < 0 || rot > D || rot % 2) return fail(GEOCACHE_ESHAPE, "%s: rot=%d must be even in [0, D=%d]", fn, rot, D);
+    if (dtype != GEOCACHE_F32 && dtype != GEOCACHE_BF16 && dtype != GEOCACHE_F16)
+        return fail(GEOCACHE_EDTYPE, "%s: unsupported dtype %d", fn, (int)dtype);
+    if (layout != GEOCACHE_ROPE_HALF && layout != GEOCACHE_ROPE_INTERLEAVED)
+        return fail(GEOCACHE_EINVAL, "%s: unknown layout %d", fn, (int)layout);
+    if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(GEOCACHE_EINVAL, "%s: eps=%g must be >= 0", fn, eps);
+    if ((table == nullptr) != (rot == 0)) return fail(GEOCACHE_EINVAL, "%s: table and rot must both be given or neither", fn);
+    if (((uintptr_t)table & 7) || (((uintptr_t)slots | (uintptr_t)q_weight | (uintptr_t)k_weight) & 3))
+        return fail(GEOCACHE_EINVAL, "%s: table must be 8-byte aligned, slots and weights 4-byte aligned", fn);
+    if (rot && (n_slots < 0 || n_slots > 0x7fffffffLL || (!slots && T > n_slots)))
+        return fail(GEOCACHE_ESHAPE, "%s: n_slots=%lld out of range (at least T without slots)", fn, (long long)n_slots);
+    const geocache_heads* in[2] = {q, k};
+    const geocache_heads* out[2] = {q_out, k_out};
+    const int H[2] = {Hq, Hk}, eb = dtype == GEOCACHE_F32 ? 4 : 2;
+    const char* name[2] = {"q", "k"};
+    geocache::NormRopeArgs a{};
+    for (int i = 0; i < 2; ++i) {
+        if (T == 0 || H[i] == 0) continue;
+        int st = check_heads(in[i], T, H[i], D, eb, false, fn, name[i]);
+        if (!st) st = check_heads(out[i], T, H[i], D, eb, true, fn, i ? "k_out" : "q_out");
+        if (st) return st;
+        a.in[i] = in[i]->data; a.in_ts[i] = in[i]->token_stride; a.in_hs[i] = in[i]->head_stride;
+        a.out[i] = out[i]->data; a.out_ts[i] = out[i]->token_stride; a.out_hs[i] = out[i]->head_stride;
+        const size_t tb = rot ? (size_t)n_slots * rot * 4 : 0;
+        if (heads_overlap_bytes(out[i], T, H[i], D, eb, table, tb) ||
+            heads_overlap_bytes(out[i], T, H[i], D, eb, slots, slots ? (size_t)T * 4 : 0) ||
+            heads_overlap_bytes(out[i], T, H[i], D, eb, q_weight, (size_t)D * 4) ||
+            heads_overlap_bytes(out[i], T, H[i], D, eb, k_weight, (size_t)D * 4))
+            return fail(GEOCACHE_EALIAS, "%s: an output overlaps the table, the slots or a weight", fn);
+        for (int j = 0; j < 2; ++j) {
+            if (H[j] == 0) continue;
+            const bool same = i == j && out[i]->data == in[j]->data && out[i]->token_stride == in[j]->token_stride &&
+                              out[i]->head_stride == in[j]->head_stride;
+            if (!same && heads_overlap(out[i], T, H[i], in[j], T, H[j], D, eb))
+                return fail(GEOCACHE_EALIAS, "%s: %s_out overlaps %s", fn, name[i], name[j]);
+        }
+    }
+    if (T > 0 && Hq > 0 && Hk > 0 && heads_overlap(q_out, T, Hq, k_out, T, Hk, D, eb))
+        return fail(GEOCACHE_EALIAS, "%s: q_out overlaps k_out", fn);
+    a.weight[0] = q_weight; a.weight[1] = k_weight;
+    a.table = reinterpret_cast<const float2*>(table);
+    a.slots = slots;
+    a.n_slots = n_slots;
+    a.T = (int)T; a.Hq = Hq; a.Hk = Hk; a.D = D; a.rot = rot; a.layout = layout; a.norm = norm != 0;
+    a.eps = (float)eps;
+    a.dtype = dtype;
+    cudaError_t e = geocache::launch_norm_rope(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, fn);
+    return ok();
 }
 
 int geocache_is_full_step(int step, int S, const geocache_schedule* sched) {

@@ -99,6 +99,32 @@ cudaError_t launch_raster(const float* V, long long nv, const int32_t* F, long l
 cudaError_t launch_pool_posmaps(const float* pos_hi, const uint8_t* valid_hi, long long n_maps, int H, int W, int ss,
                                 float* pos, uint8_t* valid, cudaStream_t s);
 
+struct RopeTableArgs {
+    double freq[128];        // of the pairs
+    double magnitude;
+    const int32_t* pos;      // or nullptr: the slot's index
+    float2* table;           // [n_slots][row_pairs], written at [first_pair, first_pair + pairs)
+    long long n_slots;
+    int pairs, row_pairs, first_pair;
+};
+cudaError_t launch_rope_table(const RopeTableArgs& a, cudaStream_t s);
+
+// Heads [0, H) of the queries are followed by those of the keys.
+struct NormRopeArgs {
+    const void* in[2];       // queries, keys
+    void* out[2];
+    long long in_ts[2], in_hs[2], out_ts[2], out_hs[2];   // strides in elements
+    const float* weight[2];  // [D] or nullptr
+    const float2* table;     // [n_slots][rot / 2]
+    const int32_t* slots;    // [T] or nullptr
+    long long n_slots;
+    int T, Hq, Hk, D, rot, layout, norm;
+    float eps;
+    int dtype;
+};
+cudaError_t launch_norm_rope(const NormRopeArgs& a, cudaStream_t s);
+cudaError_t read_rope_error(unsigned int* out, bool clear, cudaStream_t s);
+
 // Counts kernels that the calling thread's current library call enqueues
 // (geocache_last_launches).
 void note_launches(int n);

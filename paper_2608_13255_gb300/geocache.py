@@ -19,7 +19,7 @@ import torch
 from . import build as _build
 
 OK, EINVAL, ESHAPE, EDTYPE, ECUDA, ETIMEOUT, EDEVICE, EALIAS = 0, -1, -2, -3, -4, -5, -6, -7
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 DDIM, FM_EULER = 0, 1
 PRED_NONE, PRED_EPS, PRED_V, PRED_VELOCITY = 0, 1, 2, 3
 CORR_GEOMETRY, CORR_TABLE, CORR_MASK, CORR_SPARSE = 0, 1, 2, 3
@@ -27,6 +27,8 @@ UPDATE_DELTA, UPDATE_COPY = 0, 1
 TILE_TOKENS = 1024
 SCHED_EVERY_K, SCHED_HEAD_MID_TAIL, SCHED_LIST, SCHED_ALL_FULL, SCHED_SINGLE_CACHED = 0, 1, 2, 3, 4
 MAX_VIEWS = 64
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
 
 _SAMPLERS = {"ddim": DDIM, "fm_euler": FM_EULER, DDIM: DDIM, FM_EULER: FM_EULER}
 _PREDS = {None: PRED_NONE, "none": PRED_NONE, "eps": PRED_EPS, "v": PRED_V, "velocity": PRED_VELOCITY,
@@ -66,6 +68,16 @@ class Schedule(ctypes.Structure):
                 ("contiguous_rotation", ctypes.c_int)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int), ("theta", ctypes.c_double), ("scaling", ctypes.c_int),
+                ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
 assert ctypes.sizeof(Camera) == 64
 
 _LIB = None
@@ -75,6 +87,7 @@ EXPORTS = ("geocache_build_corr", "geocache_transport_step", "geocache_reconstru
            "geocache_unpack_anchors", "geocache_transport_step_update", "geocache_permute_records",
            "geocache_raster_posmaps", "geocache_debug_set_wait", "geocache_raster_posmaps_supersampled",
            "geocache_pool_posmaps", "geocache_fill_records", "geocache_last_launches",
+           "geocache_rope_table", "geocache_qk_norm_rope",
            "geocache_last_error", "geocache_abi_version")
 
 
@@ -112,6 +125,11 @@ def load():
         for name in ("geocache_pack_anchors", "geocache_unpack_anchors"):
             getattr(L, name).argtypes = [P, P, i64, i, i, P, i, P]
             getattr(L, name).restype = ctypes.c_int
+        H = ctypes.POINTER(Heads)
+        L.geocache_rope_table.argtypes = [ctypes.POINTER(Rope), P, i64, P, i, i, P]
+        L.geocache_rope_table.restype = ctypes.c_int
+        L.geocache_qk_norm_rope.argtypes = [H, H, H, H, i64, i, i, i, i, i, ctypes.c_double, P, P, P, i64, i, i, P, P]
+        L.geocache_qk_norm_rope.restype = ctypes.c_int
         L.geocache_corr_record_count.argtypes = [ctypes.POINTER(Corr), ctypes.POINTER(ctypes.c_int64), P]
         L.geocache_corr_record_count.restype = ctypes.c_int
         L.geocache_fill_records.argtypes = [ctypes.POINTER(Corr), P]
@@ -490,6 +508,91 @@ def unpack_anchors(src, dst, anchors, stream=None):
                                           arr, len(anc), _stream(stream)))
 
 
+# ------------------------------------------- attention of the anchors' rows --
+_ROPE_SCALINGS = {"plain": ROPE_PLAIN, "linear": ROPE_LINEAR, "base": ROPE_BASE, "by_parts": ROPE_BY_PARTS}
+_ROPE_LAYOUTS = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
+_HEAD_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def rope_table(n_slots=None, rot=None, theta=10000.0, pos=None, scaling=None, magnitude=1.0, table=None, first_pair=0,
+               stream=None):
+    """geocache_rope_table: cosines and sines [n_slots, rot / 2, 2] f32 of the
+    rotation, for the positions 0 .. n_slots - 1 or those of `pos` (device int32
+    [n_slots]).  scaling: None, or {"kind": "linear" | "base", "factor": f}, or
+    {"kind": "by_parts", "factor": f, "original": trained context, "low": 1,
+    "high": 32}.  With `table` (device f32 [n_slots, row_pairs, 2]) the pairs
+    [first_pair, first_pair + rot / 2) of its rows are written."""
+    spec = dict(scaling or {})
+    kind = _ROPE_SCALINGS[spec.pop("kind", "plain")]
+    r = Rope(int(rot), float(theta), kind, float(spec.pop("factor", 1.0)), float(spec.pop("original", 0.0)),
+             float(spec.pop("low", 1.0)), float(spec.pop("high", 32.0)), float(magnitude))
+    if spec:
+        raise ValueError("unknown scaling parameters: %s" % ", ".join(sorted(spec)))
+    if n_slots is None:
+        n_slots = table.shape[0] if pos is None else pos.numel()
+    n = int(n_slots)
+    if table is None:
+        table = torch.empty((n, int(rot) // 2, 2), dtype=torch.float32, device="cuda" if pos is None else pos.device)
+    elif table.dim() != 3 or table.shape[0] != n or table.shape[2] != 2:
+        raise ValueError("table must be [n_slots, row_pairs, 2]")
+    _check(load().geocache_rope_table(ctypes.byref(r), _dev(pos, torch.int32, n, "pos"), n,
+                                      _dev(table, torch.float32, None, "table"), table.shape[1], int(first_pair),
+                                      _stream(stream)))
+    return table
+
+
+def _heads(t, dtype, T, H, D, name):
+    """A [T, H, D] view (elements of a head consecutive) as the C struct."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s (got %s)" % (name, dtype, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be on a CUDA device" % name)
+    if tuple(t.shape) != (T, H, D):
+        raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, T, H, D, list(t.shape)))
+    st = t.stride()
+    if st[2] != 1 and D > 1:
+        raise ValueError("the elements of a head of %s must be consecutive" % name)
+    return Heads(t.data_ptr(), st[0], st[1])
+
+
+def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps=1e-6, norm=True, layout="half",
+                 q_out=None, k_out=None, stream=None):
+    """geocache_qk_norm_rope: each head of q [T, Hq, D] and k [T, Hk, D] (f32,
+    bf16 or f16; any strides between tokens and heads) normalised and rotated by
+    table [n_slots, rot / 2, 2] at the tokens' slots (device int32 [T]; None:
+    token t has slot t).  k may be None.  Outputs are allocated when None and
+    may be the inputs themselves.  Returns (q_out, k_out)."""
+    T, Hq, D = q.shape
+    dt = q.dtype
+    if dt not in _HEAD_DTYPES:
+        raise TypeError("q must be float32, bfloat16 or float16 (got %s)" % dt)
+    Hk = 0 if k is None else k.shape[1]
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=dt, device=q.device)
+    if k is None:
+        hk = hko = None
+        if k_out is not None:
+            raise ValueError("k_out without k")
+    else:
+        if k_out is None:
+            k_out = torch.empty((T, Hk, D), dtype=dt, device=q.device)
+        hk, hko = _heads(k, dt, T, Hk, D, "k"), _heads(k_out, dt, T, Hk, D, "k_out")
+    n_slots = rot = 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [n_slots, rot / 2, 2]")
+        n_slots, rot = table.shape[0], 2 * table.shape[1]
+    f32 = torch.float32
+    _check(load().geocache_qk_norm_rope(
+        _heads(q, dt, T, Hq, D, "q"), hk, _heads(q_out, dt, T, Hq, D, "q_out"), hko, T, Hq, Hk, D, _HEAD_DTYPES[dt],
+        1 if norm else 0, float(eps), _dev(q_weight, f32, D, "q_weight"), _dev(k_weight, f32, D, "k_weight"),
+        _dev(table, f32, None, "table"), n_slots, rot, _ROPE_LAYOUTS[layout], _dev(slots, torch.int32, T, "slots"),
+        _stream(stream)))
+    return q_out, k_out
+
+
 def reconstruct(x_t, x0, x_next, recon: Recon, x0_store=None, stream=None):
     """geocache_reconstruct (full-step passthrough) on torch tensors."""
     n = x0.numel()
@@ -537,8 +640,8 @@ def transport_launches(a: int, N: int, mode: int, in_place: bool = False) -> int
 def device_status(stream=None):
     """geocache_device_status (synchronises, reads and clears the device
     status word): raises GeocacheError with ESHAPE (a sparse build overflowed
-    max_records), EINVAL (a record permutation entry or a mesh face index was
-    out of range) or ETIMEOUT (a kernel's bounded wait gave up) for what
+    max_records), EINVAL (a record permutation entry, a mesh face index or a
+    rotary slot was out of range) or ETIMEOUT (a kernel's bounded wait gave up) for what
     happened since the last check."""
     _check(load().geocache_device_status(_stream(stream)))
 
