@@ -496,6 +496,65 @@ int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, cons
                           int64_t n_slots, int rot, geocache_rope_layout layout, const int32_t* slots, void* stream);
 
 /* --------------------------------------------------------------------------
+ * Attention over packed sequences: the rows of all sequences (one for each
+ * asset) lie one after the other, sequence s has q_lens[s] queries and
+ * k_lens[s] keys and values.  For query i of a sequence, head h and key/value
+ * head h / (Hq / Hk):
+ *     lse_i = log sum_j exp(scale q_i . k_j),  out_i = sum_j exp(scale q_i . k_j - lse_i) v_j
+ * over the keys j that the query sees: all of its sequence, or with `causal`
+ * those with j <= i + k_lens[s] - q_lens[s] (the last query sees every key).
+ * A query that sees no key has out = 0 and lse = -inf.
+ *
+ * geocache_plan_attention -- how a launch divides the work; made once for the
+ * lengths of a batch and kept over layers and steps.  Host only.
+ *   q_lens, k_lens  host [n_seq], >= 0; each sum at most 2^31 - 1024.
+ *   n_ctas          thread blocks of a launch; 0 = the current device's SMs.
+ *   plan            receives the sizes below.
+ *   schedule        host buffer of schedule_bytes that receives the schedule,
+ *                   which the caller copies to the device (16-byte aligned);
+ *                   NULL: only `plan` is filled.
+ * Sizes: 0 <= n_seq, 1 <= Hk <= Hq <= 65536 with Hq % Hk == 0, D % 8 == 0,
+ * 8 <= D <= 128, 0 <= n_ctas <= 65536.
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE (a size out of range, or more work than
+ * the schedule can index or host memory holds), EDEVICE (no device to ask for
+ * its SMs).
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    int Hq, Hk, D, causal;
+    int n_ctas;               /* thread blocks of a launch */
+    int n_items, n_joins;     /* entries of the schedule: pieces of work; rows of tiles joined from several pieces */
+    int pack;                 /* query heads of one key/value head that share a tile's rows */
+    int64_t q_tokens, k_tokens;   /* sums of the lengths */
+    int64_t schedule_bytes;
+    int64_t workspace_bytes;  /* of a call; 0 when no work is split along the keys */
+} geocache_attention_plan;
+
+int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int Hq, int Hk, int D, int causal,
+                            int n_ctas, geocache_attention_plan* plan, void* schedule, int64_t schedule_bytes);
+
+/* --------------------------------------------------------------------------
+ * geocache_attention -- the attention of a plan.  dtype is BF16 or F16;
+ * scores, softmax statistics and sums are binary32, and the weights exp(...)
+ * are rounded to `dtype` for the product with the values.
+ *   schedule   device copy of the plan's schedule, 16-byte aligned.
+ *   q, out     [plan->q_tokens, Hq, D];  k, v  [plan->k_tokens, Hk, D].  Data
+ *              16-byte aligned, strides multiples of 8 elements.
+ *   lse        device [plan->q_tokens, Hq] f32, or NULL.
+ *   scale      > 0 and finite (1/sqrt(D) is usual).
+ *   workspace  device, plan->workspace_bytes (16-byte aligned; NULL when 0); its
+ *              contents need not be set, and calls that may overlap on the GPU
+ *              need one each.
+ * out must not overlap an input.  A NaN or infinity reaches the rows of its own
+ * sequence only: a key's through its scores, a value's also those rows of its
+ * sequence whose tile of queries sees the tile of 128 keys it lies in.
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE, EDTYPE, EALIAS, ECUDA; a wait inside the
+ * kernel that ran out sets the device status word (ETIMEOUT).
+ * ------------------------------------------------------------------------ */
+int geocache_attention(const geocache_attention_plan* plan, const void* schedule, const geocache_heads* q,
+                       const geocache_heads* k, const geocache_heads* v, const geocache_heads* out, float* lse,
+                       geocache_dtype dtype, double scale, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
  * geocache_is_full_step -- 1 if `step` (0 <= step < S) is a full step under
  * `sched`, 0 if cached, a negative status on bad arguments. Host only.
  * ------------------------------------------------------------------------ */
@@ -541,7 +600,8 @@ int geocache_device_status(void* stream);
  * (large steps in MASK mode, and in TABLE and GEOMETRY mode with one anchor, with
  * H*W % 8 == 0 and 16-byte aligned buffers; MASK steps of any size while
  * drop_first_copy is pending) waits for its shared-memory copies
- * with a time limit instead of spinning forever.
+ * with a time limit instead of spinning forever; so do the roles of
+ * geocache_attention's kernel for each other.
  *   limit_ns         limit of those waits for later calls (0 = the default, 2 s).
  *   drop_first_copy  nonzero: the next call that runs the staged kernel arms
  *                    none of the copies of its first unit (asset 0, view 0,
@@ -550,7 +610,9 @@ int geocache_device_status(void* stream);
  *                    status word (geocache_device_status then returns
  *                    GEOCACHE_ETIMEOUT) and returns without writing the
  *                    outputs of its units, and the context stays usable.  The
- *                    request is consumed by that call.
+ *                    request is consumed by that call.  A geocache_attention
+ *                    consumes it as well: its first thread block leaves its first
+ *                    copy of keys unissued and ends like that.
  * Process-wide, not thread safe.  Returns GEOCACHE_OK.
  * ------------------------------------------------------------------------ */
 int geocache_debug_set_wait(uint64_t limit_ns, int drop_first_copy);

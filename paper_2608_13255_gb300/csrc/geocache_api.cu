@@ -240,12 +240,13 @@ int geocache_last_launches(void) { return g_launches; }
 int geocache_abi_version(void) { return GEOCACHE_ABI_VERSION; }
 
 int geocache_device_status(void* stream) {
-    unsigned int word = 0, raster_word = 0, rope_word = 0;
+    unsigned int word = 0, raster_word = 0, rope_word = 0, attention_word = 0;
     cudaError_t e = geocache::read_device_error(&word, true, (cudaStream_t)stream);
     if (e == cudaSuccess) e = geocache::read_raster_error(&raster_word, true, (cudaStream_t)stream);
     if (e == cudaSuccess) e = geocache::read_rope_error(&rope_word, true, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = geocache::read_attention_error(&attention_word, true, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "reading the device status word");
-    word |= raster_word | rope_word;
+    word |= raster_word | rope_word | attention_word;
     if (word & 2u)
         return fail(GEOCACHE_ESHAPE, "a sparse-form build had more records than max_records (status word 0x%x); "
                                      "query geocache_corr_record_count and rebuild", word);
@@ -680,6 +681,75 @@ int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, cons
     a.eps = (float)eps;
     a.dtype = dtype;
     cudaError_t e = geocache::launch_norm_rope(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, fn);
+    return ok();
+}
+
+int geocache_attention(const geocache_attention_plan* p, const void* schedule, const geocache_heads* q,
+                       const geocache_heads* k, const geocache_heads* v, const geocache_heads* out, float* lse,
+                       geocache_dtype dtype, double scale, void* workspace, int64_t workspace_bytes, void* stream) {
+    const char* fn = "geocache_attention";
+    g_launches = 0;
+    if (!p) return fail(GEOCACHE_EINVAL, "%s: plan is NULL", fn);
+    if (dtype != GEOCACHE_BF16 && dtype != GEOCACHE_F16) return fail(GEOCACHE_EDTYPE, "%s: unsupported dtype %d", fn, (int)dtype);
+    if (!(scale > 0.0) || !((float)scale > 0.0f) || !std::isfinite((float)scale))
+        return fail(GEOCACHE_EINVAL, "%s: scale=%g must be positive", fn, scale);
+    if (p->Hk < 1 || p->Hq < p->Hk || p->Hq > 65536 || p->Hq % p->Hk || p->D < 8 || p->D > 128 || p->D % 8 ||
+        p->pack < 1 || p->pack > 128 || (p->Hq / p->Hk) % p->pack || p->n_ctas < 1 || p->n_ctas > 65536 || p->n_items < 0 ||
+        p->n_joins < 0 || p->q_tokens < 0 || p->q_tokens > geocache::kAttentionTokens || p->k_tokens < 0 || p->k_tokens > geocache::kAttentionTokens ||
+        p->workspace_bytes < 0 || p->workspace_bytes % geocache::attention_slot_bytes(p->D) ||
+        p->schedule_bytes != geocache::attention_items_at(p->n_ctas) + 64LL * p->n_items + 32LL * p->n_joins)
+        return fail(GEOCACHE_ESHAPE, "%s: not a plan of geocache_plan_attention", fn);
+    if (p->q_tokens == 0) return ok();
+    if (!schedule || ((uintptr_t)schedule & 15)) return fail(GEOCACHE_EINVAL, "%s: schedule must be given and 16-byte aligned", fn);
+    if (p->workspace_bytes && (!workspace || workspace_bytes < p->workspace_bytes))
+        return fail(GEOCACHE_EINVAL, "%s: the plan needs a workspace of %lld bytes", fn, (long long)p->workspace_bytes);
+    if (p->workspace_bytes && ((uintptr_t)workspace & 15)) return fail(GEOCACHE_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+    if ((uintptr_t)lse & 3) return fail(GEOCACHE_EINVAL, "%s: lse must be 4-byte aligned", fn);
+    const geocache_heads* x[4] = {q, k, v, out};
+    const char* name[4] = {"q", "k", "v", "out"};
+    for (int i = 0; i < 4; ++i) {
+        const bool keys = i == 1 || i == 2;
+        if (keys && p->k_tokens == 0) continue;
+        const int st = check_heads(x[i], keys ? p->k_tokens : p->q_tokens, keys ? p->Hk : p->Hq, p->D, 2, i == 3, fn, name[i]);
+        if (st) return st;
+        if (((uintptr_t)x[i]->data & 15) || x[i]->token_stride % 8 || x[i]->head_stride % 8)
+            return fail(GEOCACHE_EINVAL, "%s: %s must be 16-byte aligned with strides that are multiples of 8 elements", fn, name[i]);
+    }
+    const size_t wb = (size_t)p->workspace_bytes, lb = lse ? (size_t)p->q_tokens * p->Hq * 4 : 0, sb = (size_t)p->schedule_bytes;
+    for (int i = 0; i < 3; ++i) {
+        const bool keys = i > 0;
+        const int64_t n = keys ? p->k_tokens : p->q_tokens;
+        const int H = keys ? p->Hk : p->Hq;
+        if (n == 0) continue;
+        if (heads_overlap(out, p->q_tokens, p->Hq, x[i], n, H, p->D, 2))
+            return fail(GEOCACHE_EALIAS, "%s: out overlaps %s", fn, name[i]);
+        if (heads_overlap_bytes(x[i], n, H, p->D, 2, workspace, wb) || heads_overlap_bytes(x[i], n, H, p->D, 2, lse, lb))
+            return fail(GEOCACHE_EALIAS, "%s: workspace or lse overlaps %s", fn, name[i]);
+    }
+    if (heads_overlap_bytes(out, p->q_tokens, p->Hq, p->D, 2, workspace, wb) ||
+        heads_overlap_bytes(out, p->q_tokens, p->Hq, p->D, 2, lse, lb) ||
+        heads_overlap_bytes(out, p->q_tokens, p->Hq, p->D, 2, schedule, sb) || overlap(workspace, wb, lse, lb) ||
+        overlap(schedule, sb, workspace, wb) || overlap(schedule, sb, lse, lb))
+        return fail(GEOCACHE_EALIAS, "%s: out, lse, workspace and schedule overlap", fn);
+    geocache::AttentionArgs a{};
+    const char* base = static_cast<const char*>(schedule);
+    a.cta_ptr = reinterpret_cast<const int32_t*>(base);
+    a.items = reinterpret_cast<const geocache::AttentionItem*>(base + geocache::attention_items_at(p->n_ctas));
+    a.joins = reinterpret_cast<const geocache::AttentionJoin*>(a.items + p->n_items);
+    a.n_ctas = p->n_ctas; a.n_joins = p->n_joins; a.pack = p->pack;
+    a.D = p->D; a.Hq = p->Hq; a.Hk = p->Hk; a.causal = p->causal; a.dtype = dtype;
+    a.q_tokens = p->q_tokens; a.k_tokens = p->k_tokens;
+    a.n_slots = p->workspace_bytes / geocache::attention_slot_bytes(p->D);
+    a.q = *q; a.out = *out;
+    if (p->k_tokens) { a.k = *k; a.v = *v; }
+    a.lse = lse;
+    a.scale = (float)scale;
+    a.parts = static_cast<float*>(workspace);
+    a.part_lse = a.parts ? a.parts + a.n_slots * 128 * p->D : nullptr;
+    a.wait_limit_ns = geocache::debug_wait_limit_ns();
+    a.drop_first_copy = geocache::take_drop_first_copy();
+    cudaError_t e = geocache::launch_attention(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, fn);
     return ok();
 }

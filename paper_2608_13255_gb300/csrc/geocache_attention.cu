@@ -1,0 +1,671 @@
+// Attention over packed sequences on the tensor cores (tcgen05), planned by geocache_plan_attention.
+//
+// A thread block takes its pieces of the schedule one after the other.  A piece is one or two tiles of 128 query rows
+// against a run of 128-key tiles; the two tiles share every load of keys and values and take turns, so that the tensor
+// cores work on one while the other's softmax runs:
+//   warp 9      loads queries (once a piece), keys and values (a ring of stages) by TMA;
+//   warp 8      issues the products: S = Q K^T into tensor memory, and O += P V with P read from tensor memory;
+//   warps 0-3   softmax of tile 0, one row a thread: S from tensor memory, the running maximum and sum in registers,
+//   warps 4-7   the same of tile 1;   P = exp2((S - m) scale log2 e) written over S as 16-bit pairs.
+// O stays in tensor memory over the whole piece.  It is rescaled only when a row's maximum has grown by more than 8
+// powers of two since the last time: until then the sums and P (at most 2^8) are kept relative to the old maximum,
+// which changes no result beyond rounding.  S, the statistics and O are binary32; P is rounded to the inputs' type, as
+// the product with the values needs, while its sum is taken before that rounding.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "geocache.h"
+#include "geocache_device.cuh"
+#include "geocache_internal.h"
+
+namespace geocache {
+
+namespace {
+
+// Status word of this file's kernels (bit 1: a wait ran out); read by geocache_device_status.
+__device__ unsigned int g_attention_error = 0;
+
+constexpr int kRows = kAttentionRows, kKeys = kAttentionKeys;
+constexpr int kThreads = 320;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr uint32_t kTmemColumns = 512;  // S of the two tiles at 0 and 128, O at 256 and 384
+constexpr uint32_t kBox = 128 * 128;    // bytes of 128 rows of 64 elements (one swizzled box)
+
+template <int DP>
+struct Shape {  // heads padded to DP = 64 or 128 elements
+    static constexpr int kBoxes = DP / 64;
+    static constexpr uint32_t kTileBytes = kBoxes * kBox;
+    static constexpr int kStages = DP == 128 ? 5 : 8;
+    static constexpr uint32_t kBytes = (2 + kStages) * kTileBytes + 1024;  // and room to align to 1024
+};
+
+struct Barriers {
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], drained;
+    uint64_t kv_full[8], kv_empty[8];
+    uint32_t tmem;
+    uint32_t dead;
+};
+
+// ------------------------------------------------------------------ PTX --
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long globaltimer() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for a phase, with the lanes of `mask` together and all with one answer.  False when the limit passed, or when
+// another role of the block has given up: the roles then leave their loops one after the other.
+__device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b,
+                                            uint32_t mask) {
+    const unsigned long long t0 = globaltimer();
+    while (!__all_sync(mask, mbar_try(bar, parity))) {
+        const bool late = globaltimer() - t0 > limit_ns;
+        if (__any_sync(mask, late || *(volatile uint32_t*)&b->dead)) {
+            if (late) {
+                *(volatile uint32_t*)&b->dead = 1;
+                atomicOr(&g_attention_error, 1u);
+            }
+            return false;
+        }
+    }
+    return true;
+}
+constexpr uint32_t kWarpMask = 0xffffffffu, kLane0 = 1u;
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b,
+                                          uint32_t mask = kWarpMask) {
+    return __all_sync(mask, mbar_try(bar, parity)) || mbar_wait_slow(bar, parity, limit_ns, b, mask);
+}
+
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+        "[%6];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+        : "memory");
+}
+
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// D (tensor memory) = A B (+ D), A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// the same with A in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+// The registers of a load are operands of the wait (or of an empty statement behind it), so that no use of them can be
+// moved before it.
+#define GEOCACHE_PIN16(r) \
+    "+r"((r)[0]), "+r"((r)[1]), "+r"((r)[2]), "+r"((r)[3]), "+r"((r)[4]), "+r"((r)[5]), "+r"((r)[6]), "+r"((r)[7]), "+r"((r)[8]), \
+        "+r"((r)[9]), "+r"((r)[10]), "+r"((r)[11]), "+r"((r)[12]), "+r"((r)[13]), "+r"((r)[14]), "+r"((r)[15])
+__device__ __forceinline__ void tmem_pin32(uint32_t* r) {
+    asm volatile("" : GEOCACHE_PIN16(r));
+    asm volatile("" : GEOCACHE_PIN16(r + 16));
+}
+__device__ __forceinline__ void tmem_wait_ld(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    tmem_pin32(r);
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// two floats as a pair of 16-bit values, `lo` in the low half
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Shared-memory operand descriptor: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lead` is the distance of
+// 64-element blocks along the contiguous axis (used where that axis is not the summed one).
+__device__ __forceinline__ uint64_t smem_desc(uint32_t at, uint32_t lead) {
+    return (uint64_t)((at >> 4) & 0x3fff) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+
+struct Params {
+    AttentionArgs a;
+    int tok;              // tokens of a tile
+    int k_steps;          // of 16 elements of a head
+    uint32_t qk_idesc, pv_idesc;
+    float c;              // scale * log2(e)
+};
+
+__device__ __forceinline__ void load_item(const AttentionItem* p, AttentionItem& it) {
+    const int4* s = reinterpret_cast<const int4*>(p);
+    int4* d = reinterpret_cast<int4*>(&it);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) d[i] = s[i];
+}
+
+// ---------------------------------------------------------------- roles --
+// Each role walks the block's pieces with its own count of the phases; a wait that gives up ends it.
+template <int DP>
+__device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensorMap* km, const CUtensorMap* vm, uint32_t smem,
+                          Barriers* b, int first, int last) {
+    using S = Shape<DP>;
+    const unsigned long long limit = p.a.wait_limit_ns;
+    const uint32_t q_bytes = S::kBoxes * 128u * p.a.pack * p.tok;
+    uint32_t stage = 0, phase = 0, q_n[2] = {0, 0}, armed = 0;
+    bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
+    for (int i = first; i < last && ok; ++i) {
+        AttentionItem it;
+        load_item(p.a.items + i, it);
+        const int n = max(it.n_kv[0], it.n_kv[1]);
+        auto queries = [&](int t) {
+            if (!it.n_tok[t] || !it.n_kv[t]) return true;
+            if (!mbar_wait(&b->q_empty[t], (q_n[t] & 1) ^ 1, limit, b, kLane0)) return false;
+            mbar_expect(&b->q_full[t], q_bytes);
+#pragma unroll
+            for (int x = 0; x < S::kBoxes; ++x)
+                tma_4d(smem + t * S::kTileBytes + x * kBox, qm, 64 * x, 0, it.head / p.a.pack, it.q_row + t * p.tok, &b->q_full[t]);
+            ++q_n[t];
+            return true;
+        };
+        auto keys = [&](const CUtensorMap* map, int j) {
+            if (!mbar_wait(&b->kv_empty[stage], phase ^ 1, limit, b, kLane0)) return false;
+            if (!drop) {
+                mbar_expect(&b->kv_full[stage], S::kTileBytes);
+#pragma unroll
+                for (int x = 0; x < S::kBoxes; ++x)
+                    tma_3d(smem + (2 + stage) * S::kTileBytes + x * kBox, map, 64 * x, it.kv_head, it.kv_row + j * kKeys,
+                           &b->kv_full[stage]);
+                armed |= 1u << stage;
+            }
+            drop = false;
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+            return true;
+        };
+        if (!queries(0)) break;
+        for (int j = 0; j < n; ++j) {
+            ok = keys(km, j);
+            if (ok && j == 0) ok = queries(1);
+            if (ok) ok = keys(vm, j);
+            if (!ok) break;
+        }
+    }
+    if (!*(volatile uint32_t*)&b->dead) return;
+    // given up: the copies in flight land before the block ends (their last phases, waited for with the same limit)
+    const unsigned long long t0 = globaltimer();
+    for (int t = 0; t < 2; ++t)
+        while (q_n[t] && !mbar_try(&b->q_full[t], (q_n[t] & 1) ^ 1) && globaltimer() - t0 < limit) {}
+    for (uint32_t s = 0; s < S::kStages; ++s) {
+        // stages below `stage` were last armed in this round, the others in the one before
+        const uint32_t parity = s < stage ? phase : phase ^ 1;
+        while ((armed >> s & 1) && !mbar_try(&b->kv_full[s], parity) && globaltimer() - t0 < limit) {}
+    }
+}
+
+template <int DP>
+__device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, int first, int last, int lane) {
+    using S = Shape<DP>;
+    const unsigned long long limit = p.a.wait_limit_ns;
+    uint32_t stage = 0, phase = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
+    auto advance = [&]() {
+        if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+    };
+    auto qk = [&](int t, uint32_t at) {
+        if (lane == 0) {
+            const uint32_t q = smem + t * S::kTileBytes;
+            for (int s = 0; s < p.k_steps; ++s) {
+                const uint32_t off = (s >> 2) * kBox + (s & 3) * 32;
+                mma_ss(tmem + t * 128, smem_desc(q + off, 16), smem_desc(at + off, 16), p.qk_idesc, s > 0);
+            }
+            tc_commit(&b->s_full[t]);
+        }
+        __syncwarp();
+    };
+    for (int i = first; i < last; ++i) {
+        AttentionItem it;
+        load_item(p.a.items + i, it);
+        const int n = max(it.n_kv[0], it.n_kv[1]);
+        for (int j = -1; j < n; ++j) {
+            // values of tile j, then keys of tile j + 1, lie in consecutive stages
+            uint32_t v_stage = 0, k_stage = 0;
+            bool have_v = false, have_k = false;
+            int v_steps = kKeys / 16;
+            if (j >= 0) v_stage = stage, advance();
+            const uint32_t v_phase = v_stage < stage || j < 0 ? phase : phase ^ 1;
+            if (j + 1 < n) k_stage = stage, advance();
+            const uint32_t k_phase = j + 1 < n && k_stage < stage ? phase : phase ^ 1;
+            const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (!it.n_tok[t]) continue;
+                if (j >= 0 && j < it.n_kv[t]) {
+                    if (!have_v) {
+                        if (!mbar_wait(&b->kv_full[v_stage], v_phase, limit, b)) return;
+                        const int keys = it.n_keys - j * kKeys;
+                        if (keys < kKeys) {
+                            // what lies behind the sequence's last key is another's: the rest of the last step of 16
+                            // keys is cleared, so that 0 * v is 0 whatever it holds, and later steps are left out
+                            v_steps = (keys + 15) / 16;
+                            const int words = (v_steps * 16 - keys) * 8;
+                            for (int x = 0; x < S::kBoxes; ++x)
+                                for (int w = lane; w < words; w += 32)
+                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + x * kBox + keys * 128 + w * 16),
+                                                 "r"(0)
+                                                 : "memory");
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                        }
+                        have_v = true;
+                    }
+                    if (!mbar_wait(&b->p_full[t], p_n[t]++ & 1, limit, b)) return;
+                    tc_after();
+                    if (lane == 0)
+                        for (int s = 0; s < v_steps; ++s)
+                            mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, smem_desc(v_at + s * 2048, kBox), p.pv_idesc,
+                                   j > 0 || s > 0);
+                    if (j + 1 == it.n_kv[t] && lane == 0) tc_commit(&b->o_full[t]);
+                    __syncwarp();
+                }
+                if (j + 1 < it.n_kv[t]) {
+                    if (j < 0 && !mbar_wait(&b->q_full[t], q_n[t]++ & 1, limit, b)) return;
+                    if (!have_k && !mbar_wait(&b->kv_full[k_stage], k_phase, limit, b)) return;
+                    have_k = true;
+                    tc_after();
+                    qk(t, k_at);
+                    if (j + 2 == it.n_kv[t] && lane == 0) tc_commit(&b->q_empty[t]);
+                }
+            }
+            if (lane == 0) {
+                if (j >= 0) tc_commit(&b->kv_empty[v_stage]);
+                if (j + 1 < n) tc_commit(&b->kv_empty[k_stage]);
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// 8 columns of a row of O
+template <typename T>
+__device__ __forceinline__ void store8(T* out, const uint32_t* o, float inv) {
+    uint4 w;
+    uint32_t* r = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+    *reinterpret_cast<uint4*>(out) = w;
+}
+
+template <int DP, typename T>
+__device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int first, int last, int t, int warp, int lane) {
+    const unsigned long long limit = p.a.wait_limit_ns;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+    const int row = warp * 32 + lane, tok = row / p.a.pack, head = row - tok * p.a.pack;
+    uint32_t s_n = 0, o_n = 0;
+    for (int i = first; i < last; ++i) {
+        AttentionItem it;
+        load_item(p.a.items + i, it);
+        const int n_tok = t ? it.n_tok[1] : it.n_tok[0], n = t ? it.n_kv[1] : it.n_kv[0], slot = t ? it.slot[1] : it.slot[0];
+        if (!n_tok) continue;
+        const bool active = tok < n_tok, warp_active = warp * 32 < n_tok * p.a.pack;
+        const int sees = p.a.causal ? min(it.n_keys, it.sees + t * p.tok + tok) : it.n_keys;
+        float m = -INFINITY, l = 0.0f;
+        for (int j = 0; j < n; ++j) {
+            if (!mbar_wait(&b->s_full[t], s_n++ & 1, limit, b)) return;
+            tc_after();
+            if (warp_active) {
+                uint32_t s[128];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) tmem_ld32(s_at + 32 * x, s + 32 * x);
+                tmem_wait_ld(s);
+#pragma unroll
+                for (int x = 1; x < 4; ++x) tmem_pin32(s + 32 * x);
+                const int here = sees - j * kKeys;
+                if (__any_sync(0xffffffffu, here < kKeys)) {
+#pragma unroll
+                    for (int x = 0; x < 128; ++x)
+                        if (x >= here) s[x] = 0xff800000u;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 128; ++x) top = fmaxf(top, __uint_as_float(s[x]));
+                if (j == 0) {
+                    m = top;
+                } else if (const bool grown = (top - m) * p.c > 8.0f; __any_sync(0xffffffffu, grown)) {
+                    // O and the sum follow the larger maximum (the product into O is complete: S came after it); each
+                    // row by its own scores alone, so that its result does not depend on the rows beside it
+                    const float f = grown ? exp2_fast((m - top) * p.c) : 1.0f;
+                    if (grown) m = top;
+                    l *= f;
+#pragma unroll 1
+                    for (int x = 0; x < p.a.D; x += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_at + x, o);
+                        tmem_wait_ld(o);
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+                        tmem_st32(o_at + x, o);
+                    }
+                }
+                const float base = m == -INFINITY ? 0.0f : m * p.c;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) {
+                        const float e0 = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * x]), p.c, -base));
+                        const float e1 = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * x + 1]), p.c, -base));
+                        sum[2 * (x & 1)] += e0;
+                        sum[2 * (x & 1) + 1] += e1;
+                        w[x] = pack2<T>(e0, e1);
+                    }
+                    tmem_st32(s_at + 32 * h, w);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_wait_st();
+            }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&b->p_full[t]);
+        }
+        if (n && !mbar_wait(&b->o_full[t], o_n++ & 1, limit, b)) return;
+        tc_after();
+        if (!warp_active) continue;
+        const long long token = (long long)it.q_row + t * p.tok + tok;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float lse = l == 0.0f ? -INFINITY : m * p.a.scale + logf(l);
+        T* out = static_cast<T*>(p.a.out.data) + token * p.a.out.token_stride + (it.head + head) * p.a.out.head_stride;
+        const long long part = (long long)slot * kRows + row;
+#pragma unroll 1
+        for (int x = 0; x < p.a.D; x += 32) {
+            uint32_t o[32];
+            if (n) {
+                tmem_ld32(o_at + x, o);
+                tmem_wait_ld(o);
+            } else {
+#pragma unroll
+                for (int y = 0; y < 32; ++y) o[y] = 0;
+            }
+            if (active && slot < 0) {
+#pragma unroll
+                for (int y = 0; y < 32; y += 8)
+                    if (x + y < p.a.D) store8<T>(out + x + y, o + y, inv);
+            } else if (active) {
+                float* dst = p.a.parts + part * p.a.D + x;
+#pragma unroll
+                for (int y = 0; y < 32; y += 4)
+                    if (x + y < p.a.D)
+                        *reinterpret_cast<float4*>(dst + y) =
+                            make_float4(__uint_as_float(o[y]) * inv, __uint_as_float(o[y + 1]) * inv,
+                                        __uint_as_float(o[y + 2]) * inv, __uint_as_float(o[y + 3]) * inv);
+            }
+            __syncwarp();
+        }
+        if (active) {
+            if (slot >= 0)
+                p.a.part_lse[part] = lse;
+            else if (p.a.lse)
+                p.a.lse[token * p.a.Hq + it.head + head] = lse;
+        }
+        tc_before();
+    }
+}
+
+template <int DP, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    attention_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap qm,
+                     const __grid_constant__ CUtensorMap km, const __grid_constant__ CUtensorMap vm) {
+    extern __shared__ uint8_t raw[];
+    __shared__ Barriers bars;
+    Barriers* b = &bars;
+    const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&b->q_full[t], 1);
+            mbar_init(&b->q_empty[t], 1);
+            mbar_init(&b->s_full[t], 1);
+            mbar_init(&b->p_full[t], 4);
+            mbar_init(&b->o_full[t], 1);
+        }
+        mbar_init(&b->drained, 1);
+        for (int s = 0; s < 8; ++s) {
+            mbar_init(&b->kv_full[s], 1);
+            mbar_init(&b->kv_empty[s], 1);
+        }
+        b->dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(kTmemColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = b->tmem;
+    pdl_wait();
+    const int first = p.a.cta_ptr[blockIdx.x], last = p.a.cta_ptr[blockIdx.x + 1];
+    if (warp == kLoadWarp) {
+        if (lane == 0) load_role<DP>(p, &qm, &km, &vm, smem, b, first, last);
+    } else if (warp == kMmaWarp) {
+        mma_role<DP>(p, smem, tmem, b, first, last, lane);
+        // every product and every arrival that it announced is done before the block ends
+        if (lane == 0) {
+            tc_commit(&b->drained);
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try(&b->drained, 0) && globaltimer() - t0 < p.a.wait_limit_ns) {}
+        }
+        __syncwarp();
+    } else {
+        softmax_role<DP, T>(p, tmem, b, first, last, warp >> 2, warp & 3, lane);
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == kMmaWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
+}
+
+// Joins the parts of rows split along the keys, in their order: a warp takes a row, a lane four of its columns.
+template <typename T>
+__global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ Params p) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_wait();
+    const AttentionJoin join = p.a.joins[blockIdx.x];
+    for (int row = blockIdx.y * 8 + warp; row < join.n_tok * p.a.pack; row += gridDim.y * 8) {
+        const int tok = row / p.a.pack, head = join.head + row - tok * p.a.pack;
+        const float* lse = p.a.part_lse + (long long)join.slot * kRows + row;
+        float top = -INFINITY;
+        for (int i = 0; i < join.n_parts; ++i) {
+            const float x = lse[(long long)i * kRows];
+            top = x > top || x != x ? x : top;  // a NaN stays
+        }
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float sum = 0.0f;
+        if (top != -INFINITY)
+            for (int i = 0; i < join.n_parts; ++i) {
+                const float w = expf(lse[(long long)i * kRows] - top);
+                sum += w;
+                if (4 * lane < p.a.D) {
+                    const float4 x =
+                        *reinterpret_cast<const float4*>(p.a.parts + (((long long)join.slot + i) * kRows + row) * p.a.D + 4 * lane);
+                    o.x = fmaf(w, x.x, o.x);
+                    o.y = fmaf(w, x.y, o.y);
+                    o.z = fmaf(w, x.z, o.z);
+                    o.w = fmaf(w, x.w, o.w);
+                }
+            }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const long long token = (long long)join.q_row + tok;
+        if (4 * lane < p.a.D) {
+            T* out = static_cast<T*>(p.a.out.data) + token * p.a.out.token_stride + head * p.a.out.head_stride + 4 * lane;
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+        }
+        if (lane == 0 && p.a.lse) p.a.lse[token * p.a.Hq + head] = sum == 0.0f ? -INFINITY : top + logf(sum);
+    }
+}
+
+// ----------------------------------------------------------------- host --
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// Boxes of 64 elements of a head x `heads` heads x `tokens` tokens.  The stride of an axis of one entry is never used
+// but has to be a valid one.
+cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_heads& x, int D, int pack, int H, long long T, int tokens) {
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t row = (cuuint64_t)D * 2, hs = H > 1 ? x.head_stride * 2 : row, ts = T > 1 ? x.token_stride * 2 : row;
+    const CUtensorMapDataType type = dtype == GEOCACHE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUresult r;
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    if (pack > 0) {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)pack, (cuuint64_t)(H / pack), (cuuint64_t)T};
+        const cuuint64_t strides[3] = {hs, H / pack > 1 ? hs * pack : row, ts};
+        const cuuint32_t box[4] = {64, (cuuint32_t)pack, 1, (cuuint32_t)tokens};
+        r = encode(map, type, 4, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else {
+        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)T};
+        const cuuint64_t strides[2] = {hs, ts};
+        const cuuint32_t box[3] = {64, 1, (cuuint32_t)tokens};
+        r = encode(map, type, 3, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    }
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int DP, typename T>
+cudaError_t launch(const Params& p, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t s) {
+    auto kern = attention_kernel<DP, T>;
+    static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kBytes);
+    if (ready != cudaSuccess) return ready;
+    cudaError_t e = launch_pdl(kern, dim3((unsigned)p.a.n_ctas), kThreads, Shape<DP>::kBytes, s, p, qm, km, vm);
+    if (e != cudaSuccess || p.a.n_joins == 0) return e;
+    // a block for every 8 rows of a tile while that leaves the device room for them at once
+    const int rows = p.tok * p.a.pack, per = p.a.n_joins > 1024 ? 4 : 1;
+    return launch_pdl(attention_join_kernel<T>, dim3((unsigned)p.a.n_joins, (unsigned)((rows + 8 * per - 1) / (8 * per))), 256, 0, s, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s) {
+    Params p{};
+    p.a = a;
+    p.tok = kRows / a.pack;
+    p.k_steps = (a.D + 15) / 16;
+    // kind f16: binary32 accumulators, operands of `dtype`, 128 rows; the keys' head axis and the queries' are summed
+    // (contiguous), the values' is not
+    const uint32_t type = a.dtype == GEOCACHE_BF16 ? 1 : 0;
+    const uint32_t idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(kRows >> 4) << 24;
+    p.qk_idesc = idesc | (uint32_t)(kKeys >> 3) << 17;
+    p.pv_idesc = idesc | 1u << 16 | (uint32_t)(2 * p.k_steps) << 17;
+    p.c = (float)((double)a.scale * 1.4426950408889634);
+    CUtensorMap qm, km, vm;
+    cudaError_t e = make_map(&qm, a.dtype, a.q, a.D, a.pack, a.Hq, a.q_tokens, p.tok);
+    if (e != cudaSuccess) return e;
+    if (a.k_tokens) {
+        e = make_map(&km, a.dtype, a.k, a.D, 0, a.Hk, a.k_tokens, kKeys);
+        if (e == cudaSuccess) e = make_map(&vm, a.dtype, a.v, a.D, 0, a.Hk, a.k_tokens, kKeys);
+        if (e != cudaSuccess) return e;
+    } else {
+        km = vm = qm;  // no key is loaded
+    }
+    if (a.dtype == GEOCACHE_BF16)
+        return a.D > 64 ? launch<128, __nv_bfloat16>(p, qm, km, vm, s) : launch<64, __nv_bfloat16>(p, qm, km, vm, s);
+    return a.D > 64 ? launch<128, __half>(p, qm, km, vm, s) : launch<64, __half>(p, qm, km, vm, s);
+}
+
+cudaError_t read_attention_error(unsigned int* out, bool clear, cudaStream_t s) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(out, g_attention_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
+    if (e != cudaSuccess) return e;
+    e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess || !clear || *out == 0) return e;
+    static const unsigned int zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_attention_error, &zero, sizeof(unsigned int), 0, cudaMemcpyHostToDevice, s);
+    if (e != cudaSuccess) return e;
+    return cudaStreamSynchronize(s);
+}
+
+}  // namespace geocache

@@ -1,0 +1,307 @@
+// How an attention launch divides its work (host only).
+//
+// A unit of work is one or two tiles of 128 query rows over the key tiles that they see.  Units go to thread blocks
+// whole, the longest first to the block with the least (no joins), or in order with the boundaries between the
+// blocks falling where the costs are even, which splits units along the keys; their parts are joined by a second
+// kernel.  Both are laid out, with one and with two tiles a unit, and the cheapest by the model below is kept.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <exception>
+#include <numeric>
+#include <queue>
+#include <vector>
+
+#include "geocache.h"
+#include "geocache_internal.h"
+
+namespace {
+
+using geocache::AttentionItem;
+using geocache::AttentionJoin;
+constexpr int kRows = geocache::kAttentionRows, kKeys = geocache::kAttentionKeys;
+
+// Nanoseconds: a key tile for two query tiles, for one, a piece's start and end, and a launch that joins.
+struct Cost {
+    double two, one, start, join, join_slot;
+};
+
+Cost cost_of(int D) {
+    if (D > 64) return {1250.0, 900.0, 2500.0, 4000.0, 0.02};
+    return {850.0, 650.0, 2200.0, 4000.0, 0.02};
+}
+
+struct Unit {
+    int seq, head, kv_head;
+    int token;        // first token of the sequence's queries
+    int n_tok[2];
+    int n_kv[2];      // key tiles each sees
+    int most() const { return std::max(n_kv[0], n_kv[1]); }
+    // cost of the key tiles [a, b)
+    double cost(const Cost& c, int a, int b) const {
+        const int both = std::min(n_tok[1] ? std::min(n_kv[0], n_kv[1]) : 0, b);
+        const int pairs = std::max(0, both - a);
+        return pairs * c.two + (b - a - pairs) * c.one;
+    }
+};
+
+struct Piece {
+    int unit, from, to;
+};
+
+struct Layout {
+    int tiles = 0;
+    std::vector<Unit> units;
+    std::vector<std::vector<Piece>> of_cta;
+    double cost = 0.0;
+};
+
+struct Problem {
+    const int32_t *q, *k;
+    int n_seq, Hq, Hk, D, causal, n_ctas, pack;
+};
+
+std::vector<Unit> make_units(const Problem& p, int tiles) {
+    const int tok = kRows / p.pack, groups = p.Hq / p.Hk / p.pack;
+    std::vector<Unit> units;
+    for (int s = 0; s < p.n_seq; ++s)
+        for (int hk = 0; hk < p.Hk; ++hk)
+            for (int g = 0; g < groups; ++g)
+                for (long long t = 0; t < p.q[s]; t += (long long)tok * tiles) {
+                    Unit u{s, hk * (p.Hq / p.Hk) + g * p.pack, hk, (int)t, {0, 0}, {0, 0}};
+                    for (int i = 0; i < tiles; ++i) {
+                        const long long first = t + (long long)i * tok;
+                        u.n_tok[i] = (int)std::max(0LL, std::min<long long>(tok, p.q[s] - first));
+                        if (!u.n_tok[i]) continue;
+                        long long sees = p.k[s];
+                        if (p.causal) sees = std::max(0LL, first + u.n_tok[i] + p.k[s] - p.q[s]);
+                        u.n_kv[i] = (int)((sees + kKeys - 1) / kKeys);
+                    }
+                    units.push_back(u);
+                }
+    return units;
+}
+
+// whole units, the longest first, each to the block with the least
+void assign_whole(const Problem& p, const Cost& c, Layout& l) {
+    std::vector<double> cost(l.units.size());
+    for (size_t i = 0; i < cost.size(); ++i) cost[i] = c.start + l.units[i].cost(c, 0, l.units[i].most());
+    std::vector<int> order(l.units.size());
+    std::iota(order.begin(), order.end(), 0);
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return cost[a] > cost[b]; });
+    using Load = std::pair<double, int>;
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+    for (int i = 0; i < p.n_ctas; ++i) least.push({0.0, i});
+    l.of_cta.assign(p.n_ctas, {});
+    for (int i : order) {
+        Load x = least.top();
+        least.pop();
+        l.of_cta[x.second].push_back({i, 0, l.units[i].most()});
+        x.first += cost[i];
+        l.cost = std::max(l.cost, x.first);
+        least.push(x);
+    }
+}
+
+// units in order, cut where the blocks' costs are even
+void assign_even(const Problem& p, const Cost& c, Layout& l) {
+    double total = 0.0;
+    for (const Unit& u : l.units) total += c.start + u.cost(c, 0, u.most());
+    l.of_cta.assign(p.n_ctas, {});
+    const double share = (total + (p.n_ctas - 1) * c.start) / p.n_ctas;
+    int cta = 0;
+    double load = 0.0, slots = 0.0;
+    for (size_t i = 0; i < l.units.size(); ++i) {
+        const Unit& u = l.units[i];
+        const int n = u.most();
+        int at = 0;
+        do {
+            int take = n - at;
+            const double left = share - load - c.start;
+            if (cta < p.n_ctas - 1 && u.cost(c, at, n) > left) {
+                // the key tiles that fit, to the nearest; a rest of under half a piece's start stays here
+                int fit = 0;
+                double sum = 0.0;
+                while (at + fit < n) {
+                    const double next = u.cost(c, at + fit, at + fit + 1);
+                    if (sum + 0.5 * next > left) break;
+                    sum += next;
+                    ++fit;
+                }
+                if (u.cost(c, at + fit, n) > 0.5 * c.start) take = load == 0.0 ? std::max(fit, 1) : fit;
+            }
+            if (take > 0 || n == 0) {
+                l.of_cta[cta].push_back({(int)i, at, at + take});
+                load += c.start + u.cost(c, at, at + take);
+                l.cost = std::max(l.cost, load);
+                if (take < n) slots += (u.n_tok[0] + u.n_tok[1]) * (double)p.pack / kRows;
+                at += take;
+            }
+            if (at < n || (load >= share - 0.5 * c.start && cta < p.n_ctas - 1)) {
+                ++cta;
+                load = 0.0;
+            }
+        } while (at < n);
+    }
+    if (slots > 0.0) l.cost += c.join + slots * c.join_slot * p.D;
+}
+
+// the query heads of a key/value head that share a tile: the divisor of their number with the fewest tiles
+int choose_pack(const int32_t* q, int n_seq, int group) {
+    int best = 1;
+    long long least = -1;
+    for (int p = 1; p <= group && p <= kRows; ++p) {
+        if (group % p) continue;
+        const int tok = kRows / p;
+        long long tiles = 0;
+        for (int s = 0; s < n_seq; ++s) tiles += (q[s] + (long long)tok - 1) / tok;
+        tiles *= group / p;
+        if (least < 0 || tiles <= least) { least = tiles; best = p; }
+    }
+    return best;
+}
+
+int plan(const Problem& prob, geocache_attention_plan* out, char* schedule, int64_t schedule_bytes) {
+    Problem p = prob;
+    p.pack = choose_pack(p.q, p.n_seq, p.Hq / p.Hk);
+    const Cost c = cost_of(p.D);
+    const int tok = kRows / p.pack;
+    long long n_units = 0;
+    for (int s = 0; s < p.n_seq; ++s) n_units += (p.q[s] + 2LL * tok - 1) / (2 * tok);
+    n_units *= p.Hq / p.pack;
+    if (n_units > (1LL << 24)) return geocache::set_error(GEOCACHE_ESHAPE, "geocache_plan_attention: over 2^24 pieces of work");
+    Layout best;
+    for (int tiles = 2; tiles >= 1; --tiles) {
+        if (tiles == 1 && n_units > 4LL * p.n_ctas) continue;  // every block has its share of pairs
+        Layout l;
+        l.tiles = tiles;
+        l.units = make_units(p, tiles);
+        Layout even = l;
+        assign_whole(p, c, l);
+        assign_even(p, c, even);
+        if (even.cost < l.cost) l = std::move(even);
+        if (!best.tiles || l.cost < best.cost) best = std::move(l);
+    }
+    // parts of a unit in the order of their keys: tile t takes part in those that begin before the end of what it sees
+    std::vector<int> parts[2], slot[2], seen(best.units.size(), 0);
+    for (int t = 0; t < 2; ++t) {
+        parts[t].assign(best.units.size(), 0);
+        slot[t].assign(best.units.size(), -1);
+    }
+    size_t n_items = 0;
+    for (const auto& list : best.of_cta)
+        for (const Piece& x : list) {
+            const Unit& u = best.units[x.unit];
+            ++n_items;
+            for (int t = 0; t < 2; ++t)
+                if (u.n_tok[t] && (x.from == 0 || x.from < u.n_kv[t])) ++parts[t][x.unit];
+        }
+    long long n_slots = 0;
+    size_t n_joins = 0;
+    for (size_t i = 0; i < best.units.size(); ++i)
+        for (int t = 0; t < 2; ++t)
+            if (parts[t][i] > 1) {
+                slot[t][i] = (int)n_slots;
+                n_slots += parts[t][i];
+                ++n_joins;
+            }
+    const int64_t bytes = geocache::attention_items_at(p.n_ctas) + 64LL * n_items + 32LL * n_joins;
+    if (n_items > (1u << 26) || n_slots > (1LL << 26))
+        return geocache::set_error(GEOCACHE_ESHAPE, "geocache_plan_attention: over 2^26 pieces of work");
+    out->Hq = p.Hq; out->Hk = p.Hk; out->D = p.D; out->causal = p.causal;
+    out->n_ctas = p.n_ctas;
+    out->n_items = (int)n_items;
+    out->n_joins = (int)n_joins;
+    out->pack = p.pack;
+    out->q_tokens = std::accumulate(p.q, p.q + p.n_seq, 0LL);
+    out->k_tokens = std::accumulate(p.k, p.k + p.n_seq, 0LL);
+    out->schedule_bytes = bytes;
+    out->workspace_bytes = n_slots * geocache::attention_slot_bytes(p.D);
+    if (!schedule) return GEOCACHE_OK;
+    if (schedule_bytes < bytes)
+        return geocache::set_error(GEOCACHE_EINVAL, "geocache_plan_attention: the schedule takes %lld bytes", (long long)bytes);
+
+    std::vector<long long> q_at(p.n_seq + 1, 0), k_at(p.n_seq + 1, 0);
+    for (int s = 0; s < p.n_seq; ++s) {
+        q_at[s + 1] = q_at[s] + p.q[s];
+        k_at[s + 1] = k_at[s] + p.k[s];
+    }
+    std::memset(schedule, 0, (size_t)bytes);
+    int32_t* ptr = reinterpret_cast<int32_t*>(schedule);
+    AttentionItem* item = reinterpret_cast<AttentionItem*>(schedule + geocache::attention_items_at(p.n_ctas));
+    AttentionJoin* join = reinterpret_cast<AttentionJoin*>(item + n_items);
+    // a unit's pieces come in the order of their keys: they lie in consecutive blocks, or one block has them all
+    std::vector<int> next[2] = {slot[0], slot[1]};
+    int n = 0;
+    for (int cta = 0; cta < p.n_ctas; ++cta) {
+        ptr[cta] = n;
+        for (const Piece& x : best.of_cta[cta]) {
+            const Unit& u = best.units[x.unit];
+            AttentionItem& o = item[n++];
+            const long long key = (long long)x.from * kKeys;
+            o.q_row = (int32_t)(q_at[u.seq] + u.token);
+            o.head = u.head;
+            o.kv_head = u.kv_head;
+            o.kv_row = (int32_t)(k_at[u.seq] + key);
+            o.n_keys = (int32_t)(p.k[u.seq] - std::min<long long>(key, p.k[u.seq]));
+            o.sees = p.causal ? (int32_t)(u.token + 1LL + p.k[u.seq] - p.q[u.seq] - key) : o.n_keys;
+            for (int t = 0; t < 2; ++t) {
+                o.slot[t] = -1;
+                if (!u.n_tok[t] || !(x.from == 0 || x.from < u.n_kv[t])) continue;
+                o.n_tok[t] = u.n_tok[t];
+                o.n_kv[t] = std::max(0, std::min(x.to, u.n_kv[t]) - x.from);
+                if (slot[t][x.unit] >= 0) o.slot[t] = next[t][x.unit]++;
+            }
+        }
+    }
+    ptr[p.n_ctas] = n;
+    for (size_t i = 0; i < best.units.size(); ++i)
+        for (int t = 0; t < 2; ++t)
+            if (slot[t][i] >= 0) {
+                const Unit& u = best.units[i];
+                *join++ = {(int32_t)(q_at[u.seq] + u.token + t * tok), u.n_tok[t], u.head, slot[t][i], parts[t][i], {0, 0, 0}};
+            }
+    return GEOCACHE_OK;
+}
+
+}  // namespace
+
+extern "C" int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int Hq, int Hk, int D,
+                                       int causal, int n_ctas, geocache_attention_plan* out, void* schedule,
+                                       int64_t schedule_bytes) {
+    const char* fn = "geocache_plan_attention";
+    if (!out || (n_seq > 0 && (!q_lens || !k_lens)))
+        return geocache::set_error(GEOCACHE_EINVAL, "%s: q_lens, k_lens and plan are required", fn);
+    if ((uintptr_t)schedule & 15) return geocache::set_error(GEOCACHE_EINVAL, "%s: schedule must be 16-byte aligned", fn);
+    if (n_seq < 0 || Hk < 1 || Hq < Hk || Hq > 65536 || Hq % Hk)
+        return geocache::set_error(GEOCACHE_ESHAPE, "%s: n_seq=%d, Hq=%d, Hk=%d out of range", fn, n_seq, Hq, Hk);
+    if (D < 8 || D > 128 || D % 8) return geocache::set_error(GEOCACHE_ESHAPE, "%s: D=%d must be a multiple of 8 in [8, 128]", fn, D);
+    if (n_ctas < 0 || n_ctas > 65536) return geocache::set_error(GEOCACHE_ESHAPE, "%s: n_ctas=%d out of range", fn, n_ctas);
+    long long sum[2] = {0, 0};
+    for (int s = 0; s < n_seq; ++s) {
+        if (q_lens[s] < 0 || k_lens[s] < 0)
+            return geocache::set_error(GEOCACHE_ESHAPE, "%s: sequence %d has a negative length", fn, s);
+        sum[0] += q_lens[s];
+        sum[1] += k_lens[s];
+    }
+    if (sum[0] > geocache::kAttentionTokens || sum[1] > geocache::kAttentionTokens)
+        return geocache::set_error(GEOCACHE_ESHAPE, "%s: over %lld tokens", fn, geocache::kAttentionTokens);
+    if (n_ctas == 0) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&n_ctas, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n_ctas < 1) {
+            cudaGetLastError();
+            return geocache::set_error(GEOCACHE_EDEVICE, "%s: no device to ask for its SMs (give n_ctas)", fn);
+        }
+    }
+    try {
+        geocache_attention_plan p{};
+        const int st = plan({q_lens, k_lens, n_seq, Hq, Hk, D, causal != 0, n_ctas, 1}, &p, static_cast<char*>(schedule), schedule_bytes);
+        if (st) return st;
+        *out = p;
+    } catch (const std::exception&) {
+        return geocache::set_error(GEOCACHE_ESHAPE, "%s: the work does not fit in host memory", fn);
+    }
+    return GEOCACHE_OK;
+}

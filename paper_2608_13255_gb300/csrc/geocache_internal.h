@@ -125,6 +125,55 @@ struct NormRopeArgs {
 cudaError_t launch_norm_rope(const NormRopeArgs& a, cudaStream_t s);
 cudaError_t read_rope_error(unsigned int* out, bool clear, cudaStream_t s);
 
+// One piece of an attention launch: up to two tiles of 128 query rows (tile t's tokens start at q_row + t *
+// (128 / pack); a row is one of `pack` heads of a token) of one sequence and key/value head, over a range of its
+// keys in tiles of 128.
+struct alignas(16) AttentionItem {
+    int32_t q_row;      // first token of tile 0
+    int32_t head;       // first query head
+    int32_t kv_head;
+    int32_t kv_row;     // first key
+    int32_t n_keys;     // keys from kv_row to the sequence's end
+    int32_t sees;       // causal: keys from kv_row on that tile 0's first token sees (may be <= 0)
+    int32_t n_tok[2];   // tokens of a tile; 0: the tile takes no part
+    int32_t n_kv[2];    // key tiles that the tile sees
+    int32_t slot[2];    // the tile's part of the workspace, -1: it writes the output
+    int32_t unused[4];
+};
+static_assert(sizeof(AttentionItem) == 64, "read as four 16-byte words");
+// The parts slot .. slot + n_parts of a tile's rows.
+struct AttentionJoin {
+    int32_t q_row, n_tok, head, slot, n_parts, unused[3];
+};
+static_assert(sizeof(AttentionJoin) == 32, "layout of the schedule");
+constexpr int kAttentionRows = 128;   // query rows of a tile
+constexpr int kAttentionKeys = 128;   // keys of a tile
+constexpr long long kAttentionTokens = 0x7fffffffLL - 1023;   // rows: an int32 index may run over the end by some tiles
+// schedule: n_ctas + 1 int32 offsets of the blocks' items (padded to 64 bytes), the items, the joins
+inline long long attention_items_at(int n_ctas) { return ((long long)n_ctas + 1 + 15) / 16 * 64; }
+// workspace: n_slots tiles of [128][D] f32, then their [128] f32 lse
+inline long long attention_slot_bytes(int D) { return 128LL * D * 4 + 128 * 4; }
+
+struct AttentionArgs {
+    const int32_t* cta_ptr;
+    const AttentionItem* items;
+    const AttentionJoin* joins;
+    int n_ctas, n_joins, pack, D, Hq, Hk, causal, dtype;
+    long long q_tokens, k_tokens, n_slots;
+    geocache_heads q, k, v, out;
+    float* lse;
+    float scale;
+    float* parts;       // workspace
+    float* part_lse;
+    unsigned long long wait_limit_ns;
+    int drop_first_copy;
+};
+cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s);
+cudaError_t read_attention_error(unsigned int* out, bool clear, cudaStream_t s);
+// the limit of bounded waits, and the test hook's pending request (consumed)
+unsigned long long debug_wait_limit_ns();
+int take_drop_first_copy();
+
 // Counts kernels that the calling thread's current library call enqueues
 // (geocache_last_launches).
 void note_launches(int n);

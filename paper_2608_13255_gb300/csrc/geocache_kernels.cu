@@ -1301,6 +1301,8 @@ void set_debug_wait(unsigned long long limit_ns, int drop_first_copy) {
     g_wait_limit_ns.store(limit_ns ? limit_ns : kWaitLimitNs);
     g_drop_first_copy.store(drop_first_copy ? 1 : 0);
 }
+unsigned long long debug_wait_limit_ns() { return g_wait_limit_ns.load(); }
+int take_drop_first_copy() { return g_drop_first_copy.exchange(0); }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {

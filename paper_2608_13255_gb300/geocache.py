@@ -78,6 +78,13 @@ class Rope(ctypes.Structure):
                 ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
 
 
+class AttentionPlanInfo(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int), ("Hk", ctypes.c_int), ("D", ctypes.c_int), ("causal", ctypes.c_int),
+                ("n_ctas", ctypes.c_int), ("n_items", ctypes.c_int), ("n_joins", ctypes.c_int), ("pack", ctypes.c_int),
+                ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64), ("schedule_bytes", ctypes.c_int64),
+                ("workspace_bytes", ctypes.c_int64)]
+
+
 assert ctypes.sizeof(Camera) == 64
 
 _LIB = None
@@ -87,7 +94,7 @@ EXPORTS = ("geocache_build_corr", "geocache_transport_step", "geocache_reconstru
            "geocache_unpack_anchors", "geocache_transport_step_update", "geocache_permute_records",
            "geocache_raster_posmaps", "geocache_debug_set_wait", "geocache_raster_posmaps_supersampled",
            "geocache_pool_posmaps", "geocache_fill_records", "geocache_last_launches",
-           "geocache_rope_table", "geocache_qk_norm_rope",
+           "geocache_rope_table", "geocache_qk_norm_rope", "geocache_plan_attention", "geocache_attention",
            "geocache_last_error", "geocache_abi_version")
 
 
@@ -130,6 +137,11 @@ def load():
         L.geocache_rope_table.restype = ctypes.c_int
         L.geocache_qk_norm_rope.argtypes = [H, H, H, H, i64, i, i, i, i, i, ctypes.c_double, P, P, P, i64, i, i, P, P]
         L.geocache_qk_norm_rope.restype = ctypes.c_int
+        A = ctypes.POINTER(AttentionPlanInfo)
+        L.geocache_plan_attention.argtypes = [P, P, i, i, i, i, i, i, A, P, i64]
+        L.geocache_plan_attention.restype = ctypes.c_int
+        L.geocache_attention.argtypes = [A, P, H, H, H, H, P, i, ctypes.c_double, P, i64, P]
+        L.geocache_attention.restype = ctypes.c_int
         L.geocache_corr_record_count.argtypes = [ctypes.POINTER(Corr), ctypes.POINTER(ctypes.c_int64), P]
         L.geocache_corr_record_count.restype = ctypes.c_int
         L.geocache_fill_records.argtypes = [ctypes.POINTER(Corr), P]
@@ -591,6 +603,68 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
         _dev(table, f32, None, "table"), n_slots, rot, _ROPE_LAYOUTS[layout], _dev(slots, torch.int32, T, "slots"),
         _stream(stream)))
     return q_out, k_out
+
+
+class AttentionPlan:
+    """A plan (sizes in `info`), its schedule on the device and the workspace
+    of its calls.  Calls that may overlap on the GPU need a workspace each."""
+
+    def __init__(self, info: AttentionPlanInfo, schedule, workspace):
+        self.info = info
+        self.schedule = schedule
+        self.workspace = workspace
+
+
+def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
+    """geocache_plan_attention: (info, schedule as a host int32 tensor)."""
+    q = [operator.index(x) for x in q_lens]
+    k = [operator.index(x) for x in k_lens]
+    if len(q) != len(k):
+        raise ValueError("%d lengths of queries, %d of keys" % (len(q), len(k)))
+    if any(not 0 <= x < 2 ** 31 for x in q + k):
+        raise ValueError("a sequence's length is outside [0, 2^31)")
+    qa, ka = (ctypes.c_int32 * max(1, len(q)))(*q), (ctypes.c_int32 * max(1, len(k)))(*k)
+    info = AttentionPlanInfo()
+    args = (qa, ka, len(q), int(Hq), int(Hk), int(D), 1 if causal else 0, int(n_ctas), ctypes.byref(info))
+    _check(load().geocache_plan_attention(*args, None, 0))
+    room = torch.zeros(info.schedule_bytes // 4 + 4, dtype=torch.int32)
+    schedule = room[(-room.data_ptr() % 16) // 4:][:info.schedule_bytes // 4]
+    _check(load().geocache_plan_attention(*args, schedule.data_ptr(), info.schedule_bytes))
+    return info, schedule
+
+
+def attention_plan(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0, device="cuda") -> AttentionPlan:
+    """The plan of an attention over packed sequences with these lengths (host
+    integers), for Hq query heads and Hk key/value heads of D elements.  Made
+    once for a batch and kept over layers and steps; the schedule and the
+    workspace are allocated here."""
+    info, schedule = plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal, n_ctas)
+    workspace = None
+    if info.workspace_bytes:
+        workspace = torch.empty(info.workspace_bytes // 4, dtype=torch.float32, device=device)
+    return AttentionPlan(info, schedule.to(device), workspace)
+
+
+def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, workspace=None, stream=None):
+    """geocache_attention: q [Tq, Hq, D], k and v [Tk, Hk, D] (bf16 or f16; any
+    strides that are multiples of 8 elements) with the rows of the plan's
+    sequences one after the other.  lse: device f32 [Tq, Hq] that receives the
+    logarithms of the softmax sums, or None.  scale: None = 1/sqrt(D).
+    Returns out (allocated when None)."""
+    f = plan.info
+    dt = q.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float16:
+        raise TypeError("q must be bfloat16 or float16 (got %s)" % dt)
+    if out is None:
+        out = torch.empty((f.q_tokens, f.Hq, f.D), dtype=dt, device=q.device)
+    ws = plan.workspace if workspace is None else workspace
+    _check(load().geocache_attention(
+        ctypes.byref(f), plan.schedule.data_ptr(), _heads(q, dt, f.q_tokens, f.Hq, f.D, "q"),
+        _heads(k, dt, f.k_tokens, f.Hk, f.D, "k"), _heads(v, dt, f.k_tokens, f.Hk, f.D, "v"),
+        _heads(out, dt, f.q_tokens, f.Hq, f.D, "out"), _dev(lse, torch.float32, f.q_tokens * f.Hq, "lse"),
+        _HEAD_DTYPES[dt], f.D ** -0.5 if scale is None else float(scale), _dev(ws, torch.float32, None, "workspace"),
+        0 if ws is None else 4 * ws.numel(), _stream(stream)))
+    return out
 
 
 def reconstruct(x_t, x0, x_next, recon: Recon, x0_store=None, stream=None):
