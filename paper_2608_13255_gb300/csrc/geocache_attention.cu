@@ -30,8 +30,12 @@ namespace {
 __device__ unsigned int g_attention_error = 0;
 
 constexpr int kRows = kAttentionRows, kKeys = kAttentionKeys;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;  // three warpgroups: two of softmax, one of which two warps work
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
+// Registers a thread: 168 at launch (65536 / 384); the softmax warps hold a row of 128 scores and take the others' share
+// (8 * 208 + 4 * 88 = 12 * 168).
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(8 * kSoftmaxRegs + 4 * kOtherRegs <= 12 * 168, "no more than the block was launched with");
 constexpr uint32_t kTmemColumns = 512;  // S of the two tiles at 0 and 128, O at 256 and 384
 constexpr uint32_t kBox = 128 * 128;    // bytes of 128 rows of 64 elements (one swizzled box)
 
@@ -75,14 +79,13 @@ __device__ __forceinline__ unsigned long long globaltimer() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a phase, with the lanes of `mask` together and all with one answer.  False when the limit passed, or when
+// Waits for a phase, the lanes of a warp together and all with one answer.  False when the limit passed, or when
 // another role of the block has given up: the roles then leave their loops one after the other.
-__device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b,
-                                            uint32_t mask) {
+__device__ __forceinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b) {
     const unsigned long long t0 = globaltimer();
-    while (!__all_sync(mask, mbar_try(bar, parity))) {
+    while (!__all_sync(0xffffffffu, mbar_try(bar, parity))) {
         const bool late = globaltimer() - t0 > limit_ns;
-        if (__any_sync(mask, late || *(volatile uint32_t*)&b->dead)) {
+        if (__any_sync(0xffffffffu, late || *(volatile uint32_t*)&b->dead)) {
             if (late) {
                 *(volatile uint32_t*)&b->dead = 1;
                 atomicOr(&g_attention_error, 1u);
@@ -92,11 +95,20 @@ __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, unsi
     }
     return true;
 }
-constexpr uint32_t kWarpMask = 0xffffffffu, kLane0 = 1u;
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b,
-                                          uint32_t mask = kWarpMask) {
-    return __all_sync(mask, mbar_try(bar, parity)) || mbar_wait_slow(bar, parity, limit_ns, b, mask);
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, Barriers* b) {
+    return __all_sync(0xffffffffu, mbar_try(bar, parity)) || mbar_wait_slow(bar, parity, limit_ns, b);
 }
+
+// True in one lane of a converged warp.  Products, commits and copies are issued under it and not under `lane == 0`:
+// the compiler then knows that one thread runs them and keeps their operands in uniform registers (a product took
+// about 130 cycles to issue otherwise).
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
+// a value that all lanes hold, as one that the compiler knows to be uniform
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
@@ -173,6 +185,28 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// pairs of floats: one issue slot for two operations
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // two floats as a pair of 16-bit values, `lo` in the low half
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi);
@@ -224,25 +258,33 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
     for (int i = first; i < last && ok; ++i) {
         AttentionItem it;
         load_item(p.a.items + i, it);
-        const int n = max(it.n_kv[0], it.n_kv[1]);
+        const int n_kv[2] = {uniform(it.n_kv[0]), uniform(it.n_kv[1])}, n_tok[2] = {uniform(it.n_tok[0]), uniform(it.n_tok[1])};
+        const int n = max(n_kv[0], n_kv[1]), q_row = uniform(it.q_row), group = uniform(it.head) / p.a.pack;
+        const int kv_head = uniform(it.kv_head), kv_row = uniform(it.kv_row);
         auto queries = [&](int t) {
-            if (!it.n_tok[t] || !it.n_kv[t]) return true;
-            if (!mbar_wait(&b->q_empty[t], (q_n[t] & 1) ^ 1, limit, b, kLane0)) return false;
-            mbar_expect(&b->q_full[t], q_bytes);
+            if (!n_tok[t] || !n_kv[t]) return true;
+            if (!mbar_wait(&b->q_empty[t], (q_n[t] & 1) ^ 1, limit, b)) return false;
+            if (elect()) {
+                mbar_expect(&b->q_full[t], q_bytes);
 #pragma unroll
-            for (int x = 0; x < S::kBoxes; ++x)
-                tma_4d(smem + t * S::kTileBytes + x * kBox, qm, 64 * x, 0, it.head / p.a.pack, it.q_row + t * p.tok, &b->q_full[t]);
+                for (int x = 0; x < S::kBoxes; ++x)
+                    tma_4d(smem + t * S::kTileBytes + x * kBox, qm, 64 * x, 0, group, q_row + t * p.tok, &b->q_full[t]);
+            }
+            __syncwarp();
             ++q_n[t];
             return true;
         };
         auto keys = [&](const CUtensorMap* map, int j) {
-            if (!mbar_wait(&b->kv_empty[stage], phase ^ 1, limit, b, kLane0)) return false;
+            if (!mbar_wait(&b->kv_empty[stage], phase ^ 1, limit, b)) return false;
             if (!drop) {
-                mbar_expect(&b->kv_full[stage], S::kTileBytes);
+                if (elect()) {
+                    mbar_expect(&b->kv_full[stage], S::kTileBytes);
 #pragma unroll
-                for (int x = 0; x < S::kBoxes; ++x)
-                    tma_3d(smem + (2 + stage) * S::kTileBytes + x * kBox, map, 64 * x, it.kv_head, it.kv_row + j * kKeys,
-                           &b->kv_full[stage]);
+                    for (int x = 0; x < S::kBoxes; ++x)
+                        tma_3d(smem + (2 + stage) * S::kTileBytes + x * kBox, map, 64 * x, kv_head, kv_row + j * kKeys,
+                               &b->kv_full[stage]);
+                }
+                __syncwarp();
                 armed |= 1u << stage;
             }
             drop = false;
@@ -277,21 +319,11 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
     auto advance = [&]() {
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
     };
-    auto qk = [&](int t, uint32_t at) {
-        if (lane == 0) {
-            const uint32_t q = smem + t * S::kTileBytes;
-            for (int s = 0; s < p.k_steps; ++s) {
-                const uint32_t off = (s >> 2) * kBox + (s & 3) * 32;
-                mma_ss(tmem + t * 128, smem_desc(q + off, 16), smem_desc(at + off, 16), p.qk_idesc, s > 0);
-            }
-            tc_commit(&b->s_full[t]);
-        }
-        __syncwarp();
-    };
     for (int i = first; i < last; ++i) {
         AttentionItem it;
         load_item(p.a.items + i, it);
-        const int n = max(it.n_kv[0], it.n_kv[1]);
+        const int n_kv[2] = {uniform(it.n_kv[0]), uniform(it.n_kv[1])}, n_keys = uniform(it.n_keys);
+        const int n = max(n_kv[0], n_kv[1]);
         for (int j = -1; j < n; ++j) {
             // values of tile j, then keys of tile j + 1, lie in consecutive stages
             uint32_t v_stage = 0, k_stage = 0;
@@ -304,11 +336,10 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
             const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                if (!it.n_tok[t]) continue;
-                if (j >= 0 && j < it.n_kv[t]) {
+                if (j >= 0 && j < n_kv[t]) {
                     if (!have_v) {
                         if (!mbar_wait(&b->kv_full[v_stage], v_phase, limit, b)) return;
-                        const int keys = it.n_keys - j * kKeys;
+                        const int keys = n_keys - j * kKeys;
                         if (keys < kKeys) {
                             // what lies behind the sequence's last key is another's: the rest of the last step of 16
                             // keys is cleared, so that 0 * v is 0 whatever it holds, and later steps are left out
@@ -326,23 +357,36 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                     }
                     if (!mbar_wait(&b->p_full[t], p_n[t]++ & 1, limit, b)) return;
                     tc_after();
-                    if (lane == 0)
-                        for (int s = 0; s < v_steps; ++s)
-                            mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, smem_desc(v_at + s * 2048, kBox), p.pv_idesc,
-                                   j > 0 || s > 0);
-                    if (j + 1 == it.n_kv[t] && lane == 0) tc_commit(&b->o_full[t]);
+                    if (elect()) {
+                        const uint64_t v = smem_desc(v_at, kBox);
+#pragma unroll
+                        for (int s = 0; s < kKeys / 16; ++s)
+                            if (s < v_steps)
+                                mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + s * (2048 >> 4), p.pv_idesc, j > 0 || s > 0);
+                        if (j + 1 == n_kv[t]) tc_commit(&b->o_full[t]);
+                    }
                     __syncwarp();
                 }
-                if (j + 1 < it.n_kv[t]) {
+                if (j + 1 < n_kv[t]) {
                     if (j < 0 && !mbar_wait(&b->q_full[t], q_n[t]++ & 1, limit, b)) return;
                     if (!have_k && !mbar_wait(&b->kv_full[k_stage], k_phase, limit, b)) return;
                     have_k = true;
                     tc_after();
-                    qk(t, k_at);
-                    if (j + 2 == it.n_kv[t] && lane == 0) tc_commit(&b->q_empty[t]);
+                    if (elect()) {
+                        const uint64_t q = smem_desc(smem + t * S::kTileBytes, 16), k = smem_desc(k_at, 16);
+#pragma unroll
+                        for (int s = 0; s < DP / 16; ++s)
+                            if (s < p.k_steps) {
+                                const uint32_t off = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
+                                mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
+                            }
+                        tc_commit(&b->s_full[t]);
+                        if (j + 2 == n_kv[t]) tc_commit(&b->q_empty[t]);
+                    }
+                    __syncwarp();
                 }
             }
-            if (lane == 0) {
+            if (elect()) {
                 if (j >= 0) tc_commit(&b->kv_empty[v_stage]);
                 if (j + 1 < n) tc_commit(&b->kv_empty[k_stage]);
             }
@@ -392,9 +436,11 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
                     for (int x = 0; x < 128; ++x)
                         if (x >= here) s[x] = 0xff800000u;
                 }
-                float top = -INFINITY;
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int x = 0; x < 128; ++x) top = fmaxf(top, __uint_as_float(s[x]));
+                for (int x = 0; x < 128; x += 2)
+                    tops[x / 2 & 3] = max3(tops[x / 2 & 3], __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+                const float top = max3(fmaxf(tops[0], tops[1]), tops[2], tops[3]);
                 if (j == 0) {
                     m = top;
                 } else if (const bool grown = (top - m) * p.c > 8.0f; __any_sync(0xffffffffu, grown)) {
@@ -414,21 +460,26 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
                     }
                 }
                 const float base = m == -INFINITY ? 0.0f : m * p.c;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint64_t c2 = pair(p.c, p.c), base2 = pair(-base, -base);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t w[32];
 #pragma unroll
                     for (int x = 0; x < 32; ++x) {
-                        const float e0 = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * x]), p.c, -base));
-                        const float e1 = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * x + 1]), p.c, -base));
-                        sum[2 * (x & 1)] += e0;
-                        sum[2 * (x & 1) + 1] += e1;
+                        float e0, e1;
+                        unpair(fma2(pair(__uint_as_float(s[64 * h + 2 * x]), __uint_as_float(s[64 * h + 2 * x + 1])), c2, base2),
+                               e0, e1);
+                        e0 = exp2_fast(e0);
+                        e1 = exp2_fast(e1);
+                        sum[x & 1] = add2(sum[x & 1], pair(e0, e1));
                         w[x] = pack2<T>(e0, e1);
                     }
                     tmem_st32(s_at + 32 * h, w);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                float l0, l1;
+                unpair(add2(sum[0], sum[1]), l0, l1);
+                l += l0 + l1;
                 tmem_wait_st();
             }
             tc_before();
@@ -486,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ Barriers bars;
     Barriers* b = &bars;
     const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int t = 0; t < 2; ++t) {
             mbar_init(&b->q_full[t], 1);
@@ -511,22 +562,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tmem = b->tmem;
+    const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
     pdl_wait();
-    const int first = p.a.cta_ptr[blockIdx.x], last = p.a.cta_ptr[blockIdx.x + 1];
-    if (warp == kLoadWarp) {
-        if (lane == 0) load_role<DP>(p, &qm, &km, &vm, smem, b, first, last);
-    } else if (warp == kMmaWarp) {
-        mma_role<DP>(p, smem, tmem, b, first, last, lane);
-        // every product and every arrival that it announced is done before the block ends
-        if (lane == 0) {
-            tc_commit(&b->drained);
+    const int first = uniform(p.a.cta_ptr[blockIdx.x]), last = uniform(p.a.cta_ptr[blockIdx.x + 1]);
+    if (warp < kMmaWarp) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        softmax_role<DP, T>(p, tmem, b, first, last, warp >> 2, warp & 3, lane);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == kLoadWarp) load_role<DP>(p, &qm, &km, &vm, smem, b, first, last);
+        if (warp == kMmaWarp) {
+            mma_role<DP>(p, smem, tmem, b, first, last, lane);
+            // every product and every arrival that it announced is done before the block ends
+            __syncwarp();
+            if (elect()) tc_commit(&b->drained);
             const unsigned long long t0 = globaltimer();
             while (!mbar_try(&b->drained, 0) && globaltimer() - t0 < p.a.wait_limit_ns) {}
         }
         __syncwarp();
-    } else {
-        softmax_role<DP, T>(p, tmem, b, first, last, warp >> 2, warp & 3, lane);
     }
     tc_before();
     __syncthreads();
