@@ -311,86 +311,97 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
     }
 }
 
+// The products of key tile j are issued in one go for each query tile, O += P V_j and then S = Q K_{j+1}: the queue of
+// products holds about four (250 cycles), so what lies between two goes (a wait for P, the ring's bookkeeping) costs
+// nothing while it stays below that.
 template <int DP>
 __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, int first, int last, int lane) {
     using S = Shape<DP>;
     const unsigned long long limit = p.a.wait_limit_ns;
     uint32_t stage = 0, phase = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
-    auto advance = [&]() {
+    // the next stage of the ring, once its copy has landed
+    auto next_stage = [&](uint32_t& at) {
+        at = stage;
+        const bool ok = mbar_wait(&b->kv_full[stage], phase, limit, b);
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+        return ok;
+    };
+    auto scores = [&](int t, uint32_t k_at) {
+        const uint64_t q = smem_desc(smem + t * S::kTileBytes, 16), k = smem_desc(k_at, 16);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+            if (s < p.k_steps) {
+                const uint32_t off = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
+                mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
+            }
+        tc_commit(&b->s_full[t]);
     };
     for (int i = first; i < last; ++i) {
         AttentionItem it;
         load_item(p.a.items + i, it);
         const int n_kv[2] = {uniform(it.n_kv[0]), uniform(it.n_kv[1])}, n_keys = uniform(it.n_keys);
         const int n = max(n_kv[0], n_kv[1]);
-        for (int j = -1; j < n; ++j) {
-            // values of tile j, then keys of tile j + 1, lie in consecutive stages
-            uint32_t v_stage = 0, k_stage = 0;
-            bool have_v = false, have_k = false;
-            int v_steps = kKeys / 16;
-            if (j >= 0) v_stage = stage, advance();
-            const uint32_t v_phase = v_stage < stage || j < 0 ? phase : phase ^ 1;
-            if (j + 1 < n) k_stage = stage, advance();
-            const uint32_t k_phase = j + 1 < n && k_stage < stage ? phase : phase ^ 1;
-            const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
+        if (n == 0) continue;
+        const int last_user = n_kv[1] > 0 ? 1 : 0;  // of a stage (tile 1 sees at least the key tiles of tile 0)
+        uint32_t v_stage = 0, k_stage = 0;
+        if (!next_stage(k_stage)) return;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (j >= 0 && j < n_kv[t]) {
-                    if (!have_v) {
-                        if (!mbar_wait(&b->kv_full[v_stage], v_phase, limit, b)) return;
-                        const int keys = n_keys - j * kKeys;
-                        if (keys < kKeys) {
-                            // what lies behind the sequence's last key is another's: the rest of the last step of 16
-                            // keys is cleared, so that 0 * v is 0 whatever it holds, and later steps are left out
-                            v_steps = (keys + 15) / 16;
-                            const int words = (v_steps * 16 - keys) * 8;
-                            for (int x = 0; x < S::kBoxes; ++x)
-                                for (int w = lane; w < words; w += 32)
-                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + x * kBox + keys * 128 + w * 16),
-                                                 "r"(0)
-                                                 : "memory");
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                            __syncwarp();
-                        }
-                        have_v = true;
-                    }
-                    if (!mbar_wait(&b->p_full[t], p_n[t]++ & 1, limit, b)) return;
-                    tc_after();
-                    if (elect()) {
-                        const uint64_t v = smem_desc(v_at, kBox);
-#pragma unroll
-                        for (int s = 0; s < kKeys / 16; ++s)
-                            if (s < v_steps)
-                                mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + s * (2048 >> 4), p.pv_idesc, j > 0 || s > 0);
-                        if (j + 1 == n_kv[t]) tc_commit(&b->o_full[t]);
-                    }
-                    __syncwarp();
-                }
-                if (j + 1 < n_kv[t]) {
-                    if (j < 0 && !mbar_wait(&b->q_full[t], q_n[t]++ & 1, limit, b)) return;
-                    if (!have_k && !mbar_wait(&b->kv_full[k_stage], k_phase, limit, b)) return;
-                    have_k = true;
-                    tc_after();
-                    if (elect()) {
-                        const uint64_t q = smem_desc(smem + t * S::kTileBytes, 16), k = smem_desc(k_at, 16);
-#pragma unroll
-                        for (int s = 0; s < DP / 16; ++s)
-                            if (s < p.k_steps) {
-                                const uint32_t off = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
-                                mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
-                            }
-                        tc_commit(&b->s_full[t]);
-                        if (j + 2 == n_kv[t]) tc_commit(&b->q_empty[t]);
-                    }
-                    __syncwarp();
-                }
-            }
+        for (int t = 0; t < 2; ++t) {
+            if (n_kv[t] == 0) continue;
+            if (!mbar_wait(&b->q_full[t], q_n[t]++ & 1, limit, b)) return;
+            tc_after();
             if (elect()) {
-                if (j >= 0) tc_commit(&b->kv_empty[v_stage]);
-                if (j + 1 < n) tc_commit(&b->kv_empty[k_stage]);
+                scores(t, smem + (2 + k_stage) * S::kTileBytes);
+                if (n_kv[t] == 1) tc_commit(&b->q_empty[t]);
+                if (t == last_user) tc_commit(&b->kv_empty[k_stage]);
             }
             __syncwarp();
+        }
+        if (!next_stage(v_stage)) return;
+        if (n > 1 && !next_stage(k_stage)) return;
+        for (int j = 0; j < n; ++j) {
+            const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
+            const uint32_t v_bar = v_stage, k_bar = k_stage;
+            int v_steps = kKeys / 16;
+            if (n_keys - j * kKeys < kKeys) {
+                // what lies behind the sequence's last key is another's: the rest of the last step of 16 keys is
+                // cleared, so that 0 * v is 0 whatever it holds, and later steps are left out
+                const int keys = n_keys - j * kKeys;
+                v_steps = (keys + 15) / 16;
+                const int words = (v_steps * 16 - keys) * 8;
+                for (int x = 0; x < S::kBoxes; ++x)
+                    for (int w = lane; w < words; w += 32)
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + x * kBox + keys * 128 + w * 16), "r"(0)
+                                     : "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (t == last_user && j + 1 < n) {  // the stages of the next turn, while the other tile's products run
+                    if (!next_stage(v_stage)) return;
+                    if (j + 2 < n && !next_stage(k_stage)) return;
+                }
+                if (j >= n_kv[t]) continue;
+                if (!mbar_wait(&b->p_full[t], p_n[t]++ & 1, limit, b)) return;
+                tc_after();
+                if (elect()) {
+                    const uint64_t v = smem_desc(v_at, kBox);
+#pragma unroll
+                    for (int s = 0; s < kKeys / 16; ++s)
+                        if (s < v_steps)
+                            mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + s * (2048 >> 4), p.pv_idesc, j > 0 || s > 0);
+                    if (t == last_user) tc_commit(&b->kv_empty[v_bar]);
+                    if (j + 1 < n_kv[t]) {
+                        scores(t, k_at);
+                        if (j + 2 == n_kv[t]) tc_commit(&b->q_empty[t]);
+                        if (t == last_user) tc_commit(&b->kv_empty[k_bar]);
+                    } else {
+                        tc_commit(&b->o_full[t]);
+                    }
+                }
+                __syncwarp();
+            }
         }
     }
 }
