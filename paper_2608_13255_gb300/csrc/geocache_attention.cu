@@ -3,8 +3,8 @@
 // A thread block takes its pieces of the schedule one after the other.  A piece is one or two tiles of 128 query rows
 // against a run of 128-key tiles; the two tiles share every load of keys and values and take turns, so that the tensor
 // cores work on one while the other's softmax runs:
-//   warp 9      loads queries (once a piece), keys and values (a ring of stages) by TMA;
-//   warp 8      issues the products: S = Q K^T into tensor memory, and O += P V with P read from tensor memory;
+//   warp 10     loads queries (once a piece), keys and values (a ring of stages) by TMA;
+//   warps 8, 9  issue the products of tile 0 and of tile 1: S = Q K^T into tensor memory, O += P V with P read from there;
 //   warps 0-3   softmax of tile 0, one row a thread: S from tensor memory, the running maximum and sum in registers,
 //   warps 4-7   the same of tile 1;   P = exp2((S - m) scale log2 e) written over S as 16-bit pairs.
 // O stays in tensor memory over the whole piece.  It is rescaled only when a row's maximum has grown by more than 8
@@ -30,8 +30,8 @@ namespace {
 __device__ unsigned int g_attention_error = 0;
 
 constexpr int kRows = kAttentionRows, kKeys = kAttentionKeys;
-constexpr int kThreads = 384;  // three warpgroups: two of softmax, one of which two warps work
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 384;  // three warpgroups: two of softmax, one of which three warps work
+constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8 and 9 issue the products of tiles 0 and 1
 // Registers a thread: 168 at launch (65536 / 384); the softmax warps hold a row of 128 scores and take the others' share
 // (8 * 208 + 4 * 88 = 12 * 168).
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
@@ -48,7 +48,7 @@ struct Shape {  // heads padded to DP = 64 or 128 elements
 };
 
 struct Barriers {
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], drained;
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], turn[2], drained;
     uint64_t kv_full[8], kv_empty[8];
     uint32_t tmem;
     uint32_t dead;
@@ -245,6 +245,8 @@ __device__ __forceinline__ void load_item(const AttentionItem* p, AttentionItem&
     for (int i = 0; i < 3; ++i) d[i] = s[i];
 }
 
+constexpr int kEarly = 1;  // products of a go that are issued after the turn has passed to the other tile
+
 // ---------------------------------------------------------------- roles --
 // Each role walks the block's pieces with its own count of the phases; a wait that gives up ends it.
 template <int DP>
@@ -311,14 +313,16 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
     }
 }
 
-// The products of key tile j are issued in one go for each query tile, O += P V_j and then S = Q K_{j+1}: the queue of
-// products holds about four (250 cycles), so what lies between two goes (a wait for P, the ring's bookkeeping) costs
-// nothing while it stays below that.
+// One warp issues the products of one query tile: S = Q K_0, and then for each key tile O += P V_j and S = Q K_{j+1} in one
+// go.  The tensor cores' queue is short (issuing waits for room), so one warp waits for P and does the ring's bookkeeping
+// while the other's products are issued.  The goes alternate: products of both tiles mixed would end together, and the
+// softmax of both would then run while the tensor cores idle (measured: 4.0 ms for what takes 3.1 by one warp in turn).
+// A stage is free when both have read it; a tile that does not need it leaves that to the other.
 template <int DP>
-__device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, int first, int last, int lane) {
+__device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, int first, int last, int t, int lane) {
     using S = Shape<DP>;
     const unsigned long long limit = p.a.wait_limit_ns;
-    uint32_t stage = 0, phase = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
+    uint32_t stage = 0, phase = 0, q_n = 0, p_n = 0, turn_n = 0;
     // the next stage of the ring, once its copy has landed
     auto next_stage = [&](uint32_t& at) {
         at = stage;
@@ -326,64 +330,58 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         return ok;
     };
-    auto scores = [&](int t, uint32_t k_at) {
+    auto free_stage = [&](uint32_t at, bool shared) {
+        tc_commit(&b->kv_empty[at]);
+        if (!shared) tc_commit(&b->kv_empty[at]);
+    };
+    auto scores = [&](uint32_t k_at, bool hand_over) {
         const uint64_t q = smem_desc(smem + t * S::kTileBytes, 16), k = smem_desc(k_at, 16);
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s)
             if (s < p.k_steps) {
                 const uint32_t off = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
                 mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
+                if (hand_over && s + kEarly + 1 == p.k_steps) mbar_arrive(&b->turn[t ^ 1]);
             }
         tc_commit(&b->s_full[t]);
     };
     for (int i = first; i < last; ++i) {
         AttentionItem it;
         load_item(p.a.items + i, it);
-        const int n_kv[2] = {uniform(it.n_kv[0]), uniform(it.n_kv[1])}, n_keys = uniform(it.n_keys);
-        const int n = max(n_kv[0], n_kv[1]);
-        if (n == 0) continue;
-        const int last_user = n_kv[1] > 0 ? 1 : 0;  // of a stage (tile 1 sees at least the key tiles of tile 0)
-        uint32_t v_stage = 0, k_stage = 0;
-        if (!next_stage(k_stage)) return;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (n_kv[t] == 0) continue;
-            if (!mbar_wait(&b->q_full[t], q_n[t]++ & 1, limit, b)) return;
+        const int n = uniform(t ? it.n_kv[1] : it.n_kv[0]), n_other = uniform(t ? it.n_kv[0] : it.n_kv[1]);
+        const int n_keys = uniform(it.n_keys);
+        if (n > 0) {
+            uint32_t v_stage = 0, k_stage = 0;
+            if (!next_stage(k_stage) || !mbar_wait(&b->q_full[t], q_n++ & 1, limit, b)) return;
             tc_after();
             if (elect()) {
-                scores(t, smem + (2 + k_stage) * S::kTileBytes);
-                if (n_kv[t] == 1) tc_commit(&b->q_empty[t]);
-                if (t == last_user) tc_commit(&b->kv_empty[k_stage]);
+                scores(smem + (2 + k_stage) * S::kTileBytes, false);
+                if (n == 1) tc_commit(&b->q_empty[t]);
+                free_stage(k_stage, n_other > 0);
             }
             __syncwarp();
-        }
-        if (!next_stage(v_stage)) return;
-        if (n > 1 && !next_stage(k_stage)) return;
-        for (int j = 0; j < n; ++j) {
-            const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
-            const uint32_t v_bar = v_stage, k_bar = k_stage;
-            int v_steps = kKeys / 16;
-            if (n_keys - j * kKeys < kKeys) {
-                // what lies behind the sequence's last key is another's: the rest of the last step of 16 keys is
-                // cleared, so that 0 * v is 0 whatever it holds, and later steps are left out
-                const int keys = n_keys - j * kKeys;
-                v_steps = (keys + 15) / 16;
-                const int words = (v_steps * 16 - keys) * 8;
-                for (int x = 0; x < S::kBoxes; ++x)
-                    for (int w = lane; w < words; w += 32)
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + x * kBox + keys * 128 + w * 16), "r"(0)
-                                     : "memory");
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (t == last_user && j + 1 < n) {  // the stages of the next turn, while the other tile's products run
-                    if (!next_stage(v_stage)) return;
-                    if (j + 2 < n && !next_stage(k_stage)) return;
+            for (int j = 0; j < n; ++j) {
+                if (!next_stage(v_stage) || (j + 1 < n && !next_stage(k_stage))) return;
+                const uint32_t v_at = smem + (2 + v_stage) * S::kTileBytes, k_at = smem + (2 + k_stage) * S::kTileBytes;
+                int v_steps = kKeys / 16;
+                if (n_keys - j * kKeys < kKeys) {
+                    // what lies behind the sequence's last key is another's: the rest of the last step of 16 keys is
+                    // cleared (by both warps), so that 0 * v is 0 whatever it holds, and later steps are left out
+                    const int keys = n_keys - j * kKeys;
+                    v_steps = (keys + 15) / 16;
+                    const int words = (v_steps * 16 - keys) * 8;
+                    for (int x = 0; x < S::kBoxes; ++x)
+                        for (int w = lane; w < words; w += 32)
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + x * kBox + keys * 128 + w * 16), "r"(0)
+                                         : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
                 }
-                if (j >= n_kv[t]) continue;
-                if (!mbar_wait(&b->p_full[t], p_n[t]++ & 1, limit, b)) return;
+                if (!mbar_wait(&b->p_full[t], p_n++ & 1, limit, b)) return;
+                // tile 0's go j comes before tile 1's and after its go j - 1 (tile 0 has no more goes than tile 1)
+                if (t == 0 ? j > 0 && n_other > 0 : j < n_other)
+                    if (!mbar_wait(&b->turn[t], turn_n++ & 1, limit, b)) return;
+                const bool turn_over = t == 0 ? n_other > 0 : j + 1 < n_other;
                 tc_after();
                 if (elect()) {
                     const uint64_t v = smem_desc(v_at, kBox);
@@ -391,17 +389,23 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                     for (int s = 0; s < kKeys / 16; ++s)
                         if (s < v_steps)
                             mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + s * (2048 >> 4), p.pv_idesc, j > 0 || s > 0);
-                    if (t == last_user) tc_commit(&b->kv_empty[v_bar]);
-                    if (j + 1 < n_kv[t]) {
-                        scores(t, k_at);
-                        if (j + 2 == n_kv[t]) tc_commit(&b->q_empty[t]);
-                        if (t == last_user) tc_commit(&b->kv_empty[k_bar]);
+                    free_stage(v_stage, j < n_other);
+                    if (j + 1 < n) {
+                        scores(k_at, turn_over);
+                        if (j + 2 == n) tc_commit(&b->q_empty[t]);
+                        free_stage(k_stage, j + 1 < n_other);
                     } else {
+                        if (turn_over) mbar_arrive(&b->turn[t ^ 1]);
                         tc_commit(&b->o_full[t]);
                     }
                 }
                 __syncwarp();
             }
+        }
+        if (n < n_other) {  // stages that the other tile alone reads
+            const uint32_t to = stage + 2 * (uint32_t)(n_other - n);
+            stage = to % S::kStages;
+            phase ^= to / S::kStages & 1;
         }
     }
 }
@@ -447,19 +451,47 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
                     for (int x = 0; x < 128; ++x)
                         if (x >= here) s[x] = 0xff800000u;
                 }
-                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int x = 0; x < 128; x += 2)
-                    tops[x / 2 & 3] = max3(tops[x / 2 & 3], __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
-                const float top = max3(fmaxf(tops[0], tops[1]), tops[2], tops[3]);
                 if (j == 0) {
-                    m = top;
-                } else if (const bool grown = (top - m) * p.c > 8.0f; __any_sync(0xffffffffu, grown)) {
+#pragma unroll
+                    for (int x = 0; x < 128; x += 2) m = max3(m, __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+                }
+                // The weights are formed relative to the maximum so far while the new one is taken beside them (the
+                // exponentials leave that pipe idle); where a row's maximum has grown by more than 8 powers of two they are
+                // formed again.
+                float sum;
+                while (true) {
+                    const float base = m == -INFINITY ? 0.0f : m * p.c;
+                    const uint64_t c2 = pair(p.c, p.c), base2 = pair(-base, -base);
+                    uint64_t sums[2] = {0, 0};
+                    float tops[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) {
+                            const float s0 = __uint_as_float(s[64 * h + 2 * x]), s1 = __uint_as_float(s[64 * h + 2 * x + 1]);
+                            float e0, e1;
+                            unpair(fma2(pair(s0, s1), c2, base2), e0, e1);
+                            e0 = exp2_fast(e0);
+                            e1 = exp2_fast(e1);
+                            tops[x & 1] = max3(tops[x & 1], s0, s1);
+                            sums[x & 1] = add2(sums[x & 1], pair(e0, e1));
+                            w[x] = pack2<T>(e0, e1);
+                        }
+                        tmem_st32(s_at + 32 * h, w);
+                    }
+                    float l0, l1;
+                    unpair(add2(sums[0], sums[1]), l0, l1);
+                    sum = l0 + l1;
+                    const float top = fmaxf(tops[0], tops[1]);
+                    const bool grown = (top - m) * p.c > 8.0f;
+                    if (!__any_sync(0xffffffffu, grown)) break;
                     // O and the sum follow the larger maximum (the product into O is complete: S came after it); each
                     // row by its own scores alone, so that its result does not depend on the rows beside it
                     const float f = grown ? exp2_fast((m - top) * p.c) : 1.0f;
                     if (grown) m = top;
                     l *= f;
+                    tmem_wait_st();  // the weights in flight go to where the new ones will
 #pragma unroll 1
                     for (int x = 0; x < p.a.D; x += 32) {
                         uint32_t o[32];
@@ -470,27 +502,7 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
                         tmem_st32(o_at + x, o);
                     }
                 }
-                const float base = m == -INFINITY ? 0.0f : m * p.c;
-                const uint64_t c2 = pair(p.c, p.c), base2 = pair(-base, -base);
-                uint64_t sum[2] = {0, 0};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) {
-                        float e0, e1;
-                        unpair(fma2(pair(__uint_as_float(s[64 * h + 2 * x]), __uint_as_float(s[64 * h + 2 * x + 1])), c2, base2),
-                               e0, e1);
-                        e0 = exp2_fast(e0);
-                        e1 = exp2_fast(e1);
-                        sum[x & 1] = add2(sum[x & 1], pair(e0, e1));
-                        w[x] = pack2<T>(e0, e1);
-                    }
-                    tmem_st32(s_at + 32 * h, w);
-                }
-                float l0, l1;
-                unpair(add2(sum[0], sum[1]), l0, l1);
-                l += l0 + l1;
+                l += sum;
                 tmem_wait_st();
             }
             tc_before();
@@ -556,11 +568,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&b->s_full[t], 1);
             mbar_init(&b->p_full[t], 4);
             mbar_init(&b->o_full[t], 1);
+            mbar_init(&b->turn[t], 1);
         }
-        mbar_init(&b->drained, 1);
+        mbar_init(&b->drained, 2);
         for (int s = 0; s < 8; ++s) {
             mbar_init(&b->kv_full[s], 1);
-            mbar_init(&b->kv_empty[s], 1);
+            mbar_init(&b->kv_empty[s], 2);
         }
         b->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -582,8 +595,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == kLoadWarp) load_role<DP>(p, &qm, &km, &vm, smem, b, first, last);
-        if (warp == kMmaWarp) {
-            mma_role<DP>(p, smem, tmem, b, first, last, lane);
+        if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+            mma_role<DP>(p, smem, tmem, b, first, last, warp - kMmaWarp, lane);
             // every product and every arrival that it announced is done before the block ends
             __syncwarp();
             if (elect()) tc_commit(&b->drained);
