@@ -7,9 +7,9 @@
 //   warps 8, 9  issue the products of tile 0 and of tile 1: S = Q K^T into tensor memory, O += P V with P read from there;
 //   warps 0-3   softmax of tile 0, one row a thread: S from tensor memory, the running maximum and sum in registers,
 //   warps 4-7   the same of tile 1;   P = exp2((S - m) scale log2 e) written over S as 16-bit pairs.
-// O stays in tensor memory over the whole piece.  It is rescaled only when a row's maximum has grown by more than 8
-// powers of two since the last time: until then the sums and P (at most 2^8) are kept relative to the old maximum,
-// which changes no result beyond rounding.  S, the statistics and O are binary32; P is rounded to the inputs' type, as
+// O stays in tensor memory over the whole piece.  It is rescaled only when a row's weights of one tile of keys sum to more
+// than 2^15: until then the sums and P are kept relative to an older maximum, which changes no result beyond rounding,
+// and the maximum itself need not be taken in every tile.  S, the statistics and O are binary32; P is rounded to the inputs' type, as
 // the product with the values needs, while its sum is taken before that rounding.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -166,6 +166,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t* r) {
         "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
 // The registers of a load are operands of the wait (or of an empty statement behind it), so that no use of them can be
 // moved before it.
 #define GEOCACHE_PIN16(r) \
@@ -245,6 +252,7 @@ __device__ __forceinline__ void load_item(const AttentionItem* p, AttentionItem&
     for (int i = 0; i < 3; ++i) d[i] = s[i];
 }
 
+constexpr float kLargest = 32768.0f;  // of the weights of a row and tile: half of what f16 holds
 constexpr int kEarly = 1;  // products of a go that are issued after the turn has passed to the other tile
 
 // ---------------------------------------------------------------- roles --
@@ -377,10 +385,10 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                if (!mbar_wait(&b->p_full[t], p_n++ & 1, limit, b)) return;
                 // tile 0's go j comes before tile 1's and after its go j - 1 (tile 0 has no more goes than tile 1)
                 if (t == 0 ? j > 0 && n_other > 0 : j < n_other)
                     if (!mbar_wait(&b->turn[t], turn_n++ & 1, limit, b)) return;
+                if (!mbar_wait(&b->p_full[t], p_n++ & 1, limit, b)) return;
                 const bool turn_over = t == 0 ? n_other > 0 : j + 1 < n_other;
                 tc_after();
                 if (elect()) {
@@ -434,6 +442,7 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
         if (!n_tok) continue;
         const bool active = tok < n_tok, warp_active = warp * 32 < n_tok * p.a.pack;
         const int sees = p.a.causal ? min(it.n_keys, it.sees + t * p.tok + tok) : it.n_keys;
+        const int least = uniform(sees);  // the rows of a warp see more and more
         float m = -INFINITY, l = 0.0f;
         for (int j = 0; j < n; ++j) {
             if (!mbar_wait(&b->s_full[t], s_n++ & 1, limit, b)) return;
@@ -446,7 +455,7 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
 #pragma unroll
                 for (int x = 1; x < 4; ++x) tmem_pin32(s + 32 * x);
                 const int here = sees - j * kKeys;
-                if (__any_sync(0xffffffffu, here < kKeys)) {
+                if (least - j * kKeys < kKeys) {
 #pragma unroll
                     for (int x = 0; x < 128; ++x)
                         if (x >= here) s[x] = 0xff800000u;
@@ -455,39 +464,42 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int fi
 #pragma unroll
                     for (int x = 0; x < 128; x += 2) m = max3(m, __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
                 }
-                // The weights are formed relative to the maximum so far while the new one is taken beside them (the
-                // exponentials leave that pipe idle); where a row's maximum has grown by more than 8 powers of two they are
-                // formed again.
+                // The weights are formed relative to the maximum of the first tile of keys, or of the last one that made
+                // them large: while a row's weights sum to at most 2^15 in a tile they lose nothing by not being relative
+                // to the latest maximum (the sums are binary32, and each is rounded relative to itself).
                 float sum;
                 while (true) {
                     const float base = m == -INFINITY ? 0.0f : m * p.c;
                     const uint64_t c2 = pair(p.c, p.c), base2 = pair(-base, -base);
                     uint64_t sums[2] = {0, 0};
-                    float tops[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t w[32];
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t w[16];
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) {
-                            const float s0 = __uint_as_float(s[64 * h + 2 * x]), s1 = __uint_as_float(s[64 * h + 2 * x + 1]);
+                        for (int x = 0; x < 16; ++x) {
                             float e0, e1;
-                            unpair(fma2(pair(s0, s1), c2, base2), e0, e1);
+                            unpair(fma2(pair(__uint_as_float(s[32 * h + 2 * x]), __uint_as_float(s[32 * h + 2 * x + 1])), c2, base2),
+                                   e0, e1);
                             e0 = exp2_fast(e0);
                             e1 = exp2_fast(e1);
-                            tops[x & 1] = max3(tops[x & 1], s0, s1);
                             sums[x & 1] = add2(sums[x & 1], pair(e0, e1));
                             w[x] = pack2<T>(e0, e1);
                         }
-                        tmem_st32(s_at + 32 * h, w);
+                        tmem_st16(s_at + 16 * h, w);
                     }
                     float l0, l1;
                     unpair(add2(sums[0], sums[1]), l0, l1);
                     sum = l0 + l1;
-                    const float top = fmaxf(tops[0], tops[1]);
-                    const bool grown = (top - m) * p.c > 8.0f;
-                    if (!__any_sync(0xffffffffu, grown)) break;
-                    // O and the sum follow the larger maximum (the product into O is complete: S came after it); each
-                    // row by its own scores alone, so that its result does not depend on the rows beside it
+                    const bool large = active && (sum > kLargest || m == -INFINITY);
+                    if (!__any_sync(0xffffffffu, large)) break;
+                    // they did not (a row without keys so far counts as such): O and the sum follow the new maximum (the
+                    // product into O is complete: S came after it), and the weights are formed again; each row by its own
+                    // scores alone, so that its result does not depend on the rows beside it
+                    float top = m;
+#pragma unroll
+                    for (int x = 0; x < 128; x += 2) top = max3(top, __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+                    const bool grown = large && top > m;
+                    if (!__any_sync(0xffffffffu, grown)) break;  // an infinite sum that no maximum mends
                     const float f = grown ? exp2_fast((m - top) * p.c) : 1.0f;
                     if (grown) m = top;
                     l *= f;
@@ -682,13 +694,13 @@ cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_heads& x, int D
         const cuuint64_t strides[3] = {hs, H / pack > 1 ? hs * pack : row, ts};
         const cuuint32_t box[4] = {64, (cuuint32_t)pack, 1, (cuuint32_t)tokens};
         r = encode(map, type, 4, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     } else {
         const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)T};
         const cuuint64_t strides[2] = {hs, ts};
         const cuuint32_t box[3] = {64, 1, (cuuint32_t)tokens};
         r = encode(map, type, 3, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     }
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
