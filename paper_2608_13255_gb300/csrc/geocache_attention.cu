@@ -47,9 +47,12 @@ struct Shape {  // heads padded to DP = 64 or 128 elements
     static constexpr uint32_t kBytes = (2 + kStages) * kTileBytes + 1024;  // and room to align to 1024
 };
 
+constexpr int kCached = 16;
+
 struct Barriers {
     uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], turn[2], drained;
     uint64_t kv_full[8], kv_empty[8];
+    AttentionItem items[kCached];  // the block's first pieces
     uint32_t tmem;
     uint32_t dead;
 };
@@ -245,8 +248,13 @@ struct Params {
     float c;              // scale * log2(e)
 };
 
-__device__ __forceinline__ void load_item(const AttentionItem* p, AttentionItem& it) {
-    const int4* s = reinterpret_cast<const int4*>(p);
+struct Items {  // a block's pieces [first, last)
+    const AttentionItem* all;
+    const Barriers* b;
+    int first, last;
+};
+__device__ __forceinline__ void load_item(const Items& p, int i, AttentionItem& it) {
+    const int4* s = reinterpret_cast<const int4*>(i - p.first < kCached ? p.b->items + (i - p.first) : p.all + i);
     int4* d = reinterpret_cast<int4*>(&it);
 #pragma unroll
     for (int i = 0; i < 3; ++i) d[i] = s[i];
@@ -259,15 +267,15 @@ constexpr int kEarly = 1;  // products of a go that are issued after the turn ha
 // Each role walks the block's pieces with its own count of the phases; a wait that gives up ends it.
 template <int DP>
 __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensorMap* km, const CUtensorMap* vm, uint32_t smem,
-                          Barriers* b, int first, int last) {
+                          Barriers* b, const Items& items) {
     using S = Shape<DP>;
     const unsigned long long limit = p.a.wait_limit_ns;
     const uint32_t q_bytes = S::kBoxes * 128u * p.a.pack * p.tok;
     uint32_t stage = 0, phase = 0, q_n[2] = {0, 0}, armed = 0;
     bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
-    for (int i = first; i < last && ok; ++i) {
+    for (int i = items.first; i < items.last && ok; ++i) {
         AttentionItem it;
-        load_item(p.a.items + i, it);
+        load_item(items, i, it);
         const int n_kv[2] = {uniform(it.n_kv[0]), uniform(it.n_kv[1])}, n_tok[2] = {uniform(it.n_tok[0]), uniform(it.n_tok[1])};
         const int n = max(n_kv[0], n_kv[1]), q_row = uniform(it.q_row), group = uniform(it.head) / p.a.pack;
         const int kv_head = uniform(it.kv_head), kv_row = uniform(it.kv_row);
@@ -325,9 +333,10 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
 // go.  The tensor cores' queue is short (issuing waits for room), so one warp waits for P and does the ring's bookkeeping
 // while the other's products are issued.  The goes alternate: products of both tiles mixed would end together, and the
 // softmax of both would then run while the tensor cores idle (measured: 4.0 ms for what takes 3.1 by one warp in turn).
-// A stage is free when both have read it; a tile that does not need it leaves that to the other.
+// Each warp waits for every stage of the ring and gives every stage back, those that only the other tile reads too: a
+// phase's parity tells it from the next one only, so neither warp may fall behind.
 template <int DP>
-__device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, int first, int last, int t, int lane) {
+__device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, const Items& items, int t, int lane) {
     using S = Shape<DP>;
     const unsigned long long limit = p.a.wait_limit_ns;
     uint32_t stage = 0, phase = 0, q_n = 0, p_n = 0, turn_n = 0;
@@ -338,10 +347,6 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         return ok;
     };
-    auto free_stage = [&](uint32_t at, bool shared) {
-        tc_commit(&b->kv_empty[at]);
-        if (!shared) tc_commit(&b->kv_empty[at]);
-    };
     auto scores = [&](uint32_t k_at, bool hand_over) {
         const uint64_t q = smem_desc(smem + t * S::kTileBytes, 16), k = smem_desc(k_at, 16);
 #pragma unroll
@@ -351,11 +356,12 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                 mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
                 if (hand_over && s + kEarly + 1 == p.k_steps) mbar_arrive(&b->turn[t ^ 1]);
             }
+        if (hand_over && p.k_steps <= kEarly) mbar_arrive(&b->turn[t ^ 1]);
         tc_commit(&b->s_full[t]);
     };
-    for (int i = first; i < last; ++i) {
+    for (int i = items.first; i < items.last; ++i) {
         AttentionItem it;
-        load_item(p.a.items + i, it);
+        load_item(items, i, it);
         const int n = uniform(t ? it.n_kv[1] : it.n_kv[0]), n_other = uniform(t ? it.n_kv[0] : it.n_kv[1]);
         const int n_keys = uniform(it.n_keys);
         if (n > 0) {
@@ -365,7 +371,7 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
             if (elect()) {
                 scores(smem + (2 + k_stage) * S::kTileBytes, false);
                 if (n == 1) tc_commit(&b->q_empty[t]);
-                free_stage(k_stage, n_other > 0);
+                tc_commit(&b->kv_empty[k_stage]);
             }
             __syncwarp();
             for (int j = 0; j < n; ++j) {
@@ -397,11 +403,11 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                     for (int s = 0; s < kKeys / 16; ++s)
                         if (s < v_steps)
                             mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + s * (2048 >> 4), p.pv_idesc, j > 0 || s > 0);
-                    free_stage(v_stage, j < n_other);
+                    tc_commit(&b->kv_empty[v_stage]);
                     if (j + 1 < n) {
                         scores(k_at, turn_over);
                         if (j + 2 == n) tc_commit(&b->q_empty[t]);
-                        free_stage(k_stage, j + 1 < n_other);
+                        tc_commit(&b->kv_empty[k_stage]);
                     } else {
                         if (turn_over) mbar_arrive(&b->turn[t ^ 1]);
                         tc_commit(&b->o_full[t]);
@@ -410,10 +416,11 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                 __syncwarp();
             }
         }
-        if (n < n_other) {  // stages that the other tile alone reads
-            const uint32_t to = stage + 2 * (uint32_t)(n_other - n);
-            stage = to % S::kStages;
-            phase ^= to / S::kStages & 1;
+        for (int x = 2 * n; x < 2 * n_other; ++x) {  // stages that the other tile alone reads
+            uint32_t at = 0;
+            if (!next_stage(at)) return;
+            if (elect()) mbar_arrive(&b->kv_empty[at]);
+            __syncwarp();
         }
     }
 }
@@ -429,15 +436,15 @@ __device__ __forceinline__ void store8(T* out, const uint32_t* o, float inv) {
 }
 
 template <int DP, typename T>
-__device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, int first, int last, int t, int warp, int lane) {
+__device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, const Items& items, int t, int warp, int lane) {
     const unsigned long long limit = p.a.wait_limit_ns;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
     const int row = warp * 32 + lane, tok = row / p.a.pack, head = row - tok * p.a.pack;
     uint32_t s_n = 0, o_n = 0;
-    for (int i = first; i < last; ++i) {
+    for (int i = items.first; i < items.last; ++i) {
         AttentionItem it;
-        load_item(p.a.items + i, it);
+        load_item(items, i, it);
         const int n_tok = t ? it.n_tok[1] : it.n_tok[0], n = t ? it.n_kv[1] : it.n_kv[0], slot = t ? it.slot[1] : it.slot[0];
         if (!n_tok) continue;
         const bool active = tok < n_tok, warp_active = warp * 32 < n_tok * p.a.pack;
@@ -600,15 +607,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_after();
     const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
     pdl_wait();
-    const int first = uniform(p.a.cta_ptr[blockIdx.x]), last = uniform(p.a.cta_ptr[blockIdx.x + 1]);
+    const Items items{p.a.items, b, uniform(p.a.cta_ptr[blockIdx.x]), uniform(p.a.cta_ptr[blockIdx.x + 1])};
+    if (threadIdx.x < 4 * kCached && items.first + (int)threadIdx.x / 4 < items.last)
+        reinterpret_cast<int4*>(b->items)[threadIdx.x] = reinterpret_cast<const int4*>(p.a.items + items.first)[threadIdx.x];
+    __syncthreads();
     if (warp < kMmaWarp) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        softmax_role<DP, T>(p, tmem, b, first, last, warp >> 2, warp & 3, lane);
+        softmax_role<DP, T>(p, tmem, b, items, warp >> 2, warp & 3, lane);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == kLoadWarp) load_role<DP>(p, &qm, &km, &vm, smem, b, first, last);
+        if (warp == kLoadWarp) load_role<DP>(p, &qm, &km, &vm, smem, b, items);
         if (warp == kMmaWarp || warp == kMmaWarp + 1) {
-            mma_role<DP>(p, smem, tmem, b, first, last, warp - kMmaWarp, lane);
+            mma_role<DP>(p, smem, tmem, b, items, warp - kMmaWarp, lane);
             // every product and every arrival that it announced is done before the block ends
             __syncwarp();
             if (elect()) tc_commit(&b->drained);

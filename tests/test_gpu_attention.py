@@ -128,6 +128,17 @@ def test_division_of_the_work(gc, n_ctas, causal):
     _run(gc, [260, 17, 128], [2600, 1111, 128], 2, 1, 64, causal, torch.float16, n_ctas=n_ctas)
 
 
+@pytest.mark.parametrize("D", [8, 24, 80])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+def test_pairs_of_tiles_beside_single_ones(gc, D, causal):
+    # one block takes pairs of query tiles, single tiles, tiles that see fewer keys than their neighbour and none at all,
+    # one after the other: each warp has to keep its place in the ring of stages through what only the other tile reads
+    lq = [1, 300, 5, 256, 64, 400, 1, 130, 700, 3]
+    lk = [900, 300, 1500, 40, 700, 0, 1, 2000, 650, 129]
+    _run(gc, lq, lk, 3, 3, D, causal, torch.bfloat16, n_ctas=1)
+    _run(gc, lq, lk, 2, 1, D, causal, torch.float16, n_ctas=2)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
 def test_peaked_and_growing_scores(gc, dtype):
     # scores whose maximum grows along the keys (the running rescale) and spreads over many powers of two
