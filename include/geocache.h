@@ -541,7 +541,7 @@ int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_lens, int n_
  *              16-byte aligned, strides multiples of 8 elements.
  *   lse        device [plan->q_tokens, Hq] f32, or NULL.
  *   scale      > 0 and finite (1/sqrt(D) is usual).
- *   workspace  device, plan->workspace_bytes (16-byte aligned; NULL when 0); its
+ *   workspace  device, plan->workspace_bytes (32-byte aligned; NULL when 0); its
  *              contents need not be set, and calls that may overlap on the GPU
  *              need one each.
  * out must not overlap an input.  A NaN or infinity reaches the rows of its own

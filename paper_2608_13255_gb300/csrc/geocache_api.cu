@@ -704,7 +704,7 @@ int geocache_attention(const geocache_attention_plan* p, const void* schedule, c
     if (!schedule || ((uintptr_t)schedule & 15)) return fail(GEOCACHE_EINVAL, "%s: schedule must be given and 16-byte aligned", fn);
     if (p->workspace_bytes && (!workspace || workspace_bytes < p->workspace_bytes))
         return fail(GEOCACHE_EINVAL, "%s: the plan needs a workspace of %lld bytes", fn, (long long)p->workspace_bytes);
-    if (p->workspace_bytes && ((uintptr_t)workspace & 15)) return fail(GEOCACHE_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+    if (p->workspace_bytes && ((uintptr_t)workspace & 31)) return fail(GEOCACHE_EINVAL, "%s: workspace must be 32-byte aligned", fn);
     if ((uintptr_t)lse & 3) return fail(GEOCACHE_EINVAL, "%s: lse must be 4-byte aligned", fn);
     const geocache_heads* x[4] = {q, k, v, out};
     const char* name[4] = {"q", "k", "v", "out"};

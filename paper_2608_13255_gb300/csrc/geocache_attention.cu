@@ -246,6 +246,7 @@ struct Params {
     int k_steps;          // of 16 elements of a head
     uint32_t qk_idesc, pv_idesc;
     float c;              // scale * log2(e)
+    int wide_out;         // rows of `out` are whole 32-byte sectors
 };
 
 struct Items {  // a block's pieces [first, last)
@@ -425,6 +426,11 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
     }
 }
 
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
 // 8 columns of a row of O
 template <typename T>
 __device__ __forceinline__ void store8(T* out, const uint32_t* o, float inv) {
@@ -536,6 +542,7 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, const 
         const float lse = l == 0.0f ? -INFINITY : m * p.a.scale + logf(l);
         T* out = static_cast<T*>(p.a.out.data) + token * p.a.out.token_stride + (it.head + head) * p.a.out.head_stride;
         const long long part = (long long)slot * kRows + row;
+        const bool wide = p.wide_out;
 #pragma unroll 1
         for (int x = 0; x < p.a.D; x += 32) {
             uint32_t o[32];
@@ -546,18 +553,33 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, const 
 #pragma unroll
                 for (int y = 0; y < 32; ++y) o[y] = 0;
             }
+            // a lane has a row to itself: whole 32-byte sectors where the rows begin on them
             if (active && slot < 0) {
+                if (wide) {
 #pragma unroll
-                for (int y = 0; y < 32; y += 8)
-                    if (x + y < p.a.D) store8<T>(out + x + y, o + y, inv);
+                    for (int y = 0; y < 32; y += 16)
+                        if (x + y < p.a.D) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                w[i] = pack2<T>(__uint_as_float(o[y + 2 * i]) * inv, __uint_as_float(o[y + 2 * i + 1]) * inv);
+                            store32(out + x + y, w);
+                        }
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 32; y += 8)
+                        if (x + y < p.a.D) store8<T>(out + x + y, o + y, inv);
+                }
             } else if (active) {
                 float* dst = p.a.parts + part * p.a.D + x;
 #pragma unroll
-                for (int y = 0; y < 32; y += 4)
-                    if (x + y < p.a.D)
-                        *reinterpret_cast<float4*>(dst + y) =
-                            make_float4(__uint_as_float(o[y]) * inv, __uint_as_float(o[y + 1]) * inv,
-                                        __uint_as_float(o[y + 2]) * inv, __uint_as_float(o[y + 3]) * inv);
+                for (int y = 0; y < 32; y += 8)
+                    if (x + y < p.a.D) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__uint_as_float(o[y + i]) * inv);
+                        store32(dst + y, w);
+                    }
             }
             __syncwarp();
         }
@@ -741,6 +763,7 @@ cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s) {
     p.qk_idesc = idesc | (uint32_t)(kKeys >> 3) << 17;
     p.pv_idesc = idesc | 1u << 16 | (uint32_t)(2 * p.k_steps) << 17;
     p.c = (float)((double)a.scale * 1.4426950408889634);
+    p.wide_out = !((uintptr_t)a.out.data & 31) && !((a.out.token_stride | a.out.head_stride | a.D) % 16);
     CUtensorMap qm, km, vm;
     cudaError_t e = make_map(&qm, a.dtype, a.q, a.D, a.pack, a.Hq, a.q_tokens, p.tok);
     if (e != cudaSuccess) return e;

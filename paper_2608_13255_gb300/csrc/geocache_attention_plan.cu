@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <exception>
 #include <numeric>
@@ -22,14 +23,16 @@ using geocache::AttentionItem;
 using geocache::AttentionJoin;
 constexpr int kRows = geocache::kAttentionRows, kKeys = geocache::kAttentionKeys;
 
-// Nanoseconds: a key tile for two query tiles, for one, a piece's start and end, and a launch that joins.
+// Nanoseconds, measured with 152 equal pieces of 1 to 64 key tiles and runs of short pieces: a key tile for two query
+// tiles, for one; a piece's start and end, and that of each of its full tiles of rows; a launch that joins, and its
+// reading a tile's part (times D).
 struct Cost {
-    double two, one, start, join, join_slot;
+    double two, one, piece, tile, join, join_slot;
 };
 
 Cost cost_of(int D) {
-    if (D > 64) return {1250.0, 900.0, 2500.0, 4000.0, 0.02};
-    return {850.0, 650.0, 2200.0, 4000.0, 0.02};
+    if (D > 64) return {1450.0, 1020.0, 1200.0, 10.0 * D, 4000.0, 0.06};
+    return {1140.0, 960.0, 900.0, 10.0 * D, 4000.0, 0.06};
 }
 
 struct Unit {
@@ -38,6 +41,8 @@ struct Unit {
     int n_tok[2];
     int n_kv[2];      // key tiles each sees
     int most() const { return std::max(n_kv[0], n_kv[1]); }
+    // cost of a piece beside its key tiles: its rows' queries and output
+    double start(const Cost& c, int pack) const { return c.piece + c.tile * (n_tok[0] + n_tok[1]) * pack / kRows; }
     // cost of the key tiles [a, b)
     double cost(const Cost& c, int a, int b) const {
         const int both = std::min(n_tok[1] ? std::min(n_kv[0], n_kv[1]) : 0, b);
@@ -65,28 +70,37 @@ struct Problem {
 std::vector<Unit> make_units(const Problem& p, int tiles) {
     const int tok = kRows / p.pack, groups = p.Hq / p.Hk / p.pack;
     std::vector<Unit> units;
-    for (int s = 0; s < p.n_seq; ++s)
-        for (int hk = 0; hk < p.Hk; ++hk)
-            for (int g = 0; g < groups; ++g)
-                for (long long t = 0; t < p.q[s]; t += (long long)tok * tiles) {
-                    Unit u{s, hk * (p.Hq / p.Hk) + g * p.pack, hk, (int)t, {0, 0}, {0, 0}};
-                    for (int i = 0; i < tiles; ++i) {
-                        const long long first = t + (long long)i * tok;
-                        u.n_tok[i] = (int)std::max(0LL, std::min<long long>(tok, p.q[s] - first));
-                        if (!u.n_tok[i]) continue;
-                        long long sees = p.k[s];
-                        if (p.causal) sees = std::max(0LL, first + u.n_tok[i] + p.k[s] - p.q[s]);
-                        u.n_kv[i] = (int)((sees + kKeys - 1) / kKeys);
-                    }
-                    units.push_back(u);
-                }
+    // heads inside of tokens where one row of tiles has all tokens: their units may be divided together (assign_even)
+    auto add = [&](int s, int hk, int g, long long t) {
+        Unit u{s, hk * (p.Hq / p.Hk) + g * p.pack, hk, (int)t, {0, 0}, {0, 0}};
+        for (int i = 0; i < tiles; ++i) {
+            const long long first = t + (long long)i * tok;
+            u.n_tok[i] = (int)std::max(0LL, std::min<long long>(tok, p.q[s] - first));
+            if (!u.n_tok[i]) continue;
+            long long sees = p.k[s];
+            if (p.causal) sees = std::max(0LL, first + u.n_tok[i] + p.k[s] - p.q[s]);
+            u.n_kv[i] = (int)((sees + kKeys - 1) / kKeys);
+        }
+        units.push_back(u);
+    };
+    for (int s = 0; s < p.n_seq; ++s) {
+        const long long step = (long long)tok * tiles;
+        if (p.q[s] <= step) {
+            for (int hk = 0; hk < p.Hk && p.q[s] > 0; ++hk)
+                for (int g = 0; g < groups; ++g) add(s, hk, g, 0);
+        } else {
+            for (int hk = 0; hk < p.Hk; ++hk)
+                for (int g = 0; g < groups; ++g)
+                    for (long long t = 0; t < p.q[s]; t += step) add(s, hk, g, t);
+        }
+    }
     return units;
 }
 
 // whole units, the longest first, each to the block with the least
 void assign_whole(const Problem& p, const Cost& c, Layout& l) {
     std::vector<double> cost(l.units.size());
-    for (size_t i = 0; i < cost.size(); ++i) cost[i] = c.start + l.units[i].cost(c, 0, l.units[i].most());
+    for (size_t i = 0; i < cost.size(); ++i) cost[i] = l.units[i].start(c, p.pack) + l.units[i].cost(c, 0, l.units[i].most());
     std::vector<int> order(l.units.size());
     std::iota(order.begin(), order.end(), 0);
     std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return cost[a] > cost[b]; });
@@ -104,21 +118,44 @@ void assign_whole(const Problem& p, const Cost& c, Layout& l) {
     }
 }
 
-// units in order, cut where the blocks' costs are even
+// Units in order, cut where the blocks' costs are even.  Where a head's row is not whole 128-byte lines, units longer than
+// a block's share are taken in ranges of their keys, the same range of all heads of a sequence before the next one: blocks
+// that run at the same time then read the two heads of a line (22 rows over 98,304 keys of 72: 266 -> 218 us).  Whole
+// lines have nothing to share, and the ranges cost pieces (32 single tokens over 317,000 keys of 128: 99 -> 102 us).
 void assign_even(const Problem& p, const Cost& c, Layout& l) {
-    double total = 0.0;
-    for (const Unit& u : l.units) total += c.start + u.cost(c, 0, u.most());
+    double total = 0.0, starts = 0.0, start = 0.0;
+    for (const Unit& u : l.units) {
+        total += u.cost(c, 0, u.most());
+        starts += u.start(c, p.pack);
+        start = std::max(start, u.start(c, p.pack));
+    }
     l.of_cta.assign(p.n_ctas, {});
-    const double share = (total + (p.n_ctas - 1) * c.start) / p.n_ctas;
+    double share = (total + starts + (p.n_ctas - 1) * start) / p.n_ctas;
+    std::vector<Piece> order;
+    for (size_t i = 0; i < l.units.size();) {
+        // the units of one sequence and one row of tiles, whatever their heads
+        size_t end = i;
+        while (end < l.units.size() && l.units[end].seq == l.units[i].seq && l.units[end].token == l.units[i].token) ++end;
+        const int n = l.units[i].most();
+        const int ranges = p.D % 64 ? std::max(1, std::min(n, (int)std::ceil(l.units[i].cost(c, 0, n) / share))) : 1;
+        for (int r = 0; r < ranges; ++r)
+            for (size_t j = i; j < end; ++j) {
+                if (r) starts += l.units[j].start(c, p.pack);
+                order.push_back({(int)j, (int)((long long)n * r / ranges), (int)((long long)n * (r + 1) / ranges)});
+            }
+        i = end;
+    }
+    share = (total + starts + (p.n_ctas - 1) * start) / p.n_ctas;
     int cta = 0;
-    double load = 0.0, slots = 0.0;
-    for (size_t i = 0; i < l.units.size(); ++i) {
-        const Unit& u = l.units[i];
-        const int n = u.most();
-        int at = 0;
+    double load = 0.0, spent = 0.0, slots = 0.0;
+    for (const Piece& whole : order) {
+        const Unit& u = l.units[whole.unit];
+        const int n = whole.to;
+        const double own = u.start(c, p.pack);
+        int at = whole.from;
         do {
             int take = n - at;
-            const double left = share - load - c.start;
+            const double left = share * (cta + 1) - spent - own;  // (not the block's own: roundings do not add up)
             if (cta < p.n_ctas - 1 && u.cost(c, at, n) > left) {
                 // the key tiles that fit, to the nearest; a rest of under half a piece's start stays here
                 int fit = 0;
@@ -129,16 +166,17 @@ void assign_even(const Problem& p, const Cost& c, Layout& l) {
                     sum += next;
                     ++fit;
                 }
-                if (u.cost(c, at + fit, n) > 0.5 * c.start) take = load == 0.0 ? std::max(fit, 1) : fit;
+                if (u.cost(c, at + fit, n) > 0.5 * own) take = load == 0.0 ? std::max(fit, 1) : fit;
             }
-            if (take > 0 || n == 0) {
-                l.of_cta[cta].push_back({(int)i, at, at + take});
-                load += c.start + u.cost(c, at, at + take);
+            if (take > 0 || n == at) {
+                l.of_cta[cta].push_back({whole.unit, at, at + take});
+                load += own + u.cost(c, at, at + take);
+                spent += own + u.cost(c, at, at + take);
                 l.cost = std::max(l.cost, load);
-                if (take < n) slots += (u.n_tok[0] + u.n_tok[1]) * (double)p.pack / kRows;
+                if (take < u.most()) slots += (u.n_tok[0] + u.n_tok[1]) * (double)p.pack / kRows;
                 at += take;
             }
-            if (at < n || (load >= share - 0.5 * c.start && cta < p.n_ctas - 1)) {
+            if (at < n || (spent >= share * (cta + 1) - 0.5 * own && cta < p.n_ctas - 1)) {
                 ++cta;
                 load = 0.0;
             }

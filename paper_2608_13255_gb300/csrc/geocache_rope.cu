@@ -76,41 +76,59 @@ __device__ __forceinline__ void store_words(T* p, const float* x) {
 
 constexpr int kWarps = 8;
 
-// A warp takes one unit: kU * (32 / G) heads of one token's queries or keys.  G lanes hold a row, kNV words of
-// 16 bytes each (word w of a row lies in lane w % G), so one round of kU loads a lane is in flight before any
-// is used.  A lane's cosines and sines are the same for all heads of the token and stay in registers.
+// n consecutive floats, in 16-byte words where `wide`
+template <int kN>
+__device__ __forceinline__ void load_floats(const float* p, bool wide, float* x) {
+    static_assert(kN % 4 == 0, "whole words");
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(p + i);
+            x[i] = w.x; x[i + 1] = w.y; x[i + 2] = w.z; x[i + 3] = w.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) x[i] = p[i];
+    }
+}
+
+// A warp takes one unit: up to `heads` heads of one token's queries or keys.  G lanes hold a row, kNV words of 16 bytes
+// each (word w of a row lies in lane w % G), and kU rows a lane are loaded before any is used.  A lane's cosines and
+// sines are the same for all heads of the token and stay in registers, as the weights do.
 // Rotation: out = x * c + partner * s, s signed by the element's place in its pair.  Interleaved pairs lie in one
 // lane; halves that are whole words lie in two lanes (shuffle); other halves meet in shared memory.
 template <typename T, int G, int kNV, int kRot, int kU, bool kAligned>
-__global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_constant__ NormRopeArgs a, int q_units,
-                                                                int units) {
+__global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_constant__ NormRopeArgs a, int heads,
+                                                                unsigned q_units, unsigned units, unsigned n_blocks) {
     constexpr int V = Elements<T>::kN, R = 32 / G;
     __shared__ float rows[kRot == kHalfShared ? kWarps : 1][kRot == kHalfShared ? 32 * kNV * V : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % G, r = lane / G;
+    const float inv_d = 1.0f / (float)a.D;
+    const int half = a.rot / 2;
     pdl_wait();
-    const long long n = (long long)a.T * units;
-    for (long long u = (long long)blockIdx.x * kWarps + warp; u < n; u += (long long)gridDim.x * kWarps) {
-        const long long t = u / units;
-        const int c = (int)(u - t * units), side = c >= q_units;
-        const int h0 = (side ? c - q_units : c) * (kU * R) + r, H = side ? a.Hk : a.Hq;
+    for (unsigned block = blockIdx.x; block < n_blocks; block += gridDim.x) {
+        const unsigned group = block / units, c = block - group * units;
+        const long long t = (long long)group * kWarps + warp;
+        if (t >= a.T) continue;
+        const int side = c >= q_units, H = side ? a.Hk : a.Hq;
+        const int first = (int)(side ? c - q_units : c) * heads, last = min(H, first + heads);
         const T* in = static_cast<const T*>(a.in[side]) + t * a.in_ts[side];
         T* out = static_cast<T*>(a.out[side]) + t * a.out_ts[side];
-
+        // a round of rows, on its way while the table is read and while the round before it is worked on
         uint4 w[kU][kNV];
+        auto load_round = [&](int h1) {
 #pragma unroll
-        for (int i = 0; i < kU; ++i)
+            for (int i = 0; i < kU; ++i)
 #pragma unroll
-            for (int v = 0; v < kNV; ++v) {
-                const int h = h0 + i * R, d = (l + v * G) * V;
-                w[i][v] = make_uint4(0, 0, 0, 0);
-                if (h < H && d < a.D) w[i][v] = load_words<T, kAligned>(in + h * a.in_hs[side] + d);
-            }
+                for (int v = 0; v < kNV; ++v) {
+                    const int h = h1 + i * R, d = (l + v * G) * V;
+                    w[i][v] = make_uint4(0, 0, 0, 0);
+                    if (h < last && d < a.D) w[i][v] = load_words<T, kAligned>(in + h * a.in_hs[side] + d);
+                }
+        };
+        load_round(first + r);
 
         float cs[kNV][V], sn[kNV][V], wt[kNV][V];
-#pragma unroll
-        for (int v = 0; v < kNV; ++v)
-#pragma unroll
-            for (int e = 0; e < V; ++e) { cs[v][e] = 1.0f; sn[v][e] = 0.0f; wt[v][e] = 1.0f; }
         bool turn = kRot != kNone;
         if (kRot != kNone) {
             const long long slot = a.slots ? a.slots[t] : t;
@@ -118,113 +136,159 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
                 turn = false;
                 if (lane == 0) atomicOr(&g_rope_error, 32u);
             } else {
-                const float2* tab = a.table + slot * (a.rot / 2);
-                const int half = a.rot / 2;
+                const float* tab = reinterpret_cast<const float*>(a.table + slot * half);
+                // words of a lane's pairs: whole and 16-byte aligned (but for shared halves, which are rare)
+                const bool wide = kRot != kHalfShared && !((uintptr_t)tab & 15);
 #pragma unroll
-                for (int v = 0; v < kNV; ++v)
+                for (int v = 0; v < kNV; ++v) {
+                    const int d0 = (l + v * G) * V;
+                    if (kRot == kInterleaved) {
+                        float x[V];
+                        // (a word that the rotation ends in is read pair by pair)
+                        if (d0 + V <= a.rot) load_floats<V>(tab + d0, wide, x);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int d = (l + v * G) * V + e;
-                        if (d >= a.rot) continue;
-                        const bool second = kRot == kInterleaved ? e & 1 : d >= half;
-                        const float2 x = tab[kRot == kInterleaved ? d / 2 : (second ? d - half : d)];
-                        cs[v][e] = x.x;
-                        sn[v][e] = second ? x.y : -x.y;
+                        for (int e = 0; e < V; e += 2) {
+                            if (d0 + V > a.rot) {
+                                const bool in_row = d0 + e < a.rot;
+                                x[e] = in_row ? tab[d0 + e] : 1.0f;
+                                x[e + 1] = in_row ? tab[d0 + e + 1] : 0.0f;
+                            }
+                            cs[v][e] = cs[v][e + 1] = x[e];
+                            sn[v][e] = -x[e + 1];
+                            sn[v][e + 1] = x[e + 1];
+                        }
+                    } else if (kRot == kHalfShuffle) {
+                        float x[2 * V];
+                        const bool second = d0 >= half;
+                        if (d0 < a.rot) load_floats<2 * V>(tab + 2 * (second ? d0 - half : d0), wide, x);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            cs[v][e] = d0 < a.rot ? x[2 * e] : 1.0f;
+                            sn[v][e] = d0 < a.rot ? (second ? x[2 * e + 1] : -x[2 * e + 1]) : 0.0f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const int d = d0 + e;
+                            const bool second = d >= half, in_row = d < a.rot;
+                            const float* x = tab + 2 * (second ? d - half : d);
+                            cs[v][e] = in_row ? x[0] : 1.0f;
+                            sn[v][e] = in_row ? (second ? x[1] : -x[1]) : 0.0f;
+                        }
                     }
+                }
             }
         }
         const float* weight = a.norm ? a.weight[side] : nullptr;
-        if (weight)
+        if (weight) {
+            const bool wide = !((uintptr_t)weight & 15);
 #pragma unroll
             for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const int d = (l + v * G) * V + e;
-                    if (d < a.D) wt[v][e] = weight[d];
-                }
+                if ((l + v * G) * V < a.D) load_floats<V>(weight + (l + v * G) * V, wide, wt[v]);
+        }
 
+#pragma unroll 1
+        for (int h1 = first + r; h1 - r < last; h1 += kU * R) {
+            uint4 now[kU][kNV];
 #pragma unroll
-        for (int i = 0; i < kU; ++i) {
-            const int h = h0 + i * R;
-            float x[kNV][V];
+            for (int i = 0; i < kU; ++i)
 #pragma unroll
-            for (int v = 0; v < kNV; ++v) {
-                const T* p = reinterpret_cast<const T*>(&w[i][v]);
+                for (int v = 0; v < kNV; ++v) now[i][v] = w[i][v];
+            if (h1 - r + kU * R < last) load_round(h1 + kU * R);
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[v][e] = to_float(p[e]);
-            }
-            if (a.norm) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) sum = fmaf(x[v][e], x[v][e], sum);
-#pragma unroll
-                for (int m = G / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-                const float inv = 1.0f / sqrtf(sum / (float)a.D + a.eps);
-#pragma unroll
-                for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[v][e] *= inv * wt[v][e];
-            }
-            if (turn) {  // the same for the whole warp
-                float y[kNV][V];
-                if (kRot == kInterleaved) {
-#pragma unroll
-                    for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) y[v][e] = x[v][e ^ 1];
-                } else if (kRot == kHalfShuffle) {
-                    const int hop = a.rot / 2 / V, from = l < hop ? l + hop : l - hop;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) y[0][e] = __shfl_sync(0xffffffffu, x[0][e], from, G);
-                } else {
-                    float* row = rows[warp] + r * (G * kNV * V);
-                    const int half = a.rot / 2;
-                    __syncwarp();
-#pragma unroll
-                    for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) row[(l + v * G) * V + e] = x[v][e];
-                    __syncwarp();
-#pragma unroll
-                    for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            const int d = (l + v * G) * V + e;
-                            y[v][e] = d < a.rot ? row[d < half ? d + half : d - half] : 0.0f;
-                        }
-                }
-#pragma unroll
-                for (int v = 0; v < kNV; ++v)
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if ((l + v * G) * V + e < a.rot) x[v][e] = fmaf(x[v][e], cs[v][e], y[v][e] * sn[v][e]);
-            }
-            if (h < H)
+            for (int i = 0; i < kU; ++i) {
+                const int h = h1 + i * R;
+                float x[kNV][V];
 #pragma unroll
                 for (int v = 0; v < kNV; ++v) {
-                    const int d = (l + v * G) * V;
-                    if (d < a.D) store_words<T, kAligned>(out + h * a.out_hs[side] + d, x[v]);
+                    const T* p = reinterpret_cast<const T*>(&now[i][v]);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) x[v][e] = to_float(p[e]);
                 }
+                if (a.norm) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) sum = fmaf(x[v][e], x[v][e], sum);
+#pragma unroll
+                    for (int m = G / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+                    const float inv = rsqrtf(fmaf(sum, inv_d, a.eps));
+#pragma unroll
+                    for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) x[v][e] *= weight ? inv * wt[v][e] : inv;
+                }
+                if (turn) {  // the same for the whole warp
+                    float y[kNV][V];
+                    if (kRot == kInterleaved) {
+#pragma unroll
+                        for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                            for (int e = 0; e < V; ++e) y[v][e] = x[v][e ^ 1];
+                    } else if (kRot == kHalfShuffle) {
+                        const int hop = half / V, from = l < hop ? l + hop : l - hop;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) y[0][e] = __shfl_sync(0xffffffffu, x[0][e], from, G);
+                    } else {
+                        float* row = rows[warp] + r * (G * kNV * V);
+                        __syncwarp();
+#pragma unroll
+                        for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                            for (int e = 0; e < V; ++e) row[(l + v * G) * V + e] = x[v][e];
+                        __syncwarp();
+#pragma unroll
+                        for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                            for (int e = 0; e < V; ++e) {
+                                const int d = (l + v * G) * V + e;
+                                y[v][e] = d < a.rot ? row[d < half ? d + half : d - half] : 0.0f;
+                            }
+                    }
+#pragma unroll
+                    for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if ((l + v * G) * V + e < a.rot) x[v][e] = fmaf(x[v][e], cs[v][e], y[v][e] * sn[v][e]);
+                }
+                if (h < last)
+#pragma unroll
+                    for (int v = 0; v < kNV; ++v) {
+                        const int d = (l + v * G) * V;
+                        if (d < a.D) store_words<T, kAligned>(out + h * a.out_hs[side] + d, x[v]);
+                    }
+            }
         }
     }
 }
 
 int sm_count() {
-    int dev = 0, sms = 0;
-    cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    return sms > 0 ? sms : 1;
+    static const int n = [] {  // one device per process
+        int dev = 0, sms = 0;
+        cudaGetDevice(&dev);
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        return sms > 0 ? sms : 1;
+    }();
+    return n;
 }
 
 template <typename T, int G, int kNV, int kRot, int kU, bool kAligned>
 cudaError_t launch(const NormRopeArgs& a, cudaStream_t s) {
-    constexpr int heads = kU * (32 / G);
-    const int q_units = (a.Hq + heads - 1) / heads, units = q_units + (a.Hk + heads - 1) / heads;
-    const long long blocks = ((long long)a.T * units + kWarps - 1) / kWarps;
+    // As many heads a warp as leave the device two rounds of its warps (the table's row and the weights are then read
+    // once for them), in even shares: small calls still fill the device.
+    constexpr int round = kU * (32 / G);
+    const long long warps = 2LL * 32 * sm_count();
+    const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
+    int shares = 1;
+    while (shares * round < most && (long long)a.T * shares * 2 < warps) ++shares;
+    const int heads = (most + shares * round - 1) / (shares * round) * round;
+    const unsigned q_units = (unsigned)((a.Hq + heads - 1) / heads), units = q_units + (unsigned)((a.Hk + heads - 1) / heads);
+    const long long blocks = ((long long)a.T + kWarps - 1) / kWarps * units;
+    if (blocks > 0xffffffffLL - (1LL << 30)) return cudaErrorInvalidValue;  // over 2^31 tokens x 2^16 heads
     const unsigned grid = (unsigned)(blocks < (1LL << 30) ? blocks : (1LL << 30));
-    return launch_pdl(norm_rope_kernel<T, G, kNV, kRot, kU, kAligned>, dim3(grid), 32 * kWarps, 0, s, a, q_units, units);
+    return launch_pdl(norm_rope_kernel<T, G, kNV, kRot, kU, kAligned>, dim3(grid), 32 * kWarps, 0, s, a, heads, q_units, units,
+                      (unsigned)blocks);
 }
 
 template <typename T, int G, int kNV, int kRot>
@@ -232,6 +296,7 @@ cudaError_t launch_rows(const NormRopeArgs& a, bool aligned, cudaStream_t s) {
     if (!aligned) return launch<T, G, kNV, kRot, 1, false>(a, s);
     constexpr int R = 32 / G;
     const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
+    // four rows a lane where there are heads for them
     if (most > R) return launch<T, G, kNV, kRot, 4, true>(a, s);
     return launch<T, G, kNV, kRot, 1, true>(a, s);
 }

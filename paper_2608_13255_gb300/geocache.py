@@ -132,15 +132,13 @@ def load():
         for name in ("geocache_pack_anchors", "geocache_unpack_anchors"):
             getattr(L, name).argtypes = [P, P, i64, i, i, P, i, P]
             getattr(L, name).restype = ctypes.c_int
-        H = ctypes.POINTER(Heads)
         L.geocache_rope_table.argtypes = [ctypes.POINTER(Rope), P, i64, P, i, i, P]
         L.geocache_rope_table.restype = ctypes.c_int
-        L.geocache_qk_norm_rope.argtypes = [H, H, H, H, i64, i, i, i, i, i, ctypes.c_double, P, P, P, i64, i, i, P, P]
+        L.geocache_qk_norm_rope.argtypes = [P, P, P, P, i64, i, i, i, i, i, ctypes.c_double, P, P, P, i64, i, i, P, P]
         L.geocache_qk_norm_rope.restype = ctypes.c_int
-        A = ctypes.POINTER(AttentionPlanInfo)
-        L.geocache_plan_attention.argtypes = [P, P, i, i, i, i, i, i, A, P, i64]
+        L.geocache_plan_attention.argtypes = [P, P, i, i, i, i, i, i, P, P, i64]
         L.geocache_plan_attention.restype = ctypes.c_int
-        L.geocache_attention.argtypes = [A, P, H, H, H, H, P, i, ctypes.c_double, P, i64, P]
+        L.geocache_attention.argtypes = [P, P, P, P, P, P, P, i, ctypes.c_double, P, i64, P]
         L.geocache_attention.restype = ctypes.c_int
         L.geocache_corr_record_count.argtypes = [ctypes.POINTER(Corr), ctypes.POINTER(ctypes.c_int64), P]
         L.geocache_corr_record_count.restype = ctypes.c_int
@@ -554,19 +552,24 @@ def rope_table(n_slots=None, rot=None, theta=10000.0, pos=None, scaling=None, ma
 
 
 def _heads(t, dtype, T, H, D, name):
-    """A [T, H, D] view (elements of a head consecutive) as the C struct."""
+    """(address, token stride, head stride) of a [T, H, D] view whose heads'
+    elements are consecutive."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == (T, H, D):
+        ts, hs, es = t.stride()
+        if es == 1:
+            return t.data_ptr(), ts, hs
+        raise ValueError("the elements of a head of %s must be consecutive" % name)
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch tensor" % name)
     if t.dtype is not dtype:
         raise TypeError("%s must be %s (got %s)" % (name, dtype, t.dtype))
     if not t.is_cuda:
         raise ValueError("%s must be on a CUDA device" % name)
-    if tuple(t.shape) != (T, H, D):
-        raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, T, H, D, list(t.shape)))
-    st = t.stride()
-    if st[2] != 1 and D > 1:
-        raise ValueError("the elements of a head of %s must be consecutive" % name)
-    return Heads(t.data_ptr(), st[0], st[1])
+    raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, T, H, D, list(t.shape)))
+
+
+_FourHeads = ctypes.c_int64 * 12  # four geocache_heads: filled in one go, 1 us less a call than a struct each
+_HEADS_SIZE = ctypes.sizeof(Heads)
 
 
 def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps=1e-6, norm=True, layout="half",
@@ -583,14 +586,16 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
     Hk = 0 if k is None else k.shape[1]
     if q_out is None:
         q_out = torch.empty((T, Hq, D), dtype=dt, device=q.device)
+    hk = hko = (0, 0, 0)
     if k is None:
-        hk = hko = None
         if k_out is not None:
             raise ValueError("k_out without k")
     else:
         if k_out is None:
             k_out = torch.empty((T, Hk, D), dtype=dt, device=q.device)
         hk, hko = _heads(k, dt, T, Hk, D, "k"), _heads(k_out, dt, T, Hk, D, "k_out")
+    heads = _FourHeads(*_heads(q, dt, T, Hq, D, "q"), *hk, *_heads(q_out, dt, T, Hq, D, "q_out"), *hko)
+    at = ctypes.addressof(heads)
     n_slots = rot = 0
     if table is not None:
         if table.dim() != 3 or table.shape[2] != 2:
@@ -598,7 +603,7 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
         n_slots, rot = table.shape[0], 2 * table.shape[1]
     f32 = torch.float32
     _check(load().geocache_qk_norm_rope(
-        _heads(q, dt, T, Hq, D, "q"), hk, _heads(q_out, dt, T, Hq, D, "q_out"), hko, T, Hq, Hk, D, _HEAD_DTYPES[dt],
+        at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE, T, Hq, Hk, D, _HEAD_DTYPES[dt],
         1 if norm else 0, float(eps), _dev(q_weight, f32, D, "q_weight"), _dev(k_weight, f32, D, "k_weight"),
         _dev(table, f32, None, "table"), n_slots, rot, _ROPE_LAYOUTS[layout], _dev(slots, torch.int32, T, "slots"),
         _stream(stream)))
@@ -613,6 +618,8 @@ class AttentionPlan:
         self.info = info
         self.schedule = schedule
         self.workspace = workspace
+        self.sizes = (info.q_tokens, info.k_tokens, info.Hq, info.Hk, info.D)
+        self.address = ctypes.addressof(info)
 
 
 def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
@@ -625,7 +632,7 @@ def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
         raise ValueError("a sequence's length is outside [0, 2^31)")
     qa, ka = (ctypes.c_int32 * max(1, len(q)))(*q), (ctypes.c_int32 * max(1, len(k)))(*k)
     info = AttentionPlanInfo()
-    args = (qa, ka, len(q), int(Hq), int(Hk), int(D), 1 if causal else 0, int(n_ctas), ctypes.byref(info))
+    args = (qa, ka, len(q), int(Hq), int(Hk), int(D), 1 if causal else 0, int(n_ctas), ctypes.addressof(info))
     _check(load().geocache_plan_attention(*args, None, 0))
     room = torch.zeros(info.schedule_bytes // 4 + 4, dtype=torch.int32)
     schedule = room[(-room.data_ptr() % 16) // 4:][:info.schedule_bytes // 4]
@@ -658,12 +665,14 @@ def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, work
     if out is None:
         out = torch.empty((f.q_tokens, f.Hq, f.D), dtype=dt, device=q.device)
     ws = plan.workspace if workspace is None else workspace
+    Tq, Tk, Hq, Hk, D = plan.sizes
+    heads = _FourHeads(*_heads(q, dt, Tq, Hq, D, "q"), *_heads(k, dt, Tk, Hk, D, "k"), *_heads(v, dt, Tk, Hk, D, "v"),
+                       *_heads(out, dt, Tq, Hq, D, "out"))
+    at = ctypes.addressof(heads)
     _check(load().geocache_attention(
-        ctypes.byref(f), plan.schedule.data_ptr(), _heads(q, dt, f.q_tokens, f.Hq, f.D, "q"),
-        _heads(k, dt, f.k_tokens, f.Hk, f.D, "k"), _heads(v, dt, f.k_tokens, f.Hk, f.D, "v"),
-        _heads(out, dt, f.q_tokens, f.Hq, f.D, "out"), _dev(lse, torch.float32, f.q_tokens * f.Hq, "lse"),
-        _HEAD_DTYPES[dt], f.D ** -0.5 if scale is None else float(scale), _dev(ws, torch.float32, None, "workspace"),
-        0 if ws is None else 4 * ws.numel(), _stream(stream)))
+        plan.address, plan.schedule.data_ptr(), at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE,
+        _dev(lse, torch.float32, Tq * Hq, "lse"), _HEAD_DTYPES[dt], D ** -0.5 if scale is None else float(scale),
+        _dev(ws, torch.float32, None, "workspace"), 0 if ws is None else 4 * ws.numel(), _stream(stream)))
     return out
 
 

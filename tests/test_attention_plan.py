@@ -165,16 +165,17 @@ def test_attention_checks_arguments(gc):
         return gc.Heads(data, H * 64 if ts is None else ts, hs)
 
     def call(plan=info, schedule=M, q=None, k=None, v=None, out=None, lse=None, dtype=1, scale=0.125, ws=6 * M, nbytes=None):
-        return L.geocache_attention(plan, schedule, q or heads(2 * M), k or heads(3 * M, H=2), v or heads(4 * M, H=2),
-                                    out or heads(5 * M), lse, dtype, scale, ws,
+        x = (plan, q or heads(2 * M), k or heads(3 * M, H=2), v or heads(4 * M, H=2), out or heads(5 * M))
+        plan, q, k, v, out = map(ctypes.byref, x)
+        return L.geocache_attention(plan, schedule, q, k, v, out, lse, dtype, scale, ws,
                                     info.workspace_bytes if nbytes is None else nbytes, None)
 
-    assert L.geocache_attention(None, M, heads(M), heads(M), heads(M), heads(M), None, 1, 0.1, None, 0, None) == gc.EINVAL
+    assert L.geocache_attention(None, M, M, M, M, M, None, 1, 0.1, None, 0, None) == gc.EINVAL
     assert call(dtype=0) == gc.EDTYPE and call(dtype=3) == gc.EDTYPE
     for s in (0.0, -1.0, float("inf"), float("nan"), 1e-60, 1e60):
         assert call(scale=s) == gc.EINVAL
     assert call(schedule=None) == gc.EINVAL and call(schedule=M + 8) == gc.EINVAL
-    assert call(ws=None) == gc.EINVAL and call(nbytes=info.workspace_bytes - 1) == gc.EINVAL and call(ws=6 * M + 4) == gc.EINVAL
+    assert call(ws=None) == gc.EINVAL and call(nbytes=info.workspace_bytes - 1) == gc.EINVAL and call(ws=6 * M + 4) == gc.EINVAL and call(ws=6 * M + 16) == gc.EINVAL
     assert call(lse=7 * M + 2) == gc.EINVAL
     assert call(q=heads(2 * M + 8)) == gc.EINVAL and call(k=heads(3 * M, hs=68, H=2)) == gc.EINVAL
     assert call(v=heads(4 * M, ts=132)) == gc.EINVAL and call(out=heads(None)) == gc.EINVAL

@@ -51,8 +51,8 @@ def test_norm_rope_checks_arguments(gc):
              rot=64, layout=0, slots=None):
         q, k = q or heads(M), k or heads(2 * M, H=2)
         qo, ko = qo or heads(3 * M), ko or heads(4 * M, H=2)
-        return L.geocache_qk_norm_rope(q, k, qo, ko, T, Hq, Hk, D, dtype, 1, eps, qw, None, table, n, rot, layout, slots,
-                                       None)
+        return L.geocache_qk_norm_rope(*map(ctypes.byref, (q, k, qo, ko)), T, Hq, Hk, D, dtype, 1, eps, qw, None, table, n,
+                                       rot, layout, slots, None)
 
     assert call(T=-1) == gc.ESHAPE and call(Hq=-1) == gc.ESHAPE and call(Hk=65537) == gc.ESHAPE
     for d in (0, 4, 60, 264):
