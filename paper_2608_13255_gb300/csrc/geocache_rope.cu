@@ -40,9 +40,6 @@ struct Elements {  // 16 bytes of a row
     static constexpr int kN = 16 / sizeof(T);
 };
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 template <typename T>
 __device__ __forceinline__ T from_float(float x);
 template <>
@@ -54,23 +51,60 @@ __device__ __forceinline__ __half from_float<__half>(float x) { return __float2h
 
 template <typename T, bool kAligned>
 __device__ __forceinline__ uint4 load_words(const T* p) {
-    if (kAligned) return __ldcs(reinterpret_cast<const uint4*>(p));
-    union { uint4 w; T e[Elements<T>::kN]; } u;
+    if constexpr (kAligned) {
+        return __ldcs(reinterpret_cast<const uint4*>(p));
+    } else {
+        union { uint4 w; T e[Elements<T>::kN]; } u;
 #pragma unroll
-    for (int e = 0; e < Elements<T>::kN; ++e) u.e[e] = p[e];
-    return u.w;
+        for (int e = 0; e < Elements<T>::kN; ++e) u.e[e] = p[e];
+        return u.w;
+    }
+}
+
+// 16 bytes of a row as floats, and back (two values a conversion)
+__device__ __forceinline__ void widen(const uint4& w, float* x, __nv_bfloat16) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void widen(const uint4& w, float* x, __half) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void widen(const uint4& w, float* x, float) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ uint32_t narrow(float lo, float hi, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t narrow(float lo, float hi, __half) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ uint4 narrow_words(const float* x) {
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    else
+        return make_uint4(narrow(x[0], x[1], T()), narrow(x[2], x[3], T()), narrow(x[4], x[5], T()), narrow(x[6], x[7], T()));
 }
 
 template <typename T, bool kAligned>
 __device__ __forceinline__ void store_words(T* p, const float* x) {
-    union { uint4 w; T e[Elements<T>::kN]; } u;
-#pragma unroll
-    for (int e = 0; e < Elements<T>::kN; ++e) u.e[e] = from_float<T>(x[e]);
-    if (kAligned) {
-        *reinterpret_cast<uint4*>(p) = u.w;
+    if constexpr (kAligned) {
+        *reinterpret_cast<uint4*>(p) = narrow_words<T>(x);
     } else {
 #pragma unroll
-        for (int e = 0; e < Elements<T>::kN; ++e) p[e] = u.e[e];
+        for (int e = 0; e < Elements<T>::kN; ++e) p[e] = from_float<T>(x[e]);
     }
 }
 
@@ -201,9 +235,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
                 float x[kNV][V];
 #pragma unroll
                 for (int v = 0; v < kNV; ++v) {
-                    const T* p = reinterpret_cast<const T*>(&now[i][v]);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[v][e] = to_float(p[e]);
+                    widen(now[i][v], x[v], T());
                 }
                 if (a.norm) {
                     float sum = 0.0f;
@@ -231,19 +263,21 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
 #pragma unroll
                         for (int e = 0; e < V; ++e) y[0][e] = __shfl_sync(0xffffffffu, x[0][e], from, G);
                     } else {
+                        // element e of word w at [e][w]: neither side meets a bank twice
                         float* row = rows[warp] + r * (G * kNV * V);
                         __syncwarp();
 #pragma unroll
                         for (int v = 0; v < kNV; ++v)
 #pragma unroll
-                            for (int e = 0; e < V; ++e) row[(l + v * G) * V + e] = x[v][e];
+                            for (int e = 0; e < V; ++e) row[e * (G * kNV) + l + v * G] = x[v][e];
                         __syncwarp();
 #pragma unroll
                         for (int v = 0; v < kNV; ++v)
 #pragma unroll
                             for (int e = 0; e < V; ++e) {
                                 const int d = (l + v * G) * V + e;
-                                y[v][e] = d < a.rot ? row[d < half ? d + half : d - half] : 0.0f;
+                                const int at = d < half ? d + half : d - half;
+                                y[v][e] = d < a.rot ? row[at % V * (G * kNV) + at / V] : 0.0f;
                             }
                     }
 #pragma unroll
@@ -263,6 +297,130 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
     }
 }
 
+// The common rows: an even number of words, two a lane, and a rotation that whole words take part in.  Rotated halves lie
+// in one lane as interleaved pairs do (lane l: word l of each half; the unrotated words two by two behind them), and
+// nothing but the sum of squares crosses lanes.  With the weights folded into the rotation a pair (a, b) becomes
+//     inv (a ca - b sb, a sa + b cb),  ca = w_a c, sa = w_a s, cb = w_b c, sb = w_b s,
+// three products and three sums an element in place of about ten operations of the general kernel, which is bound by
+// issue (24,576 tokens x 32 heads of 128 in bf16: 84 -> 73 us, 5.7 TB/s; halves of 64: 74 -> 51 us).
+// kFull: all lanes have words and the whole head is rotated (heads of 64, 128 and 256 in 16 bits), known to the compiler
+// (73 us; 79 without).
+template <typename T, int G, bool kInter, bool kFull, int kU>
+__global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const __grid_constant__ NormRopeArgs a, int heads,
+                                                                         unsigned q_units, unsigned units, unsigned n_blocks) {
+    constexpr int V = Elements<T>::kN, R = 32 / G;
+    const int D = kFull ? 2 * G * V : a.D, rot = kFull ? D : a.rot;
+    const int lane_words = D / (2 * V), turned = kInter ? 0 : rot / (2 * V);  // lanes with words; with rotated halves
+    const float inv_d = 1.0f / (float)D;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % G, r = lane / G;
+    const bool on = kFull || l < lane_words;
+    // the lane's two words, by their first elements
+    const int da = V * (kFull || kInter || l < turned ? l : turned + l), db = V * (kInter || kFull || l >= turned ? lane_words + l : turned + l);
+    pdl_wait();
+    for (unsigned block = blockIdx.x; block < n_blocks; block += gridDim.x) {
+        const unsigned group = block / units, c = block - group * units;
+        const long long t = (long long)group * kWarps + warp;
+        if (t >= a.T) continue;
+        const int side = c >= q_units, H = side ? a.Hk : a.Hq;
+        const int first = (int)(side ? c - q_units : c) * heads, last = min(H, first + heads);
+        const long long in_hs = a.in_hs[side], out_hs = a.out_hs[side];
+        const T* in = static_cast<const T*>(a.in[side]) + t * a.in_ts[side] + (first + r) * in_hs;
+        T* out = static_cast<T*>(a.out[side]) + t * a.out_ts[side] + (first + r) * out_hs;
+        uint4 w[kU][2];
+        auto load_round = [&](int h1) {
+#pragma unroll
+            for (int i = 0; i < kU; ++i)
+                if (on && h1 + i * R < last) {
+                    w[i][0] = __ldcs(reinterpret_cast<const uint4*>(in + i * R * in_hs + da));
+                    w[i][1] = __ldcs(reinterpret_cast<const uint4*>(in + i * R * in_hs + db));
+                }
+            in += kU * R * in_hs;
+        };
+#pragma unroll
+        for (int i = 0; i < kU; ++i) w[i][0] = w[i][1] = make_uint4(0, 0, 0, 0);
+        load_round(first + r);
+
+        // pair i: elements (2 i, 2 i + 1) of the lane's words, or (i, i) of the first and the second
+        float ca[V], sa[V], cb[V], sb[V];
+        {
+            float cs[2 * V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) { cs[2 * i] = 1.0f; cs[2 * i + 1] = 0.0f; }
+            const long long slot = rot == 0 ? 0 : a.slots ? a.slots[t] : t;
+            if (rot && (slot < 0 || slot >= a.n_slots)) {
+                if (lane == 0) atomicOr(&g_rope_error, 32u);
+            } else if (rot && on) {
+                const float* tab = reinterpret_cast<const float*>(a.table + slot * (rot / 2));
+                const bool wide = !((uintptr_t)tab & 15);
+                if (kInter) {
+                    if (da < rot) load_floats<V>(tab + da, wide, cs);
+                    if (db < rot) load_floats<V>(tab + db, wide, cs + V);
+                } else if (l < turned) {
+                    load_floats<2 * V>(tab + 2 * da, wide, cs);
+                }
+            }
+            float wt[2][V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) wt[0][e] = wt[1][e] = 1.0f;
+            const float* weight = a.norm ? a.weight[side] : nullptr;
+            if (weight && on) {
+                const bool wide = !((uintptr_t)weight & 15);
+                load_floats<V>(weight + da, wide, wt[0]);
+                load_floats<V>(weight + db, wide, wt[1]);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float wa = kInter ? wt[i / (V / 2)][2 * i % V] : wt[0][i], wb = kInter ? wt[i / (V / 2)][2 * i % V + 1] : wt[1][i];
+                ca[i] = wa * cs[2 * i];
+                sa[i] = wa * cs[2 * i + 1];
+                cb[i] = wb * cs[2 * i];
+                sb[i] = wb * cs[2 * i + 1];
+            }
+        }
+
+#pragma unroll 1
+        for (int h1 = first + r; h1 - r < last; h1 += kU * R) {
+            uint4 now[kU][2];
+#pragma unroll
+            for (int i = 0; i < kU; ++i) { now[i][0] = w[i][0]; now[i][1] = w[i][1]; }
+            if (h1 - r + kU * R < last) load_round(h1 + kU * R);
+#pragma unroll
+            for (int i = 0; i < kU; ++i) {
+                float x[2][V];
+                widen(now[i][0], x[0], T());
+                widen(now[i][1], x[1], T());
+                float inv = 1.0f;
+                if (a.norm) {
+                    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        sum[0] = fmaf(x[0][e], x[0][e], sum[0]);
+                        sum[1] = fmaf(x[1][e], x[1][e], sum[1]);
+                    }
+                    sum[0] += sum[1];
+#pragma unroll
+                    for (int m = G / 2; m > 0; m >>= 1) sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], m);
+                    inv = rsqrtf(fmaf(sum[0], inv_d, a.eps));
+                }
+                float z[2][V];
+#pragma unroll
+                for (int p = 0; p < V; ++p) {
+                    const int va = kInter ? p / (V / 2) : 0, ea = kInter ? 2 * p % V : p;
+                    const int vb = kInter ? va : 1, eb = kInter ? ea + 1 : p;
+                    const float xa = x[va][ea], xb = x[vb][eb];
+                    z[va][ea] = fmaf(xa, ca[p], -(xb * sb[p])) * inv;
+                    z[vb][eb] = fmaf(xa, sa[p], xb * cb[p]) * inv;
+                }
+                if (on && h1 + i * R < last) {
+                    *reinterpret_cast<uint4*>(out + i * R * out_hs + da) = narrow_words<T>(z[0]);
+                    *reinterpret_cast<uint4*>(out + i * R * out_hs + db) = narrow_words<T>(z[1]);
+                }
+            }
+            out += kU * R * out_hs;
+        }
+    }
+}
+
 int sm_count() {
     static const int n = [] {  // one device per process
         int dev = 0, sms = 0;
@@ -273,11 +431,12 @@ int sm_count() {
     return n;
 }
 
-template <typename T, int G, int kNV, int kRot, int kU, bool kAligned>
-cudaError_t launch(const NormRopeArgs& a, cudaStream_t s) {
+using Kernel = void (*)(const NormRopeArgs, int, unsigned, unsigned, unsigned);
+
+// `round`: the rows that a warp has in flight
+cudaError_t launch(Kernel kernel, int round, const NormRopeArgs& a, cudaStream_t s) {
     // As many heads a warp as leave the device two rounds of its warps (the table's row and the weights are then read
     // once for them), in even shares: small calls still fill the device.
-    constexpr int round = kU * (32 / G);
     const long long warps = 2LL * 32 * sm_count();
     const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
     int shares = 1;
@@ -287,18 +446,31 @@ cudaError_t launch(const NormRopeArgs& a, cudaStream_t s) {
     const long long blocks = ((long long)a.T + kWarps - 1) / kWarps * units;
     if (blocks > 0xffffffffLL - (1LL << 30)) return cudaErrorInvalidValue;  // over 2^31 tokens x 2^16 heads
     const unsigned grid = (unsigned)(blocks < (1LL << 30) ? blocks : (1LL << 30));
-    return launch_pdl(norm_rope_kernel<T, G, kNV, kRot, kU, kAligned>, dim3(grid), 32 * kWarps, 0, s, a, heads, q_units, units,
-                      (unsigned)blocks);
+    return launch_pdl(kernel, dim3(grid), 32 * kWarps, 0, s, a, heads, q_units, units, (unsigned)blocks);
+}
+
+template <typename T, int G>
+cudaError_t launch_pairs(const NormRopeArgs& a, cudaStream_t s) {
+    constexpr int R = 32 / G;
+    const bool inter = a.layout == GEOCACHE_ROPE_INTERLEAVED;
+    const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
+    // two rows (four words) a lane where there are heads for them
+    if (a.rot == a.D && a.D == 2 * G * Elements<T>::kN) {
+        if (most > R)
+            return launch(inter ? norm_rope_pairs_kernel<T, G, true, true, 2> : norm_rope_pairs_kernel<T, G, false, true, 2>, 2 * R, a, s);
+        return launch(inter ? norm_rope_pairs_kernel<T, G, true, true, 1> : norm_rope_pairs_kernel<T, G, false, true, 1>, R, a, s);
+    }
+    return launch(inter ? norm_rope_pairs_kernel<T, G, true, false, 2> : norm_rope_pairs_kernel<T, G, false, false, 2>, 2 * R, a, s);
 }
 
 template <typename T, int G, int kNV, int kRot>
 cudaError_t launch_rows(const NormRopeArgs& a, bool aligned, cudaStream_t s) {
-    if (!aligned) return launch<T, G, kNV, kRot, 1, false>(a, s);
+    if (!aligned) return launch(norm_rope_kernel<T, G, kNV, kRot, 1, false>, 32 / G, a, s);
     constexpr int R = 32 / G;
     const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
     // four rows a lane where there are heads for them
-    if (most > R) return launch<T, G, kNV, kRot, 4, true>(a, s);
-    return launch<T, G, kNV, kRot, 1, true>(a, s);
+    if (most > R) return launch(norm_rope_kernel<T, G, kNV, kRot, 4, true>, 4 * R, a, s);
+    return launch(norm_rope_kernel<T, G, kNV, kRot, 1, true>, R, a, s);
 }
 
 template <typename T, int G, int kNV>
@@ -319,6 +491,13 @@ cudaError_t launch_type(const NormRopeArgs& a, cudaStream_t s) {
                   !((a.in_ts[i] | a.in_hs[i] | a.out_ts[i] | a.out_hs[i]) % V);
     }
     const int words = a.D / V;
+    const int step = a.layout == GEOCACHE_ROPE_INTERLEAVED ? V : 2 * V;
+    if (aligned && words % 2 == 0 && a.rot % step == 0) {
+        if (words <= 8) return launch_pairs<T, 4>(a, s);
+        if (words <= 16) return launch_pairs<T, 8>(a, s);
+        if (words <= 32) return launch_pairs<T, 16>(a, s);
+        return launch_pairs<T, 32>(a, s);
+    }
     if (words <= 4) return launch_rotation<T, 4, 1>(a, aligned, s);
     if (words <= 8) return launch_rotation<T, 8, 1>(a, aligned, s);
     if (words <= 16) return launch_rotation<T, 16, 1>(a, aligned, s);
