@@ -512,7 +512,8 @@ int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, cons
  *   plan            receives the sizes below.
  *   schedule        host buffer of schedule_bytes that receives the schedule,
  *                   which the caller copies to the device (16-byte aligned);
- *                   NULL: only `plan` is filled.
+ *                   NULL: only `plan` is filled.  Where it is smaller than
+ *                   plan->schedule_bytes, `plan` is filled and EINVAL returned.
  * Sizes: 0 <= n_seq, 1 <= Hk <= Hq <= 65536 with Hq % Hk == 0, D % 8 == 0,
  * 8 <= D <= 128, 0 <= n_ctas <= 65536.
  * Returns GEOCACHE_OK, EINVAL, ESHAPE (a size out of range, or more work than

@@ -6,11 +6,18 @@
 //   warp 10     loads queries (once a piece), keys and values (a ring of stages) by TMA;
 //   warps 8, 9  issue the products of tile 0 and of tile 1: S = Q K^T into tensor memory, O += P V with P read from there;
 //   warps 0-3   softmax of tile 0, one row a thread: S from tensor memory, the running maximum and sum in registers,
-//   warps 4-7   the same of tile 1;   P = exp2((S - m) scale log2 e) written over S as 16-bit pairs.
+//   warps 4-7   the same of tile 1;   P = exp2((S - m) scale log2 e) as 16-bit pairs in tensor memory.
 // O stays in tensor memory over the whole piece.  It is rescaled only when a row's weights of one tile of keys sum to more
 // than 2^15: until then the sums and P are kept relative to an older maximum, which changes no result beyond rounding,
-// and the maximum itself need not be taken in every tile.  S, the statistics and O are binary32; P is rounded to the inputs' type, as
-// the product with the values needs, while its sum is taken before that rounding.
+// and the maximum itself need not be taken in every tile.  S, the statistics and O are binary32; P is rounded to the
+// inputs' type, as the product with the values needs, while its sum is taken before that rounding.
+//
+// What bounds it.  Heads over 64: the tensor cores, and the power limit in long runs (8,192 tokens x 16 heads of 128:
+// 337 us, 1,630 TFLOP/s; 24,576: 3.0 ms in short bursts, 3.6 ms back to back, where the clock falls).  Heads up to 64: the
+// softmax warps (a tile of 128 x 128 takes one 820 cycles alone and two of a scheduler 1,490; the products take 1,050 for
+// both tiles): 8,192 tokens x 8 heads of 64 133 us, 1,030 TFLOP/s.  Few rows: HBM (317,000 keys of 4 heads of 128: 100 us,
+// 6.1 TB/s).  128 x 128 tiles, since a tile's S and O for two tiles fill the 512 columns of tensor memory; two tiles a
+// block, so that products and softmax overlap; one block an SM, with a ring of 5 (8) stages in what the queries leave.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -36,7 +43,7 @@ constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8 and 9 issue the products
 // (8 * 208 + 4 * 88 = 12 * 168).
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(8 * kSoftmaxRegs + 4 * kOtherRegs <= 12 * 168, "no more than the block was launched with");
-constexpr uint32_t kTmemColumns = 512;  // S of the two tiles at 0 and 128, O at 256 and 384
+constexpr uint32_t kTmemColumns = 512;
 constexpr uint32_t kBox = 128 * 128;    // bytes of 128 rows of 64 elements (one swizzled box)
 
 template <int DP>
@@ -52,7 +59,7 @@ struct Shape {  // heads padded to DP = 64 or 128 elements
     static constexpr uint32_t kBytes = (2 + kStages) * kTileBytes + 1024;  // and room to align to 1024
 };
 
-constexpr int kCached = 16;
+constexpr int kCached = 16;  // pieces that a block reads from shared memory
 
 struct Barriers {
     uint64_t q_full[2], q_empty[2], s_full[2], s_read[2], p_full[2], o_full[2], turn[2], drained;
@@ -343,7 +350,7 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
 // phase's parity tells it from the next one only, so neither warp may fall behind.
 //
 // With P apart from S (heads up to 64) the scores of the next keys are issued as soon as the softmax has read these, and
-// the goes need no order: no tile's softmax waits for the other's products (8,192 tokens x 8 heads of 64: 141 -> 105 us).
+// the goes need no order: no tile's softmax waits for the other's products (8,192 tokens x 8 heads of 64: 141 -> 133 us).
 template <int DP>
 __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers* b, const Items& items, int t, int lane) {
     using S = Shape<DP>;
@@ -701,7 +708,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
 }
 
-// Joins the parts of rows split along the keys, in their order: a warp takes a row, a lane four of its columns.
+// Joins the parts of rows split along the keys, in their order: a warp takes a row, a lane four of its columns.  Bound by
+// its launch and one round of loads (about 4 us behind the parts; launched while the attention drains).
 template <typename T>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ Params p) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -789,7 +797,7 @@ cudaError_t launch(const Params& p, const CUtensorMap& qm, const CUtensorMap& km
     if (ready != cudaSuccess) return ready;
     cudaError_t e = launch_pdl(kern, dim3((unsigned)p.a.n_ctas), kThreads, Shape<DP>::kBytes, s, p, qm, km, vm);
     if (e != cudaSuccess || p.a.n_joins == 0) return e;
-    // a block for every 8 rows of a tile while that leaves the device room for them at once
+    // a block for every 8 rows of a tile; with many tiles for 32
     const int rows = p.tok * p.a.pack, per = p.a.n_joins > 1024 ? 4 : 1;
     return launch_pdl(attention_join_kernel<T>, dim3((unsigned)p.a.n_joins, (unsigned)((rows + 8 * per - 1) / (8 * per))), 256, 0, s, p);
 }

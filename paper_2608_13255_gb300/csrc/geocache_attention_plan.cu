@@ -336,8 +336,8 @@ extern "C" int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_l
     try {
         geocache_attention_plan p{};
         const int st = plan({q_lens, k_lens, n_seq, Hq, Hk, D, causal != 0, n_ctas, 1}, &p, static_cast<char*>(schedule), schedule_bytes);
+        if (p.n_ctas) *out = p;  // the sizes are there when only the schedule did not fit
         if (st) return st;
-        *out = p;
     } catch (const std::exception&) {
         return geocache::set_error(GEOCACHE_ESHAPE, "%s: the work does not fit in host memory", fn);
     }

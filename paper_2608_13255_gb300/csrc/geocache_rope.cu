@@ -1,8 +1,10 @@
 // Norms of queries and keys with the rotation of their positions, and the table of the rotation.
 //
-// norm_rope_kernel reads each row (one head of one token) once and writes it once; the sum of squares
-// runs over the lanes that hold the row, so nothing else moves but one table row a token and the weights,
-// which the L1 serves to all heads.  It is bound by HBM.
+// Both kernels read each row (one head of one token) once and write it once; the sum of squares runs over the lanes that
+// hold the row, and beside the rows only one table row a token and the weights move, which the L1 serves to all heads.
+// 24,576 tokens x 32 heads of 128 take 73 us in bf16 (5.7 of 6.7 TB/s; the issue slots bound the rest) and 16 heads 63 us
+// in f32 (6.5 TB/s, HBM).  Rows that the first kernel does not take (an odd number of words, halves that end inside a word,
+// no alignment) run at 1.5 to 3.4 TB/s, bound by issue.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

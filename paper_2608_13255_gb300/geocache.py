@@ -633,10 +633,17 @@ def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
     qa, ka = (ctypes.c_int32 * max(1, len(q)))(*q), (ctypes.c_int32 * max(1, len(k)))(*k)
     info = AttentionPlanInfo()
     args = (qa, ka, len(q), int(Hq), int(Hk), int(D), 1 if causal else 0, int(n_ctas), ctypes.addressof(info))
-    _check(load().geocache_plan_attention(*args, None, 0))
-    room = torch.zeros(info.schedule_bytes // 4 + 4, dtype=torch.int32)
-    schedule = room[(-room.data_ptr() % 16) // 4:][:info.schedule_bytes // 4]
-    _check(load().geocache_plan_attention(*args, schedule.data_ptr(), info.schedule_bytes))
+    room = 1 << 18  # the schedules of most batches; dividing the work is most of a call's time
+    while True:
+        buffer = torch.empty(room // 4 + 4, dtype=torch.int32)
+        schedule = buffer[(-buffer.data_ptr() % 16) // 4:]
+        status = load().geocache_plan_attention(*args, schedule.data_ptr(), room)
+        if status == OK:
+            schedule = schedule[:info.schedule_bytes // 4]
+            break
+        if info.schedule_bytes <= room:
+            _check(status)
+        room = info.schedule_bytes
     return info, schedule
 
 

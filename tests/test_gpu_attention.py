@@ -177,6 +177,18 @@ def test_views_of_one_projection(gc):
     assert torch.equal(wide[:, :Hq], ref) and bool((wide[:, Hq] == 7.0).all())
 
 
+def test_broadcast_tensors(gc):
+    # one head's keys and values for all heads, one query for all tokens: strides of zero
+    T, H, D = 70, 3, 64
+    q, k, v = _inputs([T], [T], H, 1, D, torch.bfloat16)
+    wide_k, wide_v = k.expand(T, H, D), v.expand(T, H, D)
+    plan = gc.attention_plan([T], [T], H, H, D)
+    ref = gc.attention(plan, q, wide_k.contiguous(), wide_v.contiguous())
+    assert torch.equal(gc.attention(plan, q, wide_k, wide_v), ref)
+    one = q[:1].expand(T, H, D)
+    assert torch.equal(gc.attention(plan, one, wide_k, wide_v), gc.attention(plan, one.contiguous(), wide_k, wide_v))
+
+
 def test_same_bits_in_every_call_and_on_another_stream(gc):
     lq, lk = [17, 300], [5000, 2500]
     q, k, v = _inputs(lq, lk, 4, 2, 128, torch.bfloat16)
