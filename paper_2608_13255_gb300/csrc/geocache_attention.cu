@@ -12,11 +12,12 @@
 // and the maximum itself need not be taken in every tile.  S, the statistics and O are binary32; P is rounded to the
 // inputs' type, as the product with the values needs, while its sum is taken before that rounding.
 //
-// What bounds it.  Heads over 64: the tensor cores, and the power limit in long runs (8,192 tokens x 16 heads of 128:
-// 337 us, 1,630 TFLOP/s; 24,576: 3.0 ms in short bursts, 3.6 ms back to back, where the clock falls).  Heads up to 64: the
-// softmax warps (a tile of 128 x 128 takes one 820 cycles alone and two of a scheduler 1,490; the products take 1,050 for
-// both tiles): 8,192 tokens x 8 heads of 64 133 us, 1,030 TFLOP/s.  Few rows: HBM (317,000 keys of 4 heads of 128: 100 us,
-// 6.1 TB/s).  128 x 128 tiles, since a tile's S and O for two tiles fill the 512 columns of tensor memory; two tiles a
+// What bounds it.  Heads over 64: the tensor cores (24,576 tokens x 16 heads of 128: 2.69 ms, 1,840 TFLOP/s; 8,192: 319
+// us, 1,720).  Heads up to 64: the softmax warps (a tile of 128 x 128 takes one 820 cycles alone and two of a scheduler
+// 1,490; the products take 1,050 for both tiles) and their waits: 8,192 tokens x 8 heads of 64 133 us, 1,030 TFLOP/s.  Few
+// rows: HBM (317,000 keys of 4 heads of 128: 100 us, 6.1 TB/s).
+//
+// 128 x 128 tiles, since a tile's S and O for two tiles fill the 512 columns of tensor memory; two tiles a
 // block, so that products and softmax overlap; one block an SM, with a ring of 5 (8) stages in what the queries leave.
 #include <cuda.h>
 #include <cuda_bf16.h>

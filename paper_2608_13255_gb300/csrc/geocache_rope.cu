@@ -3,13 +3,14 @@
 // Both kernels read each row (one head of one token) once and write it once; the sum of squares runs over the lanes that
 // hold the row, and beside the rows only one table row a token and the weights move, which the L1 serves to all heads.
 // 24,576 tokens x 32 heads of 128 take 73 us in bf16 (5.7 of 6.7 TB/s; the issue slots bound the rest) and 16 heads 63 us
-// in f32 (6.5 TB/s, HBM).  Rows that the first kernel does not take (an odd number of words, halves that end inside a word,
-// no alignment) run at 1.5 to 3.4 TB/s, bound by issue.
+// in f32 (6.5 TB/s, HBM).  norm_rope_kernel takes the rows that norm_rope_pairs_kernel does not (halves that end inside
+// a word of 8 bytes, no alignment, a head of one word) and is bound by issue.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "geocache.h"
 #include "geocache_device.cuh"
@@ -92,6 +93,18 @@ __device__ __forceinline__ uint32_t narrow(float lo, float hi, __half) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+// 8 bytes of a 16-bit row
+template <typename T>
+__device__ __forceinline__ void widen(const uint2& w, float* x, T t) {
+    float y[8];
+    widen(make_uint4(w.x, w.y, 0, 0), y, t);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = y[i];
+}
+template <typename T>
+__device__ __forceinline__ void store_word(uint2* p, const float* x) {
+    if constexpr (sizeof(T) == 2) *p = make_uint2(narrow(x[0], x[1], T()), narrow(x[2], x[3], T()));
+}
 template <typename T>
 __device__ __forceinline__ uint4 narrow_words(const float* x) {
     if constexpr (sizeof(T) == 4)
@@ -99,6 +112,9 @@ __device__ __forceinline__ uint4 narrow_words(const float* x) {
     else
         return make_uint4(narrow(x[0], x[1], T()), narrow(x[2], x[3], T()), narrow(x[4], x[5], T()), narrow(x[6], x[7], T()));
 }
+
+template <typename T>
+__device__ __forceinline__ void store_word(uint4* p, const float* x) { *p = narrow_words<T>(x); }
 
 template <typename T, bool kAligned>
 __device__ __forceinline__ void store_words(T* p, const float* x) {
@@ -306,11 +322,14 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
 // three products and three sums an element in place of about ten operations of the general kernel, which is bound by
 // issue (24,576 tokens x 32 heads of 128 in bf16: 84 -> 73 us, 5.7 TB/s; halves of 64: 74 -> 51 us).
 // kFull: all lanes have words and the whole head is rotated (heads of 64, 128 and 256 in 16 bits), known to the compiler
-// (73 us; 79 without).
-template <typename T, int G, bool kInter, bool kFull, int kU>
+// (73 us; 79 without).  V: elements of a word; 16-bit rows that have an odd number of 16-byte words, or halves that are
+// not whole ones, take words of 8 bytes (24,576 tokens x 20 heads of 80, half rotated: 103 -> 53
+// us; 32 heads of 40: 95 -> 45 us).
+template <typename T, int V, int G, bool kInter, bool kFull, int kU>
 __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const __grid_constant__ NormRopeArgs a, int heads,
                                                                          unsigned q_units, unsigned units, unsigned n_blocks) {
-    constexpr int V = Elements<T>::kN, R = 32 / G;
+    using Word = std::conditional_t<V * sizeof(T) == 16, uint4, uint2>;
+    constexpr int R = 32 / G;
     const int D = kFull ? 2 * G * V : a.D, rot = kFull ? D : a.rot;
     const int lane_words = D / (2 * V), turned = kInter ? 0 : rot / (2 * V);  // lanes with words; with rotated halves
     const float inv_d = 1.0f / (float)D;
@@ -328,18 +347,18 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
         const long long in_hs = a.in_hs[side], out_hs = a.out_hs[side];
         const T* in = static_cast<const T*>(a.in[side]) + t * a.in_ts[side] + (first + r) * in_hs;
         T* out = static_cast<T*>(a.out[side]) + t * a.out_ts[side] + (first + r) * out_hs;
-        uint4 w[kU][2];
+        Word w[kU][2];
         auto load_round = [&](int h1) {
 #pragma unroll
             for (int i = 0; i < kU; ++i)
                 if (on && h1 + i * R < last) {
-                    w[i][0] = __ldcs(reinterpret_cast<const uint4*>(in + i * R * in_hs + da));
-                    w[i][1] = __ldcs(reinterpret_cast<const uint4*>(in + i * R * in_hs + db));
+                    w[i][0] = __ldcs(reinterpret_cast<const Word*>(in + i * R * in_hs + da));
+                    w[i][1] = __ldcs(reinterpret_cast<const Word*>(in + i * R * in_hs + db));
                 }
             in += kU * R * in_hs;
         };
 #pragma unroll
-        for (int i = 0; i < kU; ++i) w[i][0] = w[i][1] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kU; ++i) w[i][0] = w[i][1] = Word{};
         load_round(first + r);
 
         // pair i: elements (2 i, 2 i + 1) of the lane's words, or (i, i) of the first and the second
@@ -382,7 +401,7 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
 
 #pragma unroll 1
         for (int h1 = first + r; h1 - r < last; h1 += kU * R) {
-            uint4 now[kU][2];
+            Word now[kU][2];
 #pragma unroll
             for (int i = 0; i < kU; ++i) { now[i][0] = w[i][0]; now[i][1] = w[i][1]; }
             if (h1 - r + kU * R < last) load_round(h1 + kU * R);
@@ -414,8 +433,8 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
                     z[vb][eb] = fmaf(xa, sa[p], xb * cb[p]) * inv;
                 }
                 if (on && h1 + i * R < last) {
-                    *reinterpret_cast<uint4*>(out + i * R * out_hs + da) = narrow_words<T>(z[0]);
-                    *reinterpret_cast<uint4*>(out + i * R * out_hs + db) = narrow_words<T>(z[1]);
+                    store_word<T>(reinterpret_cast<Word*>(out + i * R * out_hs + da), z[0]);
+                    store_word<T>(reinterpret_cast<Word*>(out + i * R * out_hs + db), z[1]);
                 }
             }
             out += kU * R * out_hs;
@@ -451,18 +470,42 @@ cudaError_t launch(Kernel kernel, int round, const NormRopeArgs& a, cudaStream_t
     return launch_pdl(kernel, dim3(grid), 32 * kWarps, 0, s, a, heads, q_units, units, (unsigned)blocks);
 }
 
-template <typename T, int G>
+template <typename T, int V, int G>
 cudaError_t launch_pairs(const NormRopeArgs& a, cudaStream_t s) {
     constexpr int R = 32 / G;
     const bool inter = a.layout == GEOCACHE_ROPE_INTERLEAVED;
     const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
     // two rows (four words) a lane where there are heads for them
-    if (a.rot == a.D && a.D == 2 * G * Elements<T>::kN) {
-        if (most > R)
-            return launch(inter ? norm_rope_pairs_kernel<T, G, true, true, 2> : norm_rope_pairs_kernel<T, G, false, true, 2>, 2 * R, a, s);
-        return launch(inter ? norm_rope_pairs_kernel<T, G, true, true, 1> : norm_rope_pairs_kernel<T, G, false, true, 1>, R, a, s);
+    if constexpr (V == Elements<T>::kN) {
+        if (a.rot == a.D && a.D == 2 * G * V) {
+            if (most > R)
+                return launch(inter ? norm_rope_pairs_kernel<T, V, G, true, true, 2> : norm_rope_pairs_kernel<T, V, G, false, true, 2>,
+                              2 * R, a, s);
+            return launch(inter ? norm_rope_pairs_kernel<T, V, G, true, true, 1> : norm_rope_pairs_kernel<T, V, G, false, true, 1>, R,
+                          a, s);
+        }
     }
-    return launch(inter ? norm_rope_pairs_kernel<T, G, true, false, 2> : norm_rope_pairs_kernel<T, G, false, false, 2>, 2 * R, a, s);
+    return launch(inter ? norm_rope_pairs_kernel<T, V, G, true, false, 2> : norm_rope_pairs_kernel<T, V, G, false, false, 2>, 2 * R,
+                  a, s);
+}
+
+// Rows of whole pairs of V-element words, aligned to them; false where they are not.
+template <typename T, int V>
+bool try_pairs(const NormRopeArgs& a, cudaStream_t s, cudaError_t* e) {
+    const int step = a.layout == GEOCACHE_ROPE_INTERLEAVED ? V : 2 * V;
+    if (a.D % (2 * V) || a.rot % step) return false;
+    for (int i = 0; i < 2; ++i) {
+        if (!(i ? a.Hk : a.Hq)) continue;
+        if (((uintptr_t)a.in[i] | (uintptr_t)a.out[i]) % (V * sizeof(T)) ||
+            (a.in_ts[i] | a.in_hs[i] | a.out_ts[i] | a.out_hs[i]) % V)
+            return false;
+    }
+    const int lanes = a.D / (2 * V);
+    *e = lanes <= 4    ? launch_pairs<T, V, 4>(a, s)
+         : lanes <= 8  ? launch_pairs<T, V, 8>(a, s)
+         : lanes <= 16 ? launch_pairs<T, V, 16>(a, s)
+                       : launch_pairs<T, V, 32>(a, s);
+    return true;
 }
 
 template <typename T, int G, int kNV, int kRot>
@@ -493,12 +536,10 @@ cudaError_t launch_type(const NormRopeArgs& a, cudaStream_t s) {
                   !((a.in_ts[i] | a.in_hs[i] | a.out_ts[i] | a.out_hs[i]) % V);
     }
     const int words = a.D / V;
-    const int step = a.layout == GEOCACHE_ROPE_INTERLEAVED ? V : 2 * V;
-    if (aligned && words % 2 == 0 && a.rot % step == 0) {
-        if (words <= 8) return launch_pairs<T, 4>(a, s);
-        if (words <= 16) return launch_pairs<T, 8>(a, s);
-        if (words <= 32) return launch_pairs<T, 16>(a, s);
-        return launch_pairs<T, 32>(a, s);
+    cudaError_t e;
+    if (try_pairs<T, V>(a, s, &e)) return e;
+    if constexpr (sizeof(T) == 2) {
+        if (try_pairs<T, V / 2>(a, s, &e)) return e;
     }
     if (words <= 4) return launch_rotation<T, 4, 1>(a, aligned, s);
     if (words <= 8) return launch_rotation<T, 8, 1>(a, aligned, s);

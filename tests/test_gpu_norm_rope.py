@@ -96,7 +96,7 @@ def test_strides_alignment_and_in_place(gc, dtype, rot, layout):
     T, Hq, Hk, D = 45, 6, 2, 64
     _, _, table, slots, w = _inputs(gc, T, Hq, Hk, D, rot, dtype)
     buf = torch.randn((T * (Hq + 2 * Hk) * D + 8,), device="cuda").to(dtype)
-    for shift in (0, 1, 8):  # rows on and off 16 bytes
+    for shift in (0, 1, 4, 8):  # rows on and off 16 and 8 bytes
         qkv = buf[shift:shift + T * (Hq + 2 * Hk) * D].view(T, Hq + 2 * Hk, D).clone() if shift == 0 else \
             buf[shift:shift + T * (Hq + 2 * Hk) * D].view(T, Hq + 2 * Hk, D)
         before = qkv.clone()
