@@ -275,7 +275,8 @@ __device__ __forceinline__ void load_item(const Items& p, int i, AttentionItem& 
 }
 
 constexpr float kLargest = 32768.0f;  // of the weights of a row and tile: half of what f16 holds
-constexpr int kEarly = 1;  // products of a go that are issued after the turn has passed to the other tile
+constexpr int kEarly = 1;  // products of a go that are issued after the turn has passed to the other tile (of five at
+                           // least: turns are for heads over 64)
 
 // ---------------------------------------------------------------- roles --
 // Each role walks the block's pieces with its own count of the phases; a wait that gives up ends it.
@@ -373,7 +374,6 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                 mma_ss(tmem + t * 128, q + off, k + off, p.qk_idesc, s > 0);
                 if (hand_over && s + kEarly + 1 == p.k_steps) mbar_arrive(&b->turn[t ^ 1]);
             }
-        if (hand_over && p.k_steps <= kEarly) mbar_arrive(&b->turn[t ^ 1]);
         tc_commit(&b->s_full[t]);
     };
     for (int i = items.first; i < items.last; ++i) {

@@ -510,12 +510,15 @@ bool try_pairs(const NormRopeArgs& a, cudaStream_t s, cudaError_t* e) {
 
 template <typename T, int G, int kNV, int kRot>
 cudaError_t launch_rows(const NormRopeArgs& a, bool aligned, cudaStream_t s) {
-    if (!aligned) return launch(norm_rope_kernel<T, G, kNV, kRot, 1, false>, 32 / G, a, s);
     constexpr int R = 32 / G;
-    const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
-    // four rows a lane where there are heads for them
-    if (most > R) return launch(norm_rope_kernel<T, G, kNV, kRot, 4, true>, 4 * R, a, s);
-    return launch(norm_rope_kernel<T, G, kNV, kRot, 1, true>, R, a, s);
+    // (aligned rows without a rotation, or with halves of whole words, are norm_rope_pairs_kernel's)
+    if constexpr (kRot == kInterleaved || kRot == kHalfShared) {
+        const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
+        // four rows a lane where there are heads for them
+        if (aligned && most > R) return launch(norm_rope_kernel<T, G, kNV, kRot, 4, true>, 4 * R, a, s);
+        if (aligned) return launch(norm_rope_kernel<T, G, kNV, kRot, 1, true>, R, a, s);
+    }
+    return launch(norm_rope_kernel<T, G, kNV, kRot, 1, false>, R, a, s);
 }
 
 template <typename T, int G, int kNV>
