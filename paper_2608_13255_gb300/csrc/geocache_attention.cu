@@ -62,6 +62,10 @@ struct Shape {  // heads padded to DP = 64 or 128 elements
 
 constexpr int kCached = 16;  // pieces that a block reads from shared memory
 
+// What a block has in flight when it ends is waited for with this limit, however short the limit of the waits between
+// its roles has been set: a copy that lands after the block would write into the next one's shared memory.
+constexpr unsigned long long kDrainLimitNs = 2000000000ull;
+
 struct Barriers {
     uint64_t q_full[2], q_empty[2], s_full[2], s_read[2], p_full[2], o_full[2], turn[2], drained;
     uint64_t kv_full[8], kv_empty[8];
@@ -332,15 +336,15 @@ __device__ void load_role(const Params& p, const CUtensorMap* qm, const CUtensor
             if (!ok) break;
         }
     }
-    if (!*(volatile uint32_t*)&b->dead) return;
-    // given up: the copies in flight land before the block ends (their last phases, waited for with the same limit)
+    // The copies in flight land before the block ends: the last phase of every barrier is waited for.  On every path, since
+    // this warp is up to a ring ahead and cannot know that another will give up later.
     const unsigned long long t0 = globaltimer();
     for (int t = 0; t < 2; ++t)
-        while (q_n[t] && !mbar_try(&b->q_full[t], (q_n[t] & 1) ^ 1) && globaltimer() - t0 < limit) {}
+        while (q_n[t] && !mbar_try(&b->q_full[t], (q_n[t] & 1) ^ 1) && globaltimer() - t0 < kDrainLimitNs) {}
     for (uint32_t s = 0; s < S::kStages; ++s) {
         // stages below `stage` were last armed in this round, the others in the one before
         const uint32_t parity = s < stage ? phase : phase ^ 1;
-        while ((armed >> s & 1) && !mbar_try(&b->kv_full[s], parity) && globaltimer() - t0 < limit) {}
+        while ((armed >> s & 1) && !mbar_try(&b->kv_full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
     }
 }
 
@@ -698,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (elect()) tc_commit(&b->drained);
             const unsigned long long t0 = globaltimer();
-            while (!mbar_try(&b->drained, 0) && globaltimer() - t0 < p.a.wait_limit_ns) {}
+            while (!mbar_try(&b->drained, 0) && globaltimer() - t0 < kDrainLimitNs) {}
         }
         __syncwarp();
     }
