@@ -27,6 +27,7 @@
 #include <cstdint>
 
 #include "geocache.h"
+#include "geocache_attention_turns.h"
 #include "geocache_device.cuh"
 #include "geocache_internal.h"
 
@@ -362,6 +363,7 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
     using S = Shape<DP>;
     const unsigned long long limit = p.a.wait_limit_ns;
     uint32_t stage = 0, phase = 0, q_n = 0, p_n = 0, r_n = 0, turn_n = 0;
+    bool first = true;  // no piece of two tiles with keys so far
     // the next stage of the ring, once its copy has landed
     auto next_stage = [&](uint32_t& at) {
         at = stage;
@@ -422,11 +424,15 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                // tile 0's go j comes before tile 1's and after its go j - 1 (tile 0 has no more goes than tile 1)
-                if (!S::kApart && (t == 0 ? j > 0 && n_other > 0 : j < n_other))
+                // tile 0's go j comes before tile 1's and after its go j - 1
+                if (!S::kApart && turn_taken(t, j, n_other, first))
                     if (!mbar_wait(&b->turn[t], turn_n++ & 1, limit, b)) return;
+                const bool at_once = turn_given_at_once(t, j, n_other), turn_over = turn_given(t, j, n_other) && !at_once;
+                if (!S::kApart && at_once) {
+                    if (elect()) mbar_arrive(&b->turn[t ^ 1]);
+                    __syncwarp();
+                }
                 if (!mbar_wait(&b->p_full[t], p_n++ & 1, limit, b)) return;
-                const bool turn_over = t == 0 ? n_other > 0 : j + 1 < n_other;
                 tc_after();
                 if (elect()) {
                     const uint64_t v = smem_desc(v_at, kBox);
@@ -450,6 +456,7 @@ __device__ void mma_role(const Params& p, uint32_t smem, uint32_t tmem, Barriers
                 __syncwarp();
             }
         }
+        if (n > 0 && n_other > 0) first = false;
         if (S::kApart && n > 0 && !mbar_wait(&b->s_read[t], r_n++ & 1, limit, b)) return;  // of the last scores
         for (int x = 2 * n; x < 2 * n_other; ++x) {  // stages that the other tile alone reads
             uint32_t at = 0;
