@@ -27,26 +27,32 @@ def _inputs(lq, lk, H, D, seed=0):
     return r(sum(lq)), r(sum(lk)), r(sum(lk))
 
 
-def _gives_up(gc, call):
-    """`call` under a limit, the same call directly behind it under the default one; the outputs of the second"""
+def _under_a_limit(gc, call):
+    """`call` under a limit, the same call directly behind it under the default one: (outputs of both, whether a wait
+    ran out)"""
     try:
-        call()
+        first = call()
         gc.debug_set_wait(0, drop_first_copy=False)
-        got = call()  # queued behind, before anything is waited for
+        second = call()  # queued behind, before anything is waited for
         torch.cuda.synchronize()
-        with pytest.raises(gc.GeocacheError) as e:
+        late = False
+        try:
             gc.device_status()
-        assert e.value.status == gc.ETIMEOUT
+        except gc.GeocacheError as e:
+            assert e.status == gc.ETIMEOUT
+            late = True
     finally:
         gc.debug_set_wait(0, drop_first_copy=False)
     gc.device_status()
-    return got
+    return first, second, late
 
 
 @pytest.mark.parametrize("D", [64, 80, 128])
 @pytest.mark.parametrize("n_ctas", [1, 152])
 def test_limit_shorter_than_a_copy(gc, D, n_ctas):
-    # 1 ns: every block gives up at its first wait, with a ring of copies on its way
+    # 1 ns: a block gives up at its first wait that does not end by itself, with a ring of copies on its way.  (One try of
+    # a wait lets the thread sleep for as long as the hardware likes, so a block of few copies may get through; the long
+    # chain of a single block does not.)
     lq, lk = [300, 1, 512], [2000, 700, 512]
     q, k, v = _inputs(lq, lk, 2, D)
     plan = gc.attention_plan(lq, lk, 2, 2, D, n_ctas=n_ctas)
@@ -54,8 +60,9 @@ def test_limit_shorter_than_a_copy(gc, D, n_ctas):
     gc.device_status()
     for _ in range(5):
         gc.debug_set_wait(1, drop_first_copy=False)
-        got = _gives_up(gc, lambda: gc.attention(plan, q, k, v))
-        assert torch.equal(got, ref)
+        first, second, late = _under_a_limit(gc, lambda: gc.attention(plan, q, k, v))
+        assert late or (n_ctas > 1 and torch.equal(first, ref))
+        assert torch.equal(second, ref)
 
 
 @pytest.mark.parametrize("D", [64, 80, 128])
@@ -69,5 +76,5 @@ def test_first_copy_left_out(gc, D, n_tiles):
     ref = gc.attention(plan, q, k, v).clone()
     gc.device_status()
     gc.debug_set_wait(200_000, drop_first_copy=True)
-    got = _gives_up(gc, lambda: gc.attention(plan, q, k, v))
-    assert torch.equal(got, ref)
+    _, second, late = _under_a_limit(gc, lambda: gc.attention(plan, q, k, v))
+    assert late and torch.equal(second, ref)
