@@ -547,7 +547,8 @@ int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_lens, int n_
  *              need one each.
  * out must not overlap an input.  A NaN or infinity reaches the rows of its own
  * sequence only: a key's through its scores, a value's also those rows of its
- * sequence whose tile of queries sees the tile of 128 keys it lies in.
+ * sequence that see a key and whose tile of queries sees the tile of 128 keys
+ * it lies in.
  * Returns GEOCACHE_OK, EINVAL, ESHAPE, EDTYPE, EALIAS, ECUDA; a wait inside the
  * kernel that ran out sets the device status word (ETIMEOUT).
  * ------------------------------------------------------------------------ */

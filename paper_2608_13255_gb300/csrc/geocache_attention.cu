@@ -609,10 +609,10 @@ __device__ void softmax_role(const Params& p, uint32_t tmem, Barriers* b, const 
 #pragma unroll 1
         for (int x = 0; x < p.a.D; x += 32) {
             uint32_t o[32];
-            if (n) {
-                tmem_ld32(o_at + x, o);
-                tmem_wait_ld(o);
-            } else {
+            tmem_ld32(o_at + x, o);  // (of a tile without keys what a piece before left)
+            tmem_wait_ld(o);
+            // a row without weights is zero, also where its neighbours' values are not finite (0 * NaN in the product)
+            if (inv == 0.0f) {
 #pragma unroll
                 for (int y = 0; y < 32; ++y) o[y] = 0;
             }
