@@ -315,6 +315,28 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_con
     }
 }
 
+// The rows of a token whose slot is outside the table: the norm alone, a warp a row.  Out of line and taken before the
+// rows are loaded, for the kernel below is bound by issue and registers where every element is rotated (24,576 tokens x 32
+// heads of 128 in bf16, interleaved and halves: 68 and 74 us; 73 and 76 with a flag beside the coefficients).
+template <typename T>
+__device__ __noinline__ void norm_rows(const NormRopeArgs& a, int side, long long t, int first, int last) {
+    const int lane = threadIdx.x & 31;
+    const float* weight = a.norm ? a.weight[side] : nullptr;
+    for (int h = first; h < last; ++h) {
+        const T* in = static_cast<const T*>(a.in[side]) + t * a.in_ts[side] + h * a.in_hs[side];
+        T* out = static_cast<T*>(a.out[side]) + t * a.out_ts[side] + h * a.out_hs[side];
+        float inv = 1.0f;
+        if (a.norm) {
+            float sum = 0.0f;
+            for (int d = lane; d < a.D; d += 32) sum = fmaf((float)in[d], (float)in[d], sum);
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            inv = rsqrtf(fmaf(sum, 1.0f / (float)a.D, a.eps));
+        }
+        for (int d = lane; d < a.D; d += 32) out[d] = from_float<T>((float)in[d] * (weight ? weight[d] : 1.0f) * inv);
+    }
+}
+
 // The common rows: an even number of words, two a lane, and a rotation that whole words take part in.  Rotated halves lie
 // in one lane as interleaved pairs do (lane l: word l of each half; the unrotated words two by two behind them), and
 // nothing but the sum of squares crosses lanes.  With the weights folded into the rotation a pair (a, b) becomes
@@ -345,6 +367,13 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
         const int side = c >= q_units, H = side ? a.Hk : a.Hq;
         const int first = (int)(side ? c - q_units : c) * heads, last = min(H, first + heads);
         const long long in_hs = a.in_hs[side], out_hs = a.out_hs[side];
+        const int slot = rot == 0 ? 0 : a.slots ? a.slots[t] : (int)t;
+        const bool lost = rot && (slot < 0 || slot >= (int)a.n_slots);
+        if (lost && lane == 0) atomicOr(&g_rope_error, 32u);
+        if (kFull && __builtin_expect(lost, 0)) {
+            norm_rows<T>(a, side, t, first, last);
+            continue;
+        }
         const T* in = static_cast<const T*>(a.in[side]) + t * a.in_ts[side] + (first + r) * in_hs;
         T* out = static_cast<T*>(a.out[side]) + t * a.out_ts[side] + (first + r) * out_hs;
         Word w[kU][2];
@@ -363,20 +392,22 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
 
         // pair i: elements (2 i, 2 i + 1) of the lane's words, or (i, i) of the first and the second
         float ca[V], sa[V], cb[V], sb[V];
+        // which of the lane's words are rotated (halves: both or neither); the others meet no partner, since that need not
+        // be finite
+        bool turn[2] = {kFull, kFull};
         {
             float cs[2 * V];
 #pragma unroll
             for (int i = 0; i < V; ++i) { cs[2 * i] = 1.0f; cs[2 * i + 1] = 0.0f; }
-            const long long slot = rot == 0 ? 0 : a.slots ? a.slots[t] : t;
-            if (rot && (slot < 0 || slot >= a.n_slots)) {
-                if (lane == 0) atomicOr(&g_rope_error, 32u);
-            } else if (rot && on) {
-                const float* tab = reinterpret_cast<const float*>(a.table + slot * (rot / 2));
+            if (rot && !lost && on) {
+                turn[0] = kFull || (kInter ? da < rot : l < turned);
+                turn[1] = kFull || (kInter && db < rot);
+                const float* tab = reinterpret_cast<const float*>(a.table + (long long)slot * (rot / 2));
                 const bool wide = !((uintptr_t)tab & 15);
                 if (kInter) {
-                    if (da < rot) load_floats<V>(tab + da, wide, cs);
-                    if (db < rot) load_floats<V>(tab + db, wide, cs + V);
-                } else if (l < turned) {
+                    if (turn[0]) load_floats<V>(tab + da, wide, cs);
+                    if (turn[1]) load_floats<V>(tab + db, wide, cs + V);
+                } else if (turn[0]) {
                     load_floats<2 * V>(tab + 2 * da, wide, cs);
                 }
             }
@@ -429,8 +460,13 @@ __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const _
                     const int va = kInter ? p / (V / 2) : 0, ea = kInter ? 2 * p % V : p;
                     const int vb = kInter ? va : 1, eb = kInter ? ea + 1 : p;
                     const float xa = x[va][ea], xb = x[vb][eb];
-                    z[va][ea] = fmaf(xa, ca[p], -(xb * sb[p])) * inv;
-                    z[vb][eb] = fmaf(xa, sa[p], xb * cb[p]) * inv;
+                    if (turn[va]) {
+                        z[va][ea] = fmaf(xa, ca[p], -(xb * sb[p])) * inv;
+                        z[vb][eb] = fmaf(xa, sa[p], xb * cb[p]) * inv;
+                    } else {
+                        z[va][ea] = xa * ca[p] * inv;
+                        z[vb][eb] = xb * cb[p] * inv;
+                    }
                 }
                 if (on && h1 + i * R < last) {
                     store_word<T>(reinterpret_cast<Word*>(out + i * R * out_hs + da), z[0]);
