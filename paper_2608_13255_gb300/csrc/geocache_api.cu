@@ -240,13 +240,9 @@ int geocache_last_launches(void) { return g_launches; }
 int geocache_abi_version(void) { return GEOCACHE_ABI_VERSION; }
 
 int geocache_device_status(void* stream) {
-    unsigned int word = 0, raster_word = 0, rope_word = 0, attention_word = 0;
+    unsigned int word = 0;
     cudaError_t e = geocache::read_device_error(&word, true, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = geocache::read_raster_error(&raster_word, true, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = geocache::read_rope_error(&rope_word, true, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = geocache::read_attention_error(&attention_word, true, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "reading the device status word");
-    word |= raster_word | rope_word | attention_word;
     if (word & 2u)
         return fail(GEOCACHE_ESHAPE, "a sparse-form build had more records than max_records (status word 0x%x); "
                                      "query geocache_corr_record_count and rebuild", word);

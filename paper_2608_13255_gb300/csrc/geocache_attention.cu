@@ -35,7 +35,7 @@ namespace geocache {
 
 namespace {
 
-// Status word of this file's kernels (bit 1: a wait ran out); read by geocache_device_status.
+// Status word of this file's kernels (bit 0: a wait ran out); read by geocache_device_status.
 __device__ unsigned int g_attention_error = 0;
 
 constexpr int kRows = kAttentionRows, kKeys = kAttentionKeys;
@@ -844,15 +844,6 @@ cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s) {
     return a.D > 64 ? launch<128, __half>(p, qm, km, vm, s) : launch<64, __half>(p, qm, km, vm, s);
 }
 
-cudaError_t read_attention_error(unsigned int* out, bool clear, cudaStream_t s) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(out, g_attention_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
-    if (e != cudaSuccess) return e;
-    e = cudaStreamSynchronize(s);
-    if (e != cudaSuccess || !clear || *out == 0) return e;
-    static const unsigned int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_attention_error, &zero, sizeof(unsigned int), 0, cudaMemcpyHostToDevice, s);
-    if (e != cudaSuccess) return e;
-    return cudaStreamSynchronize(s);
-}
+cudaError_t attention_error_word(unsigned int** word) { return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_attention_error); }
 
 }  // namespace geocache

@@ -87,10 +87,13 @@ cudaError_t launch_copy_anchor_rows(const TransportArgs& t, cudaStream_t s);
 cudaError_t launch_reconstruct(const void* x_t, const float* x0, void* x_next, int lat_dtype, int64_t n,
                                const ReconCoef& coef, float* pred_out, float* x0_store, cudaStream_t s);
 
+// Reads the status words of all sources (one copy and one wait), and clears them with `clear`.
 cudaError_t read_device_error(unsigned int* out, bool clear, cudaStream_t s);
+cudaError_t raster_error_word(unsigned int** word);     // their device addresses
+cudaError_t rope_error_word(unsigned int** word);
+cudaError_t attention_error_word(unsigned int** word);
 // test hook of the bounded waits (geocache_debug_set_wait)
 void set_debug_wait(unsigned long long limit_ns, int drop_first_copy);
-cudaError_t read_raster_error(unsigned int* out, bool clear, cudaStream_t s);
 // position maps at the token grid H x W; ss > 1: rendered at ss x H by
 // ss x W (zbuf holds B*N*H*W*ss*ss words) and pooled to the token grid
 cudaError_t launch_raster(const float* V, long long nv, const int32_t* F, long long nf, const int64_t* face_off,
@@ -123,7 +126,6 @@ struct NormRopeArgs {
     int dtype;
 };
 cudaError_t launch_norm_rope(const NormRopeArgs& a, cudaStream_t s);
-cudaError_t read_rope_error(unsigned int* out, bool clear, cudaStream_t s);
 
 // One piece of an attention launch: up to two tiles of 128 query rows (tile t's tokens start at q_row + t *
 // (128 / pack); a row is one of `pack` heads of a token) of one sequence and key/value head, over a range of its
@@ -169,7 +171,6 @@ struct AttentionArgs {
     int drop_first_copy;
 };
 cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s);
-cudaError_t read_attention_error(unsigned int* out, bool clear, cudaStream_t s);
 // the limit of bounded waits, and the test hook's pending request (consumed)
 unsigned long long debug_wait_limit_ns();
 int take_drop_first_copy();

@@ -681,7 +681,8 @@ cudaError_t launch_build_corr(const geocache_corr& c, cudaStream_t s) {
 // Device status word (the library's only device-resident state): bit 0 = a
 // bounded wait gave up, bit 1 = the sparse form did not fit max_records,
 // bit 2 = a record permutation entry was out of range, bit 4 = a table index
-// was outside [-1, H*W) (bit 3 is the rasteriser's word's bad face index).
+// was outside [-1, H*W).  The other sources have words of their own (bit 3: a
+// bad face index, bit 5: a rotary slot, bit 0 of the attention: a wait).
 // Read and cleared by geocache_device_status().
 __device__ unsigned int g_device_error = 0;
 
@@ -3009,8 +3010,23 @@ cudaError_t launch_reconstruct(const void* x_t, const float* x0, void* x_next, i
     return launch_reconstruct_t<float>(x_t, x0, x_next, n, coef, pred_out, x0_store, s);
 }
 
+// Moves the words of the other sources into this one's, which is then all that the host has to wait for (38 us with a
+// copy for each source).
+__global__ void gather_errors_kernel(unsigned int* raster, unsigned int* rope, unsigned int* attention) {
+    const unsigned int word = atomicExch(raster, 0u) | atomicExch(rope, 0u) | atomicExch(attention, 0u);
+    if (word) atomicOr(&g_device_error, word);
+}
+
 cudaError_t read_device_error(unsigned int* out, bool clear, cudaStream_t s) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(out, g_device_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
+    unsigned int *raster, *rope, *attention;
+    cudaError_t e = raster_error_word(&raster);
+    if (e == cudaSuccess) e = rope_error_word(&rope);
+    if (e == cudaSuccess) e = attention_error_word(&attention);
+    if (e != cudaSuccess) return e;
+    gather_errors_kernel<<<1, 1, 0, s>>>(raster, rope, attention);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    e = cudaMemcpyFromSymbolAsync(out, g_device_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
     if (e != cudaSuccess) return e;
     e = cudaStreamSynchronize(s);
     if (e != cudaSuccess || !clear || *out == 0) return e;

@@ -584,16 +584,7 @@ __global__ void __launch_bounds__(kRasterThreads) pool_posmaps_kernel(const floa
 
 }  // namespace
 
-cudaError_t read_raster_error(unsigned int* out, bool clear, cudaStream_t s) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(out, g_raster_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
-    if (e != cudaSuccess) return e;
-    e = cudaStreamSynchronize(s);
-    if (e != cudaSuccess || !clear || *out == 0) return e;
-    static const unsigned int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_raster_error, &zero, sizeof(unsigned int), 0, cudaMemcpyHostToDevice, s);
-    if (e != cudaSuccess) return e;
-    return cudaStreamSynchronize(s);
-}
+cudaError_t raster_error_word(unsigned int** word) { return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_raster_error); }
 
 static int sm_count() {
     int dev = 0, sms = 0;

@@ -20,7 +20,7 @@ namespace geocache {
 
 namespace {
 
-// Status word of this file's kernels (bit 32: a slot outside the table); read by geocache_device_status.
+// Status word of this file's kernels (bit 5: a slot outside the table); read by geocache_device_status.
 __device__ unsigned int g_rope_error = 0;
 
 // One thread per (slot, pair); double throughout, since an angle of 10^5 turns keeps 2^-53 * 10^6 of itself.
@@ -606,15 +606,6 @@ cudaError_t launch_norm_rope(const NormRopeArgs& a, cudaStream_t s) {
     return launch_type<float>(a, s);
 }
 
-cudaError_t read_rope_error(unsigned int* out, bool clear, cudaStream_t s) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(out, g_rope_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);
-    if (e != cudaSuccess) return e;
-    e = cudaStreamSynchronize(s);
-    if (e != cudaSuccess || !clear || *out == 0) return e;
-    static const unsigned int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_rope_error, &zero, sizeof(unsigned int), 0, cudaMemcpyHostToDevice, s);
-    if (e != cudaSuccess) return e;
-    return cudaStreamSynchronize(s);
-}
+cudaError_t rope_error_word(unsigned int** word) { return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_rope_error); }
 
 }  // namespace geocache
