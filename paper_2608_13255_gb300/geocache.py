@@ -186,6 +186,18 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
+def _empty(shape, dtype, device, stream):
+    """An output of a call on `stream`, allocated there: a block that the
+    current stream has given back may still have work ahead of it on that one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream)
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dev(t, dtype, numel=None, name="tensor"):
     if t is None:
         return None
@@ -532,7 +544,8 @@ def rope_table(n_slots=None, rot=None, theta=10000.0, pos=None, scaling=None, ma
     [n_slots]).  scaling: None, or {"kind": "linear" | "base", "factor": f}, or
     {"kind": "by_parts", "factor": f, "original": trained context, "low": 1,
     "high": 32}.  With `table` (device f32 [n_slots, row_pairs, 2]) the pairs
-    [first_pair, first_pair + rot / 2) of its rows are written."""
+    [first_pair, first_pair + rot / 2) of its rows are written; without, one is
+    allocated on the call's stream."""
     spec = dict(scaling or {})
     kind = _ROPE_SCALINGS[spec.pop("kind", "plain")]
     r = Rope(int(rot), float(theta), kind, float(spec.pop("factor", 1.0)), float(spec.pop("original", 0.0)),
@@ -543,7 +556,7 @@ def rope_table(n_slots=None, rot=None, theta=10000.0, pos=None, scaling=None, ma
         n_slots = table.shape[0] if pos is None else pos.numel()
     n = int(n_slots)
     if table is None:
-        table = torch.empty((n, int(rot) // 2, 2), dtype=torch.float32, device="cuda" if pos is None else pos.device)
+        table = _empty((n, int(rot) // 2, 2), torch.float32, "cuda" if pos is None else pos.device, stream)
     elif table.dim() != 3 or table.shape[0] != n or table.shape[2] != 2:
         raise ValueError("table must be [n_slots, row_pairs, 2]")
     _check(load().geocache_rope_table(ctypes.byref(r), _dev(pos, torch.int32, n, "pos"), n,
@@ -584,22 +597,22 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
     """geocache_qk_norm_rope: each head of q [T, Hq, D] and k [T, Hk, D] (f32,
     bf16 or f16; any strides between tokens and heads) normalised and rotated by
     table [n_slots, rot / 2, 2] at the tokens' slots (device int32 [T]; None:
-    token t has slot t).  k may be None.  Outputs are allocated when None and
-    may be the inputs themselves.  Returns (q_out, k_out)."""
+    token t has slot t).  k may be None.  Outputs are allocated when None (on
+    the call's stream) and may be the inputs themselves.  Returns (q_out, k_out)."""
     T, Hq, D = q.shape
     dt = q.dtype
     if dt not in _HEAD_DTYPES:
         raise TypeError("q must be float32, bfloat16 or float16 (got %s)" % dt)
     Hk = 0 if k is None else k.shape[1]
     if q_out is None:
-        q_out = torch.empty((T, Hq, D), dtype=dt, device=q.device)
+        q_out = _empty((T, Hq, D), dt, q.device, stream)
     hk = hko = (0, 0, 0)
     if k is None:
         if k_out is not None:
             raise ValueError("k_out without k")
     else:
         if k_out is None:
-            k_out = torch.empty((T, Hk, D), dtype=dt, device=q.device)
+            k_out = _empty((T, Hk, D), dt, q.device, stream)
         hk, hko = _heads(k, dt, T, Hk, D, "k"), _heads(k_out, dt, T, Hk, D, "k_out")
     heads, at = _four_heads(_heads(q, dt, T, Hq, D, "q"), hk, _heads(q_out, dt, T, Hq, D, "q_out"), hko)
     n_slots = rot = 0
@@ -670,13 +683,13 @@ def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, work
     strides that are multiples of 8 elements) with the rows of the plan's
     sequences one after the other.  lse: device f32 [Tq, Hq] that receives the
     logarithms of the softmax sums, or None.  scale: None = 1/sqrt(D).
-    Returns out (allocated when None)."""
+    Returns out (allocated on the call's stream when None)."""
     f = plan.info
     dt = q.dtype
     if dt is not torch.bfloat16 and dt is not torch.float16:
         raise TypeError("q must be bfloat16 or float16 (got %s)" % dt)
     if out is None:
-        out = torch.empty((f.q_tokens, f.Hq, f.D), dtype=dt, device=q.device)
+        out = _empty((f.q_tokens, f.Hq, f.D), dt, q.device, stream)
     ws = plan.workspace if workspace is None else workspace
     Tq, Tk, Hq, Hk, D = plan.sizes
     heads, at = _four_heads(_heads(q, dt, Tq, Hq, D, "q"), _heads(k, dt, Tk, Hk, D, "k"), _heads(v, dt, Tk, Hk, D, "v"),
