@@ -186,6 +186,15 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
+def _size(x, name):
+    """A size for a 32-bit field of the C interface: ctypes would cut a fraction
+    off and wrap what is too large."""
+    n = int(x)
+    if n != x or not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError("%s=%s must be a 32-bit integer" % (name, x))
+    return n
+
+
 def _empty(shape, dtype, device, stream):
     """An output of a call on `stream`, allocated there: a block that the
     current stream has given back may still have work ahead of it on that one."""
@@ -548,19 +557,20 @@ def rope_table(n_slots=None, rot=None, theta=10000.0, pos=None, scaling=None, ma
     allocated on the call's stream."""
     spec = dict(scaling or {})
     kind = _ROPE_SCALINGS[spec.pop("kind", "plain")]
-    r = Rope(int(rot), float(theta), kind, float(spec.pop("factor", 1.0)), float(spec.pop("original", 0.0)),
+    rot, first_pair = _size(rot, "rot"), _size(first_pair, "first_pair")
+    r = Rope(rot, float(theta), kind, float(spec.pop("factor", 1.0)), float(spec.pop("original", 0.0)),
              float(spec.pop("low", 1.0)), float(spec.pop("high", 32.0)), float(magnitude))
     if spec:
         raise ValueError("unknown scaling parameters: %s" % ", ".join(sorted(spec)))
     if n_slots is None:
         n_slots = table.shape[0] if pos is None else pos.numel()
-    n = int(n_slots)
+    n = _size(n_slots, "n_slots")
     if table is None:
-        table = _empty((n, int(rot) // 2, 2), torch.float32, "cuda" if pos is None else pos.device, stream)
+        table = _empty((n, rot // 2, 2), torch.float32, "cuda" if pos is None else pos.device, stream)
     elif table.dim() != 3 or table.shape[0] != n or table.shape[2] != 2:
         raise ValueError("table must be [n_slots, row_pairs, 2]")
     _check(load().geocache_rope_table(ctypes.byref(r), _dev(pos, torch.int32, n, "pos"), n,
-                                      _dev(table, torch.float32, None, "table"), table.shape[1], int(first_pair),
+                                      _dev(table, torch.float32, None, "table"), table.shape[1], first_pair,
                                       _stream(stream)))
     return table
 
@@ -651,7 +661,8 @@ def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
         raise ValueError("a sequence's length is outside [0, 2^31)")
     qa, ka = (ctypes.c_int32 * max(1, len(q)))(*q), (ctypes.c_int32 * max(1, len(k)))(*k)
     info = AttentionPlanInfo()
-    args = (qa, ka, len(q), int(Hq), int(Hk), int(D), 1 if causal else 0, int(n_ctas), ctypes.addressof(info))
+    args = (qa, ka, len(q), _size(Hq, "Hq"), _size(Hk, "Hk"), _size(D, "D"), 1 if causal else 0,
+            _size(n_ctas, "n_ctas"), ctypes.addressof(info))
     room = 1 << 18  # the schedules of most batches; dividing the work is most of a call's time
     while True:
         buffer = torch.empty(room // 4 + 4, dtype=torch.int32)
