@@ -127,6 +127,7 @@ __device__ __forceinline__ void store_words(T* p, const float* x) {
 }
 
 constexpr int kWarps = 8;
+constexpr int kLargestHead = 256;  // elements
 
 // n consecutive floats, in 16-byte words where `wide`
 template <int kN>
@@ -508,6 +509,7 @@ cudaError_t launch(Kernel kernel, int round, const NormRopeArgs& a, cudaStream_t
 
 template <typename T, int V, int G>
 cudaError_t launch_pairs(const NormRopeArgs& a, cudaStream_t s) {
+    static_assert(G == 4 || G * V < kLargestHead, "rows that fill no more than half of the lanes take fewer");
     constexpr int R = 32 / G;
     const bool inter = a.layout == GEOCACHE_ROPE_INTERLEAVED;
     const int most = a.Hq > a.Hk ? a.Hq : a.Hk;
@@ -537,10 +539,14 @@ bool try_pairs(const NormRopeArgs& a, cudaStream_t s, cudaError_t* e) {
             return false;
     }
     const int lanes = a.D / (2 * V);
-    *e = lanes <= 4    ? launch_pairs<T, V, 4>(a, s)
-         : lanes <= 8  ? launch_pairs<T, V, 8>(a, s)
-         : lanes <= 16 ? launch_pairs<T, V, 16>(a, s)
-                       : launch_pairs<T, V, 32>(a, s);
+    if (lanes <= 4)
+        *e = launch_pairs<T, V, 4>(a, s);
+    else if (lanes <= 8)
+        *e = launch_pairs<T, V, 8>(a, s);
+    else if (V * 32 >= kLargestHead || lanes <= 16)
+        *e = launch_pairs<T, V, 16>(a, s);
+    else if constexpr (V * 32 < kLargestHead)
+        *e = launch_pairs<T, V, 32>(a, s);
     return true;
 }
 
