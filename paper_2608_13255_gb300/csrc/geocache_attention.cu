@@ -727,7 +727,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_wait();
     const AttentionJoin join = p.a.joins[blockIdx.x];
-    for (int row = blockIdx.y * 8 + warp; row < join.n_tok * p.a.pack; row += gridDim.y * 8) {
+    const int row = blockIdx.y * 8 + warp;
+    if (row < join.n_tok * p.a.pack) {
         const int tok = row / p.a.pack, head = join.head + row - tok * p.a.pack;
         const float* lse = p.a.part_lse + (long long)join.slot * kRows + row;
         float top = -INFINITY;
@@ -809,9 +810,9 @@ cudaError_t launch(const Params& p, const CUtensorMap& qm, const CUtensorMap& km
     if (ready != cudaSuccess) return ready;
     cudaError_t e = launch_pdl(kern, dim3((unsigned)p.a.n_ctas), kThreads, Shape<DP>::kBytes, s, p, qm, km, vm);
     if (e != cudaSuccess || p.a.n_joins == 0) return e;
-    // a block for every 8 rows of a tile; with many tiles for 32
-    const int rows = p.tok * p.a.pack, per = p.a.n_joins > 1024 ? 4 : 1;
-    return launch_pdl(attention_join_kernel<T>, dim3((unsigned)p.a.n_joins, (unsigned)((rows + 8 * per - 1) / (8 * per))), 256, 0, s, p);
+    // a block for every 8 rows of a tile
+    const int rows = p.tok * p.a.pack;
+    return launch_pdl(attention_join_kernel<T>, dim3((unsigned)p.a.n_joins, (unsigned)((rows + 7) / 8)), 256, 0, s, p);
 }
 
 }  // namespace
