@@ -651,6 +651,9 @@ int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, cons
         int st = check_heads(in[i], T, H[i], D, eb, false, fn, name[i]);
         if (!st) st = check_heads(out[i], T, H[i], D, eb, true, fn, i ? "k_out" : "q_out");
         if (st) return st;
+    }
+    for (int i = 0; i < 2; ++i) {  // (each is compared with the other's, so all are there by now)
+        if (T == 0 || H[i] == 0) continue;
         a.in[i] = in[i]->data; a.in_ts[i] = in[i]->token_stride; a.in_hs[i] = in[i]->head_stride;
         a.out[i] = out[i]->data; a.out_ts[i] = out[i]->token_stride; a.out_hs[i] = out[i]->head_stride;
         const size_t tb = rot ? (size_t)n_slots * rot * 4 : 0;
