@@ -8,9 +8,11 @@
  * - Pointers marked "device" are CUDA device addresses on the current device
  *   (e.g. torch tensors' data_ptr()); pointers marked "host" are ordinary host
  *   memory.  The caller owns every buffer and the library allocates no
- *   memory; its device-resident state is a 4-byte status word that kernels
+ *   memory; its device-resident state is a few 4-byte status words that kernels
  *   set on a failure they can only detect on the GPU (geocache_device_status)
  *   and the fixed scratch array of geocache_transport_step_noalloc.
+ * - A process uses the library on one device: launch settings that depend on
+ *   the device are read or made once.
  * - Every device-side entry point is asynchronous on `stream` (a cudaStream_t,
  *   NULL = the legacy default stream) and returns after enqueueing its kernels.
  * - Latents are NCHW per view with the views on the batch axis:
@@ -419,7 +421,7 @@ int geocache_unpack_anchors(const void* src, void* dst, int64_t row_bytes, int B
  * anchor forward": the denoiser runs on the packed anchor rows, which keep
  * their structural indices and rotary slots).  The paper gives no kernels for
  * it; the operators are the standard ones that a transformer denoiser puts
- * between its projections.
+ * between its projections.  They are forward only, as the method is.
  * ------------------------------------------------------------------------ */
 
 /* Heads of a [tokens, heads, D] tensor: element (t, h, d) is at
@@ -506,7 +508,9 @@ int geocache_qk_norm_rope(const geocache_heads* q, const geocache_heads* k, cons
  * A query that sees no key has out = 0 and lse = -inf.
  *
  * geocache_plan_attention -- how a launch divides the work; made once for the
- * lengths of a batch and kept over layers and steps.  Host only.
+ * lengths of a batch and kept over layers and steps.  Host only (0.1 to 0.7 ms
+ * for up to 4,000 pieces of work, 15 ms for 128 sequences of 8,192 tokens with
+ * 16 heads).
  *   q_lens, k_lens  host [n_seq], >= 0; each sum at most 2^31 - 1024.
  *   n_ctas          thread blocks of a launch; 0 = the current device's SMs.
  *   plan            receives the sizes below.
@@ -536,7 +540,8 @@ int geocache_plan_attention(const int32_t* q_lens, const int32_t* k_lens, int n_
 /* --------------------------------------------------------------------------
  * geocache_attention -- the attention of a plan.  dtype is BF16 or F16;
  * scores, softmax statistics and sums are binary32, and the weights exp(...)
- * are rounded to `dtype` for the product with the values.
+ * are rounded to `dtype` for the product with the values (f16: those below
+ * 2^-14 of the row's reference weight keep fewer bits).
  *   schedule   device copy of the plan's schedule, 16-byte aligned.
  *   q, out     [plan->q_tokens, Hq, D];  k, v  [plan->k_tokens, Hk, D].  Data
  *              16-byte aligned, strides multiples of 8 elements.

@@ -10,12 +10,15 @@
 // O stays in tensor memory over the whole piece.  It is rescaled only when a row's weights of one tile of keys sum to more
 // than 2^15: until then the sums and P are kept relative to an older maximum, which changes no result beyond rounding,
 // and the maximum itself need not be taken in every tile.  S, the statistics and O are binary32; P is rounded to the
-// inputs' type, as the product with the values needs, while its sum is taken before that rounding.
+// inputs' type, as the product with the values needs, while its sum is taken before that rounding (f16: a weight below
+// 2^-14 of the row's reference keeps fewer bits, off by at most 2^-25 of it).
 //
-// What bounds it.  Heads over 64: the tensor cores (24,576 tokens x 16 heads of 128: 2.69 ms, 1,840 TFLOP/s; 8,192: 319
-// us, 1,720).  Heads up to 64: the softmax warps (a tile of 128 x 128 takes one 820 cycles alone and two of a scheduler
-// 1,490; the products take 1,050 for both tiles) and their waits: 8,192 tokens x 8 heads of 64 133 us, 1,030 TFLOP/s.  Few
-// rows: HBM (317,000 keys of 4 heads of 128: 100 us, 6.1 TB/s).
+// What bounds it.  Heads over 64, many rows: the tensor cores (24,576 tokens x 16 heads of 128: 2.69 to 2.86 ms from box
+// to box, 1,730 to 1,840 TFLOP/s; 8,192: 319 to 332 us, 1,660 to 1,720).  Heads up to 64: no unit is above half use
+// (tensor cores 48%, MUFU 48%, issue 46%; 8,192 tokens x 8 heads of 64 133 us, 1,030 TFLOP/s).  A pair of key tiles
+// takes about 2,190 cycles, of which the products need 1,060, and the softmax of both tiles 1,490 (820 for one alone; its
+// exponentials 1,090): the chain score - softmax - product is what takes the time, some 700 cycles of it between the
+// roles.  Few rows: HBM (298,000 keys of 4 heads of 128: 100 us, 6.1 TB/s).
 //
 // 128 x 128 tiles, since a tile's S and O for two tiles fill the 512 columns of tensor memory; two tiles a
 // block, so that products and softmax overlap; one block an SM, with a ring of 5 (8) stages in what the queries leave.

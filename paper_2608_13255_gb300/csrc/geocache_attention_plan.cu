@@ -1,10 +1,12 @@
 // How an attention launch divides its work (host only).
 //
 // A unit of work is one or two tiles of 128 query rows over the key tiles that they see.  Units go to thread blocks
-// whole, the longest first to the block with the least (no joins); or whole as long as they fit into an even share, the
-// rest cut along the keys to fill the blocks up; or, where little of the work fits so, all in order with the
-// boundaries between the blocks falling where the costs are even.  Parts of a unit are joined by a second kernel.  These
-// are laid out with one and with two tiles a unit, and the cheapest by the model below is kept.
+// whole, the longest first to the block with the least (no joins); or they are cut along their keys, and the parts of a
+// unit are joined by a second kernel: whole as long as they fit into an even share, the rest cut to fill the blocks up,
+// or, where less than a quarter of the work is in units that fit so, all in order with the boundaries between the blocks
+// falling where the costs are even.  The whole and the cut layout are made with one and with two tiles a unit, and the
+// cheapest by the model below is kept.  The model counts time on the SMs and no bytes: where HBM bounds the launch (few
+// rows, long keys) it is too low, which is why the two ways of cutting are told apart by the quarter and not by it.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -169,7 +171,7 @@ void assign_whole(const Problem& p, const Cost& c, Layout& l, bool fill) {
 // Units in order, cut where the blocks' costs are even.  Where a head's row is not whole 128-byte lines, units longer than
 // a block's share are taken in ranges of their keys, the same range of all heads of a sequence before the next one: blocks
 // that run at the same time then read the two heads of a line (22 rows over 98,304 keys of 72: 266 -> 218 us).  Whole
-// lines have nothing to share, and the ranges cost pieces (32 single tokens over 317,000 keys of 128: 99 -> 102 us).
+// lines have nothing to share, and the ranges cost pieces (32 single tokens over 298,000 keys of 128: 99 -> 102 us).
 void assign_even(const Problem& p, const Cost& c, Layout& l) {
     double total = 0.0, starts = 0.0, start = 0.0;
     for (const Unit& u : l.units) {
@@ -263,8 +265,9 @@ int plan(const Problem& prob, geocache_attention_plan* out, char* schedule, int6
         Layout l;
         l.tiles = tiles;
         l.units = make_units(p, tiles);
-        // cut what is left over where a good part of the work is in units that fit into a share (a quarter: continued
-        // prompts 42.6 -> 39.7 us by that), else cut all in order (32 single tokens, an eighth: 99.6 us, 102.6 otherwise)
+        // Cut what is left over where a good part of the work is in units that fit into a share, else cut all in order.
+        // Measured on both sides: continued prompts with a third of it 42.6 us in order and 39.7 so, 32 single tokens with a
+        // seventh 99.6 in order and 102.6 so; the quarter lies between.
         double total = 0.0, fitting = 0.0;
         for (const Unit& u : l.units) total += u.start(c, p.pack) + u.cost(c, 0, u.most());
         for (const Unit& u : l.units) {
@@ -328,7 +331,8 @@ int plan(const Problem& prob, geocache_attention_plan* out, char* schedule, int6
     int32_t* ptr = reinterpret_cast<int32_t*>(schedule);
     AttentionItem* item = reinterpret_cast<AttentionItem*>(schedule + geocache::attention_items_at(p.n_ctas));
     AttentionJoin* join = reinterpret_cast<AttentionJoin*>(item + n_items);
-    // a unit's pieces come in the order of their keys: they lie in consecutive blocks, or one block has them all
+    // a unit's pieces come in the order of their keys, block by block: each way fills the blocks one after the other, and
+    // ranges of keys come in their order, with other units' pieces between them
     std::vector<int> next[2] = {slot[0], slot[1]};
     int n = 0;
     for (int cta = 0; cta < p.n_ctas; ++cta) {

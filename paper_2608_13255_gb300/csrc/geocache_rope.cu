@@ -2,8 +2,10 @@
 //
 // Both kernels read each row (one head of one token) once and write it once; the sum of squares runs over the lanes that
 // hold the row, and beside the rows only one table row a token and the weights move, which the L1 serves to all heads.
-// 24,576 tokens x 32 heads of 128 take 73 us in bf16 (5.7 of 6.7 TB/s; the issue slots bound the rest) and 16 heads 63 us
-// in f32 (6.5 TB/s, HBM).  norm_rope_kernel takes the rows that norm_rope_pairs_kernel does not (halves that end inside
+// Back to back on one set of buffers 24,576 tokens x 32 heads of 128 take 68 (interleaved) and 74 us (halves) in bf16, 6.1
+// and 5.6 of 6.7 TB/s (72 us interleaved where the inputs change), and 120 us in f32, which is all of HBM.  Narrower heads are bound by issue, a lane's coefficients being made for two rows only: 32 heads
+// of 64 43 and 47 us (4.9 and 4.4 TB/s), of 40, 72 and 80 39, 64 and 66 us (3.4, 3.6 and 3.9 TB/s, lanes without words
+// besides).  norm_rope_kernel takes the rows that norm_rope_pairs_kernel does not (halves that end inside
 // a word of 8 bytes, no alignment, a head of one word) and is bound by issue.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -23,7 +25,9 @@ namespace {
 // Status word of this file's kernels (bit 5: a slot outside the table); read by geocache_device_status.
 __device__ unsigned int g_rope_error = 0;
 
-// One thread per (slot, pair); double throughout, since an angle of 10^5 turns keeps 2^-53 * 10^6 of itself.
+// One thread per (slot, pair); double throughout, since an angle of 10^5 turns keeps 2^-53 * 10^6 of itself.  Made once
+// per model and bound by the few binary64 units: 24,576 slots x 32 pairs 50 us, x 64 pairs 92 us, 17 pairs a ns (the
+// writes alone would take 1 and 2 us).
 __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__ RopeTableArgs a) {
     const long long n = a.n_slots * a.pairs;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
@@ -343,11 +347,12 @@ __device__ __noinline__ void norm_rows(const NormRopeArgs& a, int side, long lon
 // nothing but the sum of squares crosses lanes.  With the weights folded into the rotation a pair (a, b) becomes
 //     inv (a ca - b sb, a sa + b cb),  ca = w_a c, sa = w_a s, cb = w_b c, sb = w_b s,
 // three products and three sums an element in place of about ten operations of the general kernel, which is bound by
-// issue (24,576 tokens x 32 heads of 128 in bf16: 84 -> 73 us, 5.7 TB/s; halves of 64: 74 -> 51 us).
+// issue (24,576 tokens x 32 heads of 128 in bf16: 84 -> 73 us; halves of 64: 74 -> 51 us).
 // kFull: all lanes have words and the whole head is rotated (heads of 64, 128 and 256 in 16 bits), known to the compiler
-// (73 us; 79 without).  V: elements of a word; 16-bit rows that have an odd number of 16-byte words, or halves that are
-// not whole ones, take words of 8 bytes (24,576 tokens x 20 heads of 80, half rotated: 103 -> 53
-// us; 32 heads of 40: 95 -> 45 us).
+// (73 us; 79 without).  Two rows of 16-byte words of 16-bit elements a lane want more than the 80 registers that three
+// blocks an SM leave: these instances spill 36 to 60 bytes a thread, the others nothing.  V: elements of a word; 16-bit
+// rows that have an odd number of 16-byte words, or halves that are not whole ones, take words of 8 bytes (24,576 tokens x
+// 20 heads of 80, half rotated: 103 -> 53 us; 32 heads of 40: 95 -> 45 us).
 template <typename T, int V, int G, bool kInter, bool kFull, int kU>
 __global__ void __launch_bounds__(32 * kWarps, 3) norm_rope_pairs_kernel(const __grid_constant__ NormRopeArgs a, int heads,
                                                                          unsigned q_units, unsigned units, unsigned n_blocks) {

@@ -608,7 +608,8 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
     bf16 or f16; any strides between tokens and heads) normalised and rotated by
     table [n_slots, rot / 2, 2] at the tokens' slots (device int32 [T]; None:
     token t has slot t).  k may be None.  Outputs are allocated when None (on
-    the call's stream) and may be the inputs themselves.  Returns (q_out, k_out)."""
+    the call's stream) and may be the inputs themselves.  Forward only: results
+    carry no gradient.  Returns (q_out, k_out)."""
     T, Hq, D = q.shape
     dt = q.dtype
     if dt not in _HEAD_DTYPES:
@@ -641,7 +642,8 @@ def qk_norm_rope(q, k, table=None, slots=None, q_weight=None, k_weight=None, eps
 
 class AttentionPlan:
     """A plan (sizes in `info`), its schedule on the device and the workspace
-    of its calls.  Calls that may overlap on the GPU need a workspace each."""
+    of its calls.  Calls that may overlap on the GPU (on two streams) need a
+    workspace each: a plan each, or `attention`'s argument."""
 
     def __init__(self, info: AttentionPlanInfo, schedule, workspace):
         self.info = info
@@ -680,8 +682,8 @@ def plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0):
 def attention_plan(q_lens, k_lens, Hq, Hk, D, causal=False, n_ctas=0, device="cuda") -> AttentionPlan:
     """The plan of an attention over packed sequences with these lengths (host
     integers), for Hq query heads and Hk key/value heads of D elements.  Made
-    once for a batch and kept over layers and steps; the schedule and the
-    workspace are allocated here."""
+    once for a batch (0.1 to 0.7 ms for up to 4,000 pieces of work) and kept over
+    layers and steps; the schedule and the workspace are allocated here."""
     info, schedule = plan_attention_host(q_lens, k_lens, Hq, Hk, D, causal, n_ctas)
     workspace = None
     if info.workspace_bytes:
@@ -694,7 +696,9 @@ def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, work
     strides that are multiples of 8 elements) with the rows of the plan's
     sequences one after the other.  lse: device f32 [Tq, Hq] that receives the
     logarithms of the softmax sums, or None.  scale: None = 1/sqrt(D).
-    Returns out (allocated on the call's stream when None)."""
+    workspace: as large as plan.workspace, which is used when None; calls that
+    may overlap on the GPU need one each.  Forward only: the result carries no
+    gradient.  Returns out (allocated on the call's stream when None)."""
     f = plan.info
     dt = q.dtype
     if dt is not torch.bfloat16 and dt is not torch.float16:
