@@ -3,10 +3,11 @@
 // Both kernels read each row (one head of one token) once and write it once; the sum of squares runs over the lanes that
 // hold the row, and beside the rows only one table row a token and the weights move, which the L1 serves to all heads.
 // Back to back on one set of buffers 24,576 tokens x 32 heads of 128 take 68 (interleaved) and 74 us (halves) in bf16, 6.1
-// and 5.6 of 6.7 TB/s (72 us interleaved where the inputs change), and 120 us in f32, which is all of HBM.  Narrower heads are bound by issue, a lane's coefficients being made for two rows only: 32 heads
-// of 64 43 and 47 us (4.9 and 4.4 TB/s), of 40, 72 and 80 39, 64 and 66 us (3.4, 3.6 and 3.9 TB/s, lanes without words
-// besides).  norm_rope_kernel takes the rows that norm_rope_pairs_kernel does not (halves that end inside
-// a word of 8 bytes, no alignment, a head of one word) and is bound by issue.
+// and 5.6 of 6.7 TB/s (72 us interleaved where the inputs change), and 120 us in f32, which is all of HBM.  Narrower heads
+// are bound by issue, a lane's coefficients being made for two rows only: 32 heads of 64 43 and 47 us (4.9 and 4.4 TB/s),
+// of 40, 72 and 80 39, 64 and 66 us (3.4, 3.6 and 3.9 TB/s, lanes without words besides).  norm_rope_kernel takes the rows
+// that norm_rope_pairs_kernel does not (halves that end inside a word of 8 bytes, no alignment, a head of one word) and
+// is bound by issue.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
