@@ -50,7 +50,8 @@ typedef enum {
 typedef enum {
     GEOCACHE_F32 = 0,
     GEOCACHE_BF16 = 1,
-    GEOCACHE_F16 = 2  /* queries, keys and values of the attention block only */
+    GEOCACHE_F16 = 2, /* rows and heads of a denoiser's block only */
+    GEOCACHE_E4M3 = 3 /* 8-bit rows with a scale each (geocache_add_rms_norm, geocache_quantize_rows, geocache_linear) */
 } geocache_dtype;
 
 typedef enum { GEOCACHE_DDIM = 0, GEOCACHE_FM_EULER = 1 } geocache_sampler;
@@ -562,6 +563,89 @@ int geocache_attention(const geocache_attention_plan* plan, const void* schedule
                        geocache_dtype dtype, double scale, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* --------------------------------------------------------------------------
+ * What stands around the attention in a denoiser's block: the norm with the
+ * residual's addition, 8-bit rows, and the projections.  Rows are tokens, those
+ * of all assets one after the other; forward only.
+ * ------------------------------------------------------------------------ */
+
+/* Rows of a [T, C] tensor: element (t, c) is at data + t * stride + c (the
+ * stride in elements, >= 0). */
+typedef struct {
+    void* data;            /* device */
+    int64_t stride;
+} geocache_rows;
+
+/* --------------------------------------------------------------------------
+ * geocache_add_rms_norm -- the residual's addition and the RMS norm of each
+ * row, in one pass:
+ *     h = x + residual, rounded to residual_dtype and written to residual_out
+ *     y = h * rsqrt(mean_c(h_c^2) + eps) * weight_c
+ * and out = y rounded to `dtype` (scale NULL), or 8-bit rows (scale given):
+ *     scale = max(max_c |y_c| / 448, 2^-126),  out = e4m3(y / scale),
+ * so that out * scale stands for y.  What is rounded to residual_dtype is what
+ * is normalised; the mean, y and the scale are binary32 (a row whose h^2 or
+ * h * weight overflow binary32 has no useful result).  A NaN or infinity stays
+ * in its row.
+ *   x                       [T, C] of `dtype` (F32, BF16 or F16).
+ *   residual, residual_out  [T, C] of residual_dtype (`dtype` or F32), or NULL both.
+ *   out                     [T, C] of `dtype`, or E4M3 with `scale`.
+ *   weight                  device [C] f32, or NULL (ones).
+ *   scale                   device [T] f32, or NULL.
+ * residual_out may be the residual or, in one type, x itself (pointer and
+ * stride), and out may be x or the residual; any other overlap with an output is
+ * refused.  Sizes: 0 <= T < 2^31, 1 <= C <= 65536, eps >= 0.  Any alignment of
+ * the elements is accepted; rows that are 16-byte aligned are read and written
+ * in words of 16 bytes (8-bit rows: 8).
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE, EDTYPE, EALIAS, ECUDA.
+ * ------------------------------------------------------------------------ */
+int geocache_add_rms_norm(const geocache_rows* x, const geocache_rows* residual, const geocache_rows* residual_out,
+                          const geocache_rows* out, int64_t T, int C, geocache_dtype dtype,
+                          geocache_dtype residual_dtype, const float* weight, double eps, float* scale, void* stream);
+
+/* --------------------------------------------------------------------------
+ * geocache_quantize_rows -- 8-bit rows of what follows no norm (the
+ * attention's output, a feed-forward's hidden rows, weights):
+ *     scale = max(max_c |x_c| / 448, 2^-126),  out = e4m3(x / scale).
+ * x [T, C] of `dtype` (F32, BF16 or F16), out [T, C] E4M3, scale device [T] f32.
+ * Sizes, alignment and statuses as geocache_add_rms_norm; no buffers overlap.
+ * ------------------------------------------------------------------------ */
+int geocache_quantize_rows(const geocache_rows* x, const geocache_rows* out, int64_t T, int C, geocache_dtype dtype,
+                           float* scale, void* stream);
+
+typedef enum {
+    GEOCACHE_ACT_NONE = 0,
+    GEOCACHE_ACT_GELU = 1,       /* z (1 + erf(z / sqrt 2)) / 2 */
+    GEOCACHE_ACT_GELU_TANH = 2,  /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+    GEOCACHE_ACT_SILU = 3        /* z / (1 + exp(-z)) */
+} geocache_activation;
+
+/* --------------------------------------------------------------------------
+ * geocache_linear -- a projection with its epilogue:
+ *     z = x_scale_t weight_scale_n (x_t . weight_n) + bias_n
+ *     out = act(z) + residual, or, gated, out_n = z_n act(z_{N+n}) + residual
+ * with the sums and the epilogue in binary32, rounded once to out_dtype.  Every
+ * call gives the same bits for the same arguments.
+ *   x             [T, K] of in_dtype: BF16, F16, or E4M3 with both scales.
+ *   weight        [N, K] of in_dtype; gated [2 N, K], the values' rows first.
+ *   bias          device f32 [N] (gated [2 N]), or NULL.
+ *   x_scale       device [T] f32, weight_scale [N] (gated [2 N]): E4M3 only.
+ *   residual      [T, N] of out_dtype, or NULL; may be out itself.
+ *   out           [T, N] of out_dtype: in_dtype or F32; for E4M3 BF16, F16 or F32.
+ * x and weight are 16-byte aligned with strides of whole 16 bytes (of a single
+ * row the stride is not read); out and the residual have any alignment and are
+ * written and read in wider words where their rows are aligned to them.
+ * Otherwise out must not overlap an input.  Sizes: 0 <= T < 2^31 - 1024, 1 <= K <= 2^20,
+ * 1 <= N <= 2^20.  A NaN or infinity in a row of x (of the weights) reaches that
+ * row (column) of out only.
+ * Returns GEOCACHE_OK, EINVAL, ESHAPE, EDTYPE, EALIAS, ECUDA; a wait inside the
+ * kernel that ran out sets the device status word (ETIMEOUT).
+ * ------------------------------------------------------------------------ */
+int geocache_linear(const geocache_rows* x, const geocache_rows* weight, const geocache_rows* residual,
+                    const geocache_rows* out, int64_t T, int K, int N, geocache_dtype in_dtype,
+                    geocache_dtype out_dtype, geocache_activation act, int gated, const float* bias,
+                    const float* x_scale, const float* weight_scale, void* stream);
+
+/* --------------------------------------------------------------------------
  * geocache_is_full_step -- 1 if `step` (0 <= step < S) is a full step under
  * `sched`, 0 if cached, a negative status on bad arguments. Host only.
  * ------------------------------------------------------------------------ */
@@ -608,7 +692,7 @@ int geocache_device_status(void* stream);
  * H*W % 8 == 0 and 16-byte aligned buffers; MASK steps of any size while
  * drop_first_copy is pending) waits for its shared-memory copies
  * with a time limit instead of spinning forever; so do the roles of
- * geocache_attention's kernel for each other.
+ * geocache_attention's and geocache_linear's kernels for each other.
  *   limit_ns         limit of those waits for later calls (0 = the default, 2 s).
  *   drop_first_copy  nonzero: the next call that runs the staged kernel arms
  *                    none of the copies of its first unit (asset 0, view 0,
@@ -619,7 +703,9 @@ int geocache_device_status(void* stream);
  *                    outputs of its units, and the context stays usable.  The
  *                    request is consumed by that call.  A geocache_attention
  *                    consumes it as well: its first thread block leaves its first
- *                    copy of keys unissued and ends like that.
+ *                    copy of keys unissued and ends like that.  So does a
+ *                    geocache_linear, whose first thread block leaves its first
+ *                    copies unissued.
  * Process-wide, not thread safe.  Returns GEOCACHE_OK.
  * ------------------------------------------------------------------------ */
 int geocache_debug_set_wait(uint64_t limit_ns, int drop_first_copy);

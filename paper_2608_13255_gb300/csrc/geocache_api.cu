@@ -136,6 +136,75 @@ int check_heads(const geocache_heads* x, int64_t T, int H, int D, int eb, bool w
     return GEOCACHE_OK;
 }
 
+// [T, C] rows are heads of a single one
+geocache_heads as_heads(const geocache_rows* x) { return {x->data, x->stride, 0}; }
+
+int check_rows(const geocache_rows* x, int64_t T, int C, int eb, bool write, const char* fn, const char* name) {
+    if (!x) return fail(GEOCACHE_EINVAL, "%s: %s is required", fn, name);
+    const geocache_heads h = as_heads(x);
+    return check_heads(&h, T, 1, C, eb, write, fn, name);
+}
+
+size_t rows_extent(const geocache_rows* x, int64_t T, int C, int eb) {
+    const geocache_heads h = as_heads(x);
+    return heads_extent(&h, T, 1, C, eb);
+}
+
+bool rows_overlap_bytes(const geocache_rows* x, int64_t T, int C, int eb, const void* p, size_t n) {
+    return overlap(x->data, rows_extent(x, T, C, eb), p, n);
+}
+
+// Two row tensors share a byte.  Exact where both have one stride (in bytes) that holds a row of each.
+bool rows_overlap(const geocache_rows* a, int64_t Ta, int Ca, int ea, const geocache_rows* b, int64_t Tb, int Cb, int eb) {
+    if (!overlap(a->data, rows_extent(a, Ta, Ca, ea), b->data, rows_extent(b, Tb, Cb, eb))) return false;
+    const int64_t row = a->stride * ea, wa = (int64_t)Ca * ea, wb = (int64_t)Cb * eb;
+    if (Ta > 1 && Tb > 1 && row == b->stride * eb && wa <= row && wb <= row)
+        return meet(0, wa, (int64_t)((uintptr_t)b->data - (uintptr_t)a->data), wb, row);
+    return true;
+}
+
+int norm_rows(const char* fn, const geocache_rows* x, const geocache_rows* residual, const geocache_rows* residual_out,
+              const geocache_rows* out, int64_t T, int C, int dtype, int residual_dtype, const float* weight, int norm, float eps,
+              float* scale, void* stream) {
+    if (T < 0 || T > 0x7fffffffLL || C < 1 || C > 65536)
+        return fail(GEOCACHE_ESHAPE, "%s: T=%lld, C=%d out of range", fn, (long long)T, C);
+    if (dtype != GEOCACHE_F32 && dtype != GEOCACHE_BF16 && dtype != GEOCACHE_F16)
+        return fail(GEOCACHE_EDTYPE, "%s: unsupported dtype %d", fn, dtype);
+    if (((uintptr_t)weight | (uintptr_t)scale) & 3) return fail(GEOCACHE_EINVAL, "%s: weight and scale must be 4-byte aligned", fn);
+    if (T == 0) return ok();
+    const int eb = dtype == GEOCACHE_F32 ? 4 : 2, rb = residual_dtype == GEOCACHE_F32 ? 4 : eb, ob = scale ? 1 : eb;
+    int st = check_rows(x, T, C, eb, false, fn, "x");
+    if (!st) st = check_rows(out, T, C, ob, true, fn, "out");
+    if (!st && residual) st = check_rows(residual, T, C, rb, false, fn, "residual");
+    if (!st && residual) st = check_rows(residual_out, T, C, rb, true, fn, "residual_out");
+    if (st) return st;
+    // an output takes an input's place only element by element, as the thread that reads an element writes it
+    auto apart = [&](const geocache_rows* w, int wb, const geocache_rows* r, int b) {
+        return (w->data == r->data && (T == 1 || w->stride == r->stride) && wb == b) || !rows_overlap(w, T, C, wb, r, T, C, b);
+    };
+    if (!apart(out, ob, x, eb) || (residual && (!apart(out, ob, residual, rb) || !apart(residual_out, rb, x, eb) ||
+                                                !apart(residual_out, rb, residual, rb))))
+        return fail(GEOCACHE_EALIAS, "%s: an output overlaps an input in part", fn);
+    if (residual && rows_overlap(out, T, C, ob, residual_out, T, C, rb))
+        return fail(GEOCACHE_EALIAS, "%s: out overlaps residual_out", fn);
+    const size_t wn = weight ? (size_t)C * 4 : 0, sn = scale ? (size_t)T * 4 : 0;
+    if (rows_overlap_bytes(out, T, C, ob, weight, wn) || rows_overlap_bytes(out, T, C, ob, scale, sn) ||
+        rows_overlap_bytes(x, T, C, eb, scale, sn) || overlap(weight, wn, scale, sn) ||
+        (residual && (rows_overlap_bytes(residual_out, T, C, rb, weight, wn) || rows_overlap_bytes(residual_out, T, C, rb, scale, sn) ||
+                      rows_overlap_bytes(residual, T, C, rb, scale, sn))))
+        return fail(GEOCACHE_EALIAS, "%s: an output overlaps the weight, the scales or another buffer", fn);
+    geocache::NormRowsArgs a{};
+    a.x = *x; a.out = *out;
+    if (residual) { a.residual = *residual; a.residual_out = *residual_out; }
+    a.weight = weight; a.scale = scale;
+    a.T = T; a.C = C; a.norm = norm; a.dtype = dtype;
+    a.residual_f32 = residual && residual_dtype == GEOCACHE_F32;
+    a.eps = eps;
+    cudaError_t e = geocache::launch_norm_rows(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, fn);
+    return ok();
+}
+
 size_t lat_bytes(int dtype) { return dtype == GEOCACHE_BF16 ? 2 : 4; }
 
 // total record count of the sparse form (synchronises the stream)
@@ -749,6 +818,80 @@ int geocache_attention(const geocache_attention_plan* p, const void* schedule, c
     a.wait_limit_ns = geocache::debug_wait_limit_ns();
     a.drop_first_copy = geocache::take_drop_first_copy();
     cudaError_t e = geocache::launch_attention(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, fn);
+    return ok();
+}
+
+int geocache_add_rms_norm(const geocache_rows* x, const geocache_rows* residual, const geocache_rows* residual_out,
+                          const geocache_rows* out, int64_t T, int C, geocache_dtype dtype,
+                          geocache_dtype residual_dtype, const float* weight, double eps, float* scale, void* stream) {
+    const char* fn = "geocache_add_rms_norm";
+    g_launches = 0;
+    if (!(eps >= 0.0) || !std::isfinite((float)eps)) return fail(GEOCACHE_EINVAL, "%s: eps=%g must be >= 0", fn, eps);
+    if ((residual == nullptr) != (residual_out == nullptr))
+        return fail(GEOCACHE_EINVAL, "%s: residual and residual_out must both be given or neither", fn);
+    if (residual && residual_dtype != dtype && residual_dtype != GEOCACHE_F32)
+        return fail(GEOCACHE_EDTYPE, "%s: residual's dtype %d is neither x's nor F32", fn, (int)residual_dtype);
+    return norm_rows(fn, x, residual, residual_out, out, T, C, dtype, residual_dtype, weight, 1, (float)eps, scale, stream);
+}
+
+int geocache_quantize_rows(const geocache_rows* x, const geocache_rows* out, int64_t T, int C, geocache_dtype dtype,
+                           float* scale, void* stream) {
+    const char* fn = "geocache_quantize_rows";
+    g_launches = 0;
+    if (T > 0 && !scale) return fail(GEOCACHE_EINVAL, "%s: scale is required", fn);
+    return norm_rows(fn, x, nullptr, nullptr, out, T, C, dtype, dtype, nullptr, 0, 0.0f, scale, stream);
+}
+
+int geocache_linear(const geocache_rows* x, const geocache_rows* weight, const geocache_rows* residual,
+                    const geocache_rows* out, int64_t T, int K, int N, geocache_dtype in_dtype,
+                    geocache_dtype out_dtype, geocache_activation act, int gated, const float* bias,
+                    const float* x_scale, const float* weight_scale, void* stream) {
+    const char* fn = "geocache_linear";
+    g_launches = 0;
+    if (T < 0 || T > geocache::kAttentionTokens || K < 1 || K > 1 << 20 || N < 1 || N > 1 << 20)
+        return fail(GEOCACHE_ESHAPE, "%s: T=%lld, K=%d, N=%d out of range", fn, (long long)T, K, N);
+    const bool eight = in_dtype == GEOCACHE_E4M3;
+    if (!eight && in_dtype != GEOCACHE_BF16 && in_dtype != GEOCACHE_F16)
+        return fail(GEOCACHE_EDTYPE, "%s: unsupported dtype %d", fn, (int)in_dtype);
+    if (out_dtype != GEOCACHE_F32 && !(eight && (out_dtype == GEOCACHE_BF16 || out_dtype == GEOCACHE_F16)) &&
+        (eight || out_dtype != in_dtype))
+        return fail(GEOCACHE_EDTYPE, "%s: out's dtype %d does not go with x's %d", fn, (int)out_dtype, (int)in_dtype);
+    if (act < GEOCACHE_ACT_NONE || act > GEOCACHE_ACT_SILU) return fail(GEOCACHE_EINVAL, "%s: unknown activation %d", fn, (int)act);
+    if ((x_scale != nullptr) != eight || (weight_scale != nullptr) != eight)
+        return fail(GEOCACHE_EINVAL, "%s: 8-bit operands, and no others, have x_scale and weight_scale", fn);
+    if (((uintptr_t)bias | (uintptr_t)x_scale | (uintptr_t)weight_scale) & 3)
+        return fail(GEOCACHE_EINVAL, "%s: bias and scales must be 4-byte aligned", fn);
+    if (T == 0) return ok();
+    const int eb = eight ? 1 : 2, ob = out_dtype == GEOCACHE_F32 ? 4 : 2, rows = gated ? 2 * N : N;
+    int st = check_rows(x, T, K, eb, false, fn, "x");
+    if (!st) st = check_rows(weight, rows, K, eb, false, fn, "weight");
+    if (!st) st = check_rows(out, T, N, ob, true, fn, "out");
+    if (!st && residual) st = check_rows(residual, T, N, ob, false, fn, "residual");
+    if (st) return st;
+    const geocache_rows* in[2] = {x, weight};
+    const char* name[2] = {"x", "weight"};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t n = i ? rows : T;
+        if (((uintptr_t)in[i]->data & 15) || (n > 1 && in[i]->stride * eb % 16))
+            return fail(GEOCACHE_EINVAL, "%s: %s must be 16-byte aligned with a stride of whole 16 bytes", fn, name[i]);
+        if (rows_overlap(out, T, N, ob, in[i], n, K, eb)) return fail(GEOCACHE_EALIAS, "%s: out overlaps %s", fn, name[i]);
+    }
+    if (residual && !(residual->data == out->data && (T == 1 || residual->stride == out->stride)) &&
+        rows_overlap(out, T, N, ob, residual, T, N, ob))
+        return fail(GEOCACHE_EALIAS, "%s: out overlaps the residual in part", fn);
+    if (rows_overlap_bytes(out, T, N, ob, bias, (size_t)rows * 4) || rows_overlap_bytes(out, T, N, ob, weight_scale, (size_t)rows * 4) ||
+        rows_overlap_bytes(out, T, N, ob, x_scale, (size_t)T * 4))
+        return fail(GEOCACHE_EALIAS, "%s: out overlaps the bias or a scale", fn);
+    geocache::LinearArgs a{};
+    a.x = *x; a.w = *weight; a.out = *out;
+    if (residual) a.residual = *residual;
+    a.T = T; a.K = K; a.N = N;
+    a.in_dtype = in_dtype; a.out_dtype = out_dtype; a.act = act; a.gated = gated != 0;
+    a.bias = bias; a.x_scale = x_scale; a.w_scale = weight_scale;
+    a.wait_limit_ns = geocache::debug_wait_limit_ns();
+    a.drop_first_copy = geocache::take_drop_first_copy();
+    cudaError_t e = geocache::launch_linear(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, fn);
     return ok();
 }

@@ -92,6 +92,7 @@ cudaError_t read_device_error(unsigned int* out, bool clear, cudaStream_t s);
 cudaError_t raster_error_word(unsigned int** word);     // their device addresses
 cudaError_t rope_error_word(unsigned int** word);
 cudaError_t attention_error_word(unsigned int** word);
+cudaError_t linear_error_word(unsigned int** word);
 // test hook of the bounded waits (geocache_debug_set_wait)
 void set_debug_wait(unsigned long long limit_ns, int drop_first_copy);
 // position maps at the token grid H x W; ss > 1: rendered at ss x H by
@@ -171,6 +172,28 @@ struct AttentionArgs {
     int drop_first_copy;
 };
 cudaError_t launch_attention(const AttentionArgs& a, cudaStream_t s);
+
+struct NormRowsArgs {
+    geocache_rows x, residual, residual_out, out;   // residual.data = nullptr: none
+    const float* weight;     // [C] or nullptr
+    float* scale;            // [T]: the output is e4m3; nullptr: of the input's type
+    long long T;
+    int C, norm, dtype, residual_f32;
+    float eps;
+    // set by the launch: threads of a row, and which rows are whole 16-byte words
+    int lanes, x_aligned, residual_aligned, out_aligned, weight_aligned;
+};
+cudaError_t launch_norm_rows(const NormRowsArgs& a, cudaStream_t s);
+
+struct LinearArgs {
+    geocache_rows x, w, out, residual;   // residual.data = nullptr: none
+    long long T;
+    int K, N, in_dtype, out_dtype, act, gated;
+    const float *bias, *x_scale, *w_scale;
+    unsigned long long wait_limit_ns;
+    int drop_first_copy;
+};
+cudaError_t launch_linear(const LinearArgs& a, cudaStream_t s);
 // the limit of bounded waits, and the test hook's pending request (consumed)
 unsigned long long debug_wait_limit_ns();
 int take_drop_first_copy();

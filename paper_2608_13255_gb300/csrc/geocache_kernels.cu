@@ -3012,18 +3012,19 @@ cudaError_t launch_reconstruct(const void* x_t, const float* x0, void* x_next, i
 
 // Moves the words of the other sources into this one's, which is then all that the host has to wait for (38 us with a
 // copy for each source).
-__global__ void gather_errors_kernel(unsigned int* raster, unsigned int* rope, unsigned int* attention) {
-    const unsigned int word = atomicExch(raster, 0u) | atomicExch(rope, 0u) | atomicExch(attention, 0u);
+__global__ void gather_errors_kernel(unsigned int* raster, unsigned int* rope, unsigned int* attention, unsigned int* linear) {
+    const unsigned int word = atomicExch(raster, 0u) | atomicExch(rope, 0u) | atomicExch(attention, 0u) | atomicExch(linear, 0u);
     if (word) atomicOr(&g_device_error, word);
 }
 
 cudaError_t read_device_error(unsigned int* out, bool clear, cudaStream_t s) {
-    unsigned int *raster, *rope, *attention;
+    unsigned int *raster, *rope, *attention, *linear;
     cudaError_t e = raster_error_word(&raster);
     if (e == cudaSuccess) e = rope_error_word(&rope);
     if (e == cudaSuccess) e = attention_error_word(&attention);
+    if (e == cudaSuccess) e = linear_error_word(&linear);
     if (e != cudaSuccess) return e;
-    gather_errors_kernel<<<1, 1, 0, s>>>(raster, rope, attention);
+    gather_errors_kernel<<<1, 1, 0, s>>>(raster, rope, attention, linear);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     e = cudaMemcpyFromSymbolAsync(out, g_device_error, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, s);

@@ -20,7 +20,7 @@ import torch
 from . import build as _build
 
 OK, EINVAL, ESHAPE, EDTYPE, ECUDA, ETIMEOUT, EDEVICE, EALIAS = 0, -1, -2, -3, -4, -5, -6, -7
-F32, BF16, F16 = 0, 1, 2
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
 DDIM, FM_EULER = 0, 1
 PRED_NONE, PRED_EPS, PRED_V, PRED_VELOCITY = 0, 1, 2, 3
 CORR_GEOMETRY, CORR_TABLE, CORR_MASK, CORR_SPARSE = 0, 1, 2, 3
@@ -30,6 +30,7 @@ SCHED_EVERY_K, SCHED_HEAD_MID_TAIL, SCHED_LIST, SCHED_ALL_FULL, SCHED_SINGLE_CAC
 MAX_VIEWS = 64
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
+ACT_NONE, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3
 
 _SAMPLERS = {"ddim": DDIM, "fm_euler": FM_EULER, DDIM: DDIM, FM_EULER: FM_EULER}
 _PREDS = {None: PRED_NONE, "none": PRED_NONE, "eps": PRED_EPS, "v": PRED_V, "velocity": PRED_VELOCITY,
@@ -73,6 +74,10 @@ class Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
 class Rope(ctypes.Structure):
     _fields_ = [("rot", ctypes.c_int), ("theta", ctypes.c_double), ("scaling", ctypes.c_int),
                 ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double),
@@ -96,6 +101,7 @@ EXPORTS = ("geocache_build_corr", "geocache_transport_step", "geocache_reconstru
            "geocache_raster_posmaps", "geocache_debug_set_wait", "geocache_raster_posmaps_supersampled",
            "geocache_pool_posmaps", "geocache_fill_records", "geocache_last_launches",
            "geocache_rope_table", "geocache_qk_norm_rope", "geocache_plan_attention", "geocache_attention",
+           "geocache_add_rms_norm", "geocache_quantize_rows", "geocache_linear",
            "geocache_last_error", "geocache_abi_version")
 
 
@@ -141,6 +147,12 @@ def load():
         L.geocache_plan_attention.restype = ctypes.c_int
         L.geocache_attention.argtypes = [P, P, P, P, P, P, P, i, ctypes.c_double, P, i64, P]
         L.geocache_attention.restype = ctypes.c_int
+        L.geocache_add_rms_norm.argtypes = [P, P, P, P, i64, i, i, i, P, ctypes.c_double, P, P]
+        L.geocache_add_rms_norm.restype = ctypes.c_int
+        L.geocache_quantize_rows.argtypes = [P, P, i64, i, i, P, P]
+        L.geocache_quantize_rows.restype = ctypes.c_int
+        L.geocache_linear.argtypes = [P, P, P, P, i64, i, i, i, i, i, i, P, P, P, P]
+        L.geocache_linear.restype = ctypes.c_int
         L.geocache_corr_record_count.argtypes = [ctypes.POINTER(Corr), ctypes.POINTER(ctypes.c_int64), P]
         L.geocache_corr_record_count.restype = ctypes.c_int
         L.geocache_fill_records.argtypes = [ctypes.POINTER(Corr), P]
@@ -713,6 +725,132 @@ def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, work
         plan.address, plan.schedule.data_ptr(), at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE,
         _dev(lse, torch.float32, Tq * Hq, "lse"), _HEAD_DTYPES[dt], D ** -0.5 if scale is None else float(scale),
         _dev(ws, torch.float32, None, "workspace"), 0 if ws is None else 4 * ws.numel(), _stream(stream)))
+    return out
+
+
+# ------------------------------------ around the attention of a block --
+_E4M3 = torch.float8_e4m3fn
+_ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, _E4M3: E4M3}
+_ACTIVATIONS = {None: ACT_NONE, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
+_ROWS_SIZE = ctypes.sizeof(Rows)
+
+
+def _rows_of(t, dtype, T, C, name):
+    """(address, stride) of a [T, C] view whose rows' elements are consecutive."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == (T, C):
+        rs, es = t.stride()
+        if es == 1 or C == 1:
+            return t.data_ptr(), rs
+        raise ValueError("the elements of a row of %s must be consecutive" % name)
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s (got %s)" % (name, dtype, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be on a CUDA device" % name)
+    raise ValueError("%s must be [%d, %d] (got %s)" % (name, T, C, list(t.shape)))
+
+
+def _norm_input(x):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch tensor")
+    if x.dtype is _E4M3 or x.dtype not in _ROW_DTYPES:
+        raise TypeError("x must be float32, bfloat16 or float16 (got %s)" % x.dtype)
+    T, C = x.shape
+    return T, C, x.dtype
+
+
+def add_rms_norm(x, residual=None, weight=None, eps=1e-6, out=None, scale=None, residual_out=None, quantize=False,
+                 stream=None):
+    """geocache_add_rms_norm: the rows of x [T, C] (f32, bf16 or f16; any stride
+    between rows) with the residual [T, C] (x's type or f32) added, normalised and
+    multiplied by weight (device f32 [C]).  The output has x's type, or, with
+    `quantize` (or an `out` of float8_e4m3fn, or `scale`), 8 bits with a scale for
+    each row: out * scale[:, None] stands for the result.  Outputs are allocated when
+    None (on the call's stream); residual_out may be the residual itself.  Forward
+    only: results carry no gradient.  Returns (out, scale or None, residual_out or
+    None)."""
+    T, C, dt = _norm_input(x)
+    if scale is not None or (out is not None and out.dtype is _E4M3):
+        quantize = True
+    if out is None:
+        out = _empty((T, C), _E4M3 if quantize else dt, x.device, stream)
+    if quantize and scale is None:
+        scale = _empty((T,), torch.float32, x.device, stream)
+    at_r = at_o = 0
+    f32 = torch.float32
+    rd, rows = dt, _rows_of(x, dt, T, C, "x") + _rows_of(out, _E4M3 if quantize else dt, T, C, "out")
+    if residual is not None:
+        rd = residual.dtype
+        if rd is not dt and rd is not f32:
+            raise TypeError("residual must be %s or float32 (got %s)" % (dt, rd))
+        if residual_out is None:
+            residual_out = _empty((T, C), rd, x.device, stream)
+        rows += _rows_of(residual, rd, T, C, "residual") + _rows_of(residual_out, rd, T, C, "residual_out")
+    elif residual_out is not None:
+        raise ValueError("residual_out without residual")
+    held = array.array("q", rows)
+    at = held.buffer_info()[0]
+    if residual is not None:
+        at_r, at_o = at + 2 * _ROWS_SIZE, at + 3 * _ROWS_SIZE
+    _check(load().geocache_add_rms_norm(at, at_r, at_o, at + _ROWS_SIZE, T, C, _ROW_DTYPES[dt], _ROW_DTYPES[rd],
+                                        _dev(weight, f32, C, "weight"), float(eps), _dev(scale, f32, T, "scale"),
+                                        _stream(stream)))
+    return out, scale, residual_out
+
+
+def quantize_rows(x, out=None, scale=None, stream=None):
+    """geocache_quantize_rows: the rows of x [T, C] (f32, bf16 or f16; any stride
+    between rows) in 8 bits (float8_e4m3fn) with a scale each (device f32 [T]).
+    Outputs are allocated when None (on the call's stream).  Returns (out, scale)."""
+    T, C, dt = _norm_input(x)
+    if out is None:
+        out = _empty((T, C), _E4M3, x.device, stream)
+    if scale is None:
+        scale = _empty((T,), torch.float32, x.device, stream)
+    held = array.array("q", _rows_of(x, dt, T, C, "x") + _rows_of(out, _E4M3, T, C, "out"))
+    at = held.buffer_info()[0]
+    _check(load().geocache_quantize_rows(at, at + _ROWS_SIZE, T, C, _ROW_DTYPES[dt], _dev(scale, torch.float32, T, "scale"),
+                                         _stream(stream)))
+    return out, scale
+
+
+def linear(x, weight, bias=None, activation=None, gated=False, residual=None, x_scale=None, weight_scale=None, out=None,
+           out_dtype=None, stream=None):
+    """geocache_linear: act(x weight^T + bias) + residual for x [T, K] and weight
+    [N, K] (bf16, f16, or float8_e4m3fn with the scales of their rows, x_scale
+    [T] and weight_scale [N] f32; 16-byte aligned, strides of whole 16 bytes).
+    activation: None, "gelu", "gelu_tanh" or "silu".  gated: weight is [2 N, K], the
+    values' rows before the gates', and the result (values + bias) * act(gates +
+    bias) + residual.  bias: f32 [N] (gated [2 N]).  residual: [T, N] of the
+    output's type; may be `out` itself.  The output is x's type or f32 (8-bit
+    operands: bf16, f16 or f32); it is allocated on the call's stream when None, as
+    `out_dtype` (None: x's type, or bf16).  Forward only: the result carries no
+    gradient.  Returns out."""
+    T, K = x.shape
+    rows = weight.shape[0]
+    if gated and rows % 2:
+        raise ValueError("a gated product has an even number of weight rows (got %d)" % rows)
+    N = rows // 2 if gated else rows
+    dt = x.dtype
+    if out is None:
+        if out_dtype is None:
+            out_dtype = torch.bfloat16 if dt is _E4M3 else dt
+        out = _empty((T, N), out_dtype, x.device, stream)
+    elif out_dtype is not None and out.dtype is not out_dtype:
+        raise TypeError("out must be %s (got %s)" % (out_dtype, out.dtype))
+    od = out.dtype
+    if dt not in _ROW_DTYPES or od not in _ROW_DTYPES:
+        raise TypeError("x and out cannot be %s and %s" % (dt, od))
+    held = array.array("q", _rows_of(x, dt, T, K, "x") + _rows_of(weight, dt, rows, K, "weight") +
+                       _rows_of(out, od, T, N, "out") +
+                       ((0, 0) if residual is None else _rows_of(residual, od, T, N, "residual")))
+    at = held.buffer_info()[0]
+    f32 = torch.float32
+    _check(load().geocache_linear(
+        at, at + _ROWS_SIZE, 0 if residual is None else at + 3 * _ROWS_SIZE, at + 2 * _ROWS_SIZE, T, K, N, _ROW_DTYPES[dt],
+        _ROW_DTYPES[od], _ACTIVATIONS[activation], 1 if gated else 0, _dev(bias, f32, rows, "bias"),
+        _dev(x_scale, f32, T, "x_scale"), _dev(weight_scale, f32, rows, "weight_scale"), _stream(stream)))
     return out
 
 
