@@ -1,0 +1,123 @@
+// What the matrix products' kernels share: copies, products, the epilogue's arithmetic, the launch.
+#pragma once
+
+#include <cstdint>
+#include <type_traits>
+
+#include "geocache.h"
+#include "geocache_device.cuh"
+#include "geocache_internal.h"
+#include "geocache_tcgen05.cuh"
+
+namespace geocache {
+
+constexpr int kRowBytes = 128;   // of an operand's row in a stage: 64 16-bit elements or 128 of 8 bits (one swizzle row)
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+        : "memory");
+}
+// D (tensor memory) = A B (+ D), A and B in shared memory, 32 bytes of a row of each
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool eight, uint32_t accumulate) {
+    if (eight)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_cluster(uint32_t at, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
+    return r;
+}
+
+// ------------------------------------------------------------- epilogue --
+// exp(-x) overflows to infinity below -88, where the quotient is -0 as it should be
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+__device__ __forceinline__ float activate(float x, int act) {
+    switch (act) {
+        case GEOCACHE_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+        // (1 + tanh u) / 2 = sigmoid(2 u)
+        case GEOCACHE_ACT_GELU_TANH: return x * sigmoid(1.5957691216057308f * fmaf(0.044715f * x * x, x, x));
+        case GEOCACHE_ACT_SILU: return x * sigmoid(x);
+        default: return x;
+    }
+}
+template <typename T>
+__device__ __forceinline__ T rounded(float x) {
+    if constexpr (std::is_same<T, float>::value) return x;
+    else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
+    else return __float2bfloat16_rn(x);
+}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+
+template <typename T>
+__device__ __forceinline__ void unpack2(uint32_t w, float* v) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        v[0] = f.x;
+        v[1] = f.y;
+    } else {
+        v[0] = __uint_as_float(w << 16);
+        v[1] = __uint_as_float(w & 0xffff0000u);
+    }
+}
+
+// ----------------------------------------------------------------- host --
+// Boxes of one swizzle row of `rows` rows.  What lies behind the last row or the last element is read as zero.
+inline cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_rows& x, int K, long long n_rows, int rows) {
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const int eb = dtype == GEOCACHE_E4M3 ? 1 : 2;
+    const CUtensorMapDataType type = dtype == GEOCACHE_E4M3   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                     : dtype == GEOCACHE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                              : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)n_rows};
+    const cuuint64_t strides[1] = {n_rows > 1 ? (cuuint64_t)x.stride * eb : ((cuuint64_t)K * eb + 15) / 16 * 16};
+    const cuuint32_t box[2] = {(cuuint32_t)(kRowBytes / eb), (cuuint32_t)rows}, ones[2] = {1, 1};
+    const CUresult r = encode(map, type, 2, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename... Params_, typename... Args>
+cudaError_t launch_cluster(void (*kern)(Params_...), unsigned blocks, int threads, size_t smem, int cluster, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    note_launches(1);
+    return cudaLaunchKernelEx(&cfg, kern, Params_(args)...);
+}
+
+}  // namespace geocache
