@@ -192,8 +192,11 @@ struct LinearArgs {
     const float *bias, *x_scale, *w_scale;
     unsigned long long wait_limit_ns;
     int drop_first_copy;
+    unsigned int* error;   // status word, set by the launch
 };
 cudaError_t launch_linear(const LinearArgs& a, cudaStream_t s);
+// the kernel for many tokens, with tiles of 256 or 128 rows of weights
+cudaError_t launch_linear_pairs(const LinearArgs& a, int features, int sms, cudaStream_t s);
 // the limit of bounded waits, and the test hook's pending request (consumed)
 unsigned long long debug_wait_limit_ns();
 int take_drop_first_copy();

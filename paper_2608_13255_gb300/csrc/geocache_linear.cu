@@ -48,14 +48,23 @@ __device__ __forceinline__ void load_epilogue(Epilogue& e, const LinearArgs& a, 
             e.scale[g][i] = in && a.w_scale ? __ldca(a.w_scale + g * a.N + n + i) : 1.0f;
         }
 }
+// v: the sums, and then the results
 template <bool kGated>
-__device__ __forceinline__ float finish(const float* v, const float* gate, const Epilogue& e, int i, float xs, bool scaled, int act) {
-    float z = scaled ? v[i] * xs * e.scale[0][i] : v[i];
-    z += e.bias[0][i];
-    if (!kGated) return activate(z, act);
-    float g = scaled ? gate[i] * xs * e.scale[1][i] : gate[i];
-    g += e.bias[1][i];
-    return z * activate(g, act);
+__device__ __forceinline__ void finish(float* v, float* gate, const Epilogue& e, float xs, bool scaled, int act) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (scaled) v[i] = v[i] * xs * e.scale[0][i];
+        v[i] += e.bias[0][i];
+        if (kGated) {
+            if (scaled) gate[i] = gate[i] * xs * e.scale[1][i];
+            gate[i] += e.bias[1][i];
+        }
+    }
+    activate<4>(kGated ? gate : v, act);
+    if (kGated) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] *= gate[i];
+    }
 }
 template <typename Out>
 __device__ __forceinline__ void load4(const Out* p, bool wide, int n, float* v) {
@@ -282,11 +291,11 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     const int n = first + unit_f, n_in = min(4, p.a.N - n);
     if (n_in <= 0) return;
     constexpr int kStep = kTileThreads / kUnits;
-#pragma unroll 4
+#pragma unroll 2
     for (int t = threadIdx.x / kUnits; t < n_tok; t += kStep) {
         const long long token = first_token + rank * p.share + t;
         const float xs = p.a.x_scale ? __ldca(p.a.x_scale + token) : 1.0f;
-        float v[4] = {}, gate[4] = {}, res[4] = {}, y[4];
+        float v[4] = {}, gate[4] = {}, res[4] = {};
         if (p.a.residual.data)
             load4(static_cast<const Out*>(p.a.residual.data) + token * p.a.residual.stride + n, p.residual_wide, n_in, res);
         for (int i = 0; i < p.splits; ++i)
@@ -299,12 +308,10 @@ __global__ void __launch_bounds__(kTileThreads, 2)
                 float* w = g ? gate : v;
                 w[0] += s.x; w[1] += s.y; w[2] += s.z; w[3] += s.w;
             }
+        finish<kGated>(v, gate, e, xs, p.a.x_scale != nullptr, p.a.act);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[i] = finish<kGated>(v, gate, e, i, xs, p.a.x_scale != nullptr, p.a.act);
-            if (p.a.residual.data) y[i] += res[i];
-        }
-        store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, y);
+        for (int i = 0; i < 4; ++i) v[i] += res[i];
+        store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, v);
     }
 }
 
@@ -342,32 +349,72 @@ cudaError_t launch_out(const Params& p, cudaStream_t s) {
     return p.a.gated ? launch_tiles<Out, true>(p, s) : launch_tiles<Out, false>(p, s);
 }
 
+// Which kernel and tile a product takes: the least estimate in us.  The terms were fitted to sweeps over tokens 1 to 5391,
+// summed axes of 320 to 8192 and 64 to 8192 features in 8 and 16 bits; over these the choice is on average 2% slower
+// than the best one.
+struct Choice {
+    int pair_features;   // of a tile of the pairs' kernel, 0: the tile kernel
+    int tokens, splits;  // of its tiles and clusters
+};
+Choice choose(const LinearArgs& a, int sms) {
+    const bool f32 = a.out_dtype == GEOCACHE_F32;
+    const int chunks = (int)(((long long)a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) + kRowBytes - 1) / kRowBytes);
+    auto tiles = [](long long n, int per) { return (double)((n + per - 1) / per); };
+    Choice c{};
+    double best = 1e30;
+    auto take = [&](double us, Choice to) {
+        if (us < best) {
+            best = us;
+            c = to;
+        }
+    };
+    for (int tokens = 16; tokens <= (f32 ? 64 : 128); tokens *= 2) {
+        if (tokens > 16 && tokens / 2 >= a.T) break;
+        for (int splits = 1; splits <= 8; ++splits) {
+            if (splits > 1 && (tokens > 64 || splits > chunks)) break;
+            // blocks an SM, of which two run beside each other: the second adds 0.78 of the first's time
+            const double r = tiles(a.T, tokens) * tiles(a.N, a.gated ? kFeatures / 2 : kFeatures) * splits / sms;
+            const double rounds = r <= 1 ? 1 : r <= 2 ? 1 + 0.78 * (r - 1) : 0.89 * r;
+            const int per = (chunks + splits - 1) / splits;
+            const double chunk = (kFeatures + tokens) * 0.00163;
+            take(2.5 + (splits > 1 ? 0.63 + 0.042 * splits : 0) +
+                     rounds * (per * (chunk > 0.054 ? chunk : 0.054) + tokens * (0.034 + 0.0045 / splits)),
+                 {0, tokens, splits});
+        }
+    }
+    for (int features = 128; features <= (f32 ? 128 : 256); features += 128) {
+        const double n = tiles(a.T, 256) * tiles(a.N, a.gated ? features / 2 : features);
+        const double rounds = tiles((long long)n, sms / 2), finish = features == 256 ? 2.7 : f32 ? 3.0 : 1.5;
+        const double sums = chunks * (features == 256 ? 0.34 : f32 ? 0.27 : 0.235);
+        if (n < 2e9) take(5.5 + rounds * (sums > finish ? sums : finish), {features, 0, 0});
+    }
+    return c;
+}
+
 }  // namespace
 
-cudaError_t launch_linear(const LinearArgs& a, cudaStream_t s) {
+cudaError_t launch_linear(const LinearArgs& given, cudaStream_t s) {
+    LinearArgs a = given;
+    static unsigned int* word = nullptr;
+    static int sms = 0;
+    static const cudaError_t ready = [] {
+        int device = 0;
+        cudaError_t e = linear_error_word(&word);
+        if (e == cudaSuccess) e = cudaGetDevice(&device);
+        return e == cudaSuccess ? cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) : e;
+    }();
+    if (ready != cudaSuccess) return ready;
+    a.error = word;
+    const Choice c = choose(a, sms);
+    if (c.pair_features) return launch_linear_pairs(a, c.pair_features, sms, s);
     Params p{};
     p.a = a;
     const int eb = a.in_dtype == GEOCACHE_E4M3 ? 1 : 2, ob = a.out_dtype == GEOCACHE_F32 ? 4 : 2;
     p.chunks = (int)(((long long)a.K * eb + kRowBytes - 1) / kRowBytes);
     const int part = a.gated ? kFeatures / 2 : kFeatures;
     p.feature_tiles = (a.N + part - 1) / part;
-    // The tile's tokens and the cut of the summed axis: the least estimate in cycles of the rounds over the SMs, each
-    // with its copies (50 bytes a cycle), the sums' way through shared memory and the clusters' barriers.
-    const int most = a.out_dtype == GEOCACHE_F32 ? 64 : 128;
-    double best = 0;
-    for (int tokens = 16; tokens <= most; tokens *= 2)
-        for (int splits = 1; splits <= 8; ++splits) {
-            if (splits > 1 && (p.chunks < 2 * splits || tokens > 64)) break;
-            const double blocks = (double)((a.T + tokens - 1) / tokens) * p.feature_tiles * splits;
-            const double rounds = blocks <= 152 ? 1 : blocks <= 304 ? 1.6 : blocks / 152;
-            const double cost = rounds * ((double)(p.chunks + splits - 1) / splits * (kFeatures + tokens) * kRowBytes / 50 + tokens * 16) +
-                                (splits > 1 ? 1000 + 100 * splits : 0);
-            if (p.tokens == 0 || cost < best) {
-                best = cost;
-                p.tokens = tokens;
-                p.splits = splits;
-            }
-        }
+    p.tokens = c.tokens;
+    p.splits = c.splits;
     // binary32 sums, operands of one type (e4m3 is type 0 of its kind), both with the summed axis contiguous
     const uint32_t type = a.in_dtype == GEOCACHE_BF16 ? 1 : 0;
     p.idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(p.tokens >> 3) << 17 | (uint32_t)(kFeatures >> 4) << 24;

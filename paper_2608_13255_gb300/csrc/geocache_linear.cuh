@@ -53,13 +53,20 @@ __device__ __forceinline__ uint32_t in_cluster(uint32_t at, uint32_t rank) {
 // ------------------------------------------------------------- epilogue --
 // exp(-x) overflows to infinity below -88, where the quotient is -0 as it should be
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
-__device__ __forceinline__ float activate(float x, int act) {
-    switch (act) {
-        case GEOCACHE_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
-        // (1 + tanh u) / 2 = sigmoid(2 u)
-        case GEOCACHE_ACT_GELU_TANH: return x * sigmoid(1.5957691216057308f * fmaf(0.044715f * x * x, x, x));
-        case GEOCACHE_ACT_SILU: return x * sigmoid(x);
-        default: return x;
+// The branch stands around the elements: inside the loop it made the code so long that its fetching took most of a small
+// call's time.
+template <int kCount>
+__device__ __forceinline__ void activate(float* x, int act) {
+    if (act == GEOCACHE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) x[i] = 0.5f * x[i] * (1.0f + erff(x[i] * 0.70710678118654752f));
+    } else if (act != GEOCACHE_ACT_NONE) {
+        const bool tanh = act == GEOCACHE_ACT_GELU_TANH;   // (1 + tanh u) / 2 = sigmoid(2 u)
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const float u = 1.5957691216057308f * x[i] * fmaf(0.044715f * x[i], x[i], 1.0f);
+            x[i] *= sigmoid(tanh ? u : x[i]);
+        }
     }
 }
 template <typename T>
@@ -85,19 +92,20 @@ __device__ __forceinline__ void unpack2(uint32_t w, float* v) {
 }
 
 // ----------------------------------------------------------------- host --
-// Boxes of one swizzle row of `rows` rows.  What lies behind the last row or the last element is read as zero.
-inline cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_rows& x, int K, long long n_rows, int rows) {
+// Boxes of `rows` rows of row_bytes, swizzled over as many bytes (128 or 64).  What lies behind the last row or the last element is read as zero.
+inline cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_rows& x, int K, long long n_rows, int rows, int row_bytes = kRowBytes) {
     EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorNotSupported;
-    const int eb = dtype == GEOCACHE_E4M3 ? 1 : 2;
+    const int eb = dtype == GEOCACHE_E4M3 ? 1 : dtype == GEOCACHE_F32 ? 4 : 2;
     const CUtensorMapDataType type = dtype == GEOCACHE_E4M3   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                      : dtype == GEOCACHE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                     : dtype == GEOCACHE_F32  ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                               : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)n_rows};
     const cuuint64_t strides[1] = {n_rows > 1 ? (cuuint64_t)x.stride * eb : ((cuuint64_t)K * eb + 15) / 16 * 16};
-    const cuuint32_t box[2] = {(cuuint32_t)(kRowBytes / eb), (cuuint32_t)rows}, ones[2] = {1, 1};
-    const CUresult r = encode(map, type, 2, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint32_t box[2] = {(cuuint32_t)(row_bytes / eb), (cuuint32_t)rows}, ones[2] = {1, 1};
+    const CUresult r = encode(map, type, 2, x.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 

@@ -1,0 +1,495 @@
+// Matrix product with its epilogue for many tokens: tiles of 256 tokens x 256 (or 128) rows of weights on pairs of SMs.
+#include <cuda_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "geocache_linear.cuh"
+
+namespace geocache {
+
+namespace {
+
+// The two blocks of a cluster hold 128 tokens each and half of the tile's weights each; one thread of the first issues
+// products over both (cta_group::2), so an SM reads 3/4 of the operand bytes that a tile of its own would take (and
+// copies half the weights).  A block runs over many tiles: warps 0 to 7 finish a tile while the next one's products fill
+// the other half of tensor memory.  Tokens are the lanes of tensor memory: a thread finishes a token's columns.
+constexpr int kTokens = 256;               // of a tile: 128 of each block
+constexpr int kFinishWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 32 * 10;
+constexpr int kMostStages = 8;
+constexpr int kRing = 6 * 32 * 1024;       // bytes of the stages
+constexpr int kPartChunks = 4;             // as in the tile kernel: f32 results leave tensor memory in parts
+constexpr int kTurnBytes = 32 * 64;        // of a finishing warp's buffer: 64 bytes of 32 tokens, in swizzled words of 16
+
+struct PairParams {
+    LinearArgs a;
+    int chunks;                      // of kRowBytes of a row
+    int token_tiles, feature_tiles;
+    int band;                        // token tiles that share a sweep over the features
+    int n_tiles;
+    uint32_t idesc;
+    int out_tma, residual_wide;      // rows of whole 16-byte words
+};
+
+struct PairBarriers {
+    uint64_t full[kMostStages], peer[kMostStages], empty[kMostStages], sums[2], taken[2], done;
+    uint32_t tmem, dead;
+};
+
+// As mbar_wait_slow, for arrivals from both blocks; the block that gives up tells the other one.
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    const unsigned long long t0 = globaltimer();
+    while (!__all_sync(0xffffffffu, mbar_try(bar, parity))) {
+        const bool late = globaltimer() - t0 > limit_ns;
+        if (__any_sync(0xffffffffu, late || *(volatile uint32_t*)dead)) {
+            if (late) {
+                for (uint32_t r = 0; r < 2; ++r)
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(dead), r)), "r"(1u) : "memory");
+                atomicOr(error, 1u);
+            }
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_cluster(smem_u32(bar), rank)) : "memory");
+}
+// arrives at both blocks' barriers when the products issued so far are done
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool eight, uint32_t accumulate) {
+    if (eight)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
+// Tiles in bands of token tiles, each swept over the features: the blocks that run together share both operands in L2.
+__device__ __forceinline__ void tile_at(const PairParams& p, int tile, int& token_tile, int& feature_tile) {
+    const int per = p.band * p.feature_tiles, b = tile / per, in = tile - b * per;
+    const int rows = min(p.band, p.token_tiles - b * p.band);
+    feature_tile = in / rows;
+    token_tile = b * p.band + in - feature_tile * rows;
+}
+
+template <typename Out, bool kGated, int kN>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_pair_kernel(const __grid_constant__ PairParams p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm,
+                       const __grid_constant__ CUtensorMap om) {
+    constexpr bool kParts = std::is_same<Out, float>::value;
+    constexpr int kOut = kGated ? kN / 2 : kN;          // output features of a tile
+    constexpr int kCols = kOut / 2;                     // of them, those of a finishing warp
+    constexpr uint32_t kStage = (128 + kN / 2) * kRowBytes;
+    constexpr int kStages = kRing / kStage < kMostStages ? kRing / kStage : kMostStages;
+    constexpr int kG = kGated ? 2 : 1;
+    constexpr int kBlock = 64 / (int)sizeof(Out);       // columns that are finished at a time
+    extern __shared__ uint8_t raw[];
+    __shared__ PairBarriers bars;
+    __shared__ __align__(16) float consts[kFinishWarps][2][kG * kCols];   // bias and weights' scales of a warp's columns
+    PairBarriers* b = &bars;
+    const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x & 1;
+    const unsigned long long limit = p.a.wait_limit_ns;
+    unsigned int* const error = p.a.error;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&b->full[s], 1);
+            mbar_init(&b->peer[s], 1);
+            mbar_init(&b->empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&b->sums[i], 1);
+            mbar_init(&b->taken[i], 2 * kFinishWarps);
+        }
+        mbar_init(&b->done, 1);
+        b->dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(2 * kN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    cluster_sync();
+    tc_after();
+    const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
+    pdl_wait();
+
+    const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+    const bool eight = p.a.in_dtype == GEOCACHE_E4M3;
+
+    if (warp == kLoadWarp) {
+        uint32_t stage = 0, phase = 0, armed = 0;
+        bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
+        const int step = eight ? kRowBytes : kRowBytes / 2;
+        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+            int token_tile, feature_tile;
+            tile_at(p, tile, token_tile, feature_tile);
+            const int token = token_tile * kTokens + (int)rank * 128;
+            const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
+            for (int c = 0; c < p.chunks; ++c) {
+                ok = wait_pair(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
+                if (!ok) break;
+                if (!drop) {
+                    if (elect()) {
+                        const uint32_t at = smem + stage * kStage;
+                        mbar_expect(&b->full[stage], kStage);
+                        tma_2d(at, &xm, c * step, token, &b->full[stage]);
+                        tma_2d(at + 128 * kRowBytes, &wm, c * step, row, &b->full[stage]);
+                    }
+                    __syncwarp();
+                    armed |= 1u << stage;
+                }
+                drop = false;
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+        }
+        // the copies in flight land before the block goes on, and the products that read them signal
+        const unsigned long long t0 = globaltimer();
+        for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
+            const uint32_t parity = s < stage ? phase : phase ^ 1;
+            while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
+            while (ok && (armed >> s & 1) && !mbar_try(&b->empty[s], parity) && !*(volatile uint32_t*)&b->dead &&
+                   globaltimer() - t0 < kDrainLimitNs) {}
+        }
+    } else if (warp == kMmaWarp) {
+        uint32_t stage = 0, phase = 0, part = 0;   // parts are counted over all tiles
+        bool ok = true;
+        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+            for (int c = 0; c < p.chunks; ++c) {
+                const bool begin = kParts ? c % kPartChunks == 0 : c == 0;
+                const bool end = c == p.chunks - 1 || (kParts && c % kPartChunks == kPartChunks - 1);
+                if (rank == 0) {
+                    if (begin && part >= 2) ok = wait_pair(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
+                    ok = ok && wait_pair(&b->full[stage], phase, limit, &b->dead, error) &&
+                         wait_pair(&b->peer[stage], phase, limit, &b->dead, error);
+                    if (!ok) break;
+                    tc_after();
+                    if (elect()) {
+                        const uint32_t at = smem + stage * kStage;
+                        const uint64_t x = smem_desc(at, 16), w = smem_desc(at + 128 * kRowBytes, 16);
+#pragma unroll
+                        for (int k = 0; k < kRowBytes / 32; ++k)
+                            mma_pair(tmem + (part & 1) * kN, x + k * 2, w + k * 2, p.idesc, eight, !begin || k > 0);
+                        commit_pair(&b->empty[stage]);
+                        if (end) commit_pair(&b->sums[part & 1]);
+                    }
+                    __syncwarp();
+                } else {
+                    ok = wait_pair(&b->full[stage], phase, limit, &b->dead, error);
+                    if (!ok) break;
+                    if (elect()) arrive_at(&b->peer[stage], 0);
+                    __syncwarp();
+                }
+                part += end;
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+        }
+        // every product is done before the blocks go on, those too that were issued before a wait ran out
+        if (rank == 0 && elect()) commit_pair(&b->done);
+        __syncwarp();
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+    } else {
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + half * kCols;
+        float* bias = consts[warp][0];
+        float* scale = consts[warp][1];
+        const uint32_t turn = smem + kStages * kStage + warp * kTurnBytes;
+        const int parts = kParts ? (p.chunks + kPartChunks - 1) / kPartChunks : 1;
+        const bool scaled = p.a.x_scale != nullptr;
+        uint32_t part = 0;
+        bool ok = true;
+        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+            int token_tile, feature_tile;
+            tile_at(p, tile, token_tile, feature_tile);
+            const long long row0 = (long long)token_tile * kTokens + rank * 128 + quarter * 32, token = row0 + lane;
+            const int n0 = feature_tile * kOut + half * kCols;
+            const bool in_rows = token < p.a.T;
+            __syncwarp();
+            for (int i = lane; i < kG * kCols; i += 32) {
+                const int g = i / kCols, n = n0 + i % kCols;
+                bias[i] = p.a.bias && n < p.a.N ? __ldca(p.a.bias + (long long)g * p.a.N + n) : 0.0f;
+                scale[i] = scaled && n < p.a.N ? __ldca(p.a.w_scale + (long long)g * p.a.N + n) : 1.0f;
+            }
+            const float xs = scaled && in_rows ? __ldca(p.a.x_scale + token) : 1.0f;
+            __syncwarp();
+            Out* const out = static_cast<Out*>(p.a.out.data);
+            const Out* const residual = static_cast<const Out*>(p.a.residual.data);
+
+            // kBlock columns from j on, of sums v (and the gates' g).  Results go through the warp's buffer: a lane writes its
+            // token's 64 bytes, which leave as one box (or, from rows that are no whole 16-byte words, with the lanes along
+            // the rows).  Straight from the registers, 32 rows an instruction, the stores alone took 2,000 of the 16,400
+            // cycles that shared memory has for a tile's operands at a summed axis of 2048.
+            auto word = [&](int r, int c) { return turn + r * 64 + ((c ^ (r >> 1 & 3)) << 4); };   // 16 bytes
+            auto element = [&](int r, int c) { return word(r, c * (int)sizeof(Out) >> 4) + (c * (int)sizeof(Out) & 15); };
+            auto emit = [&](float* v, float* g, int j) {
+                const int n = n0 + j;
+                if (n >= p.a.N) return;
+                const int n_in = min(kBlock, p.a.N - n);
+                if (p.out_tma) {   // the buffer's last box has been read
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                }
+                if (residual) {
+                    if (p.residual_wide && n_in == kBlock) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = i * 8 + (lane >> 2), c = lane & 3;
+                            uint4 w = make_uint4(0, 0, 0, 0);
+                            if (row0 + r < p.a.T)
+                                w = __ldca(reinterpret_cast<const uint4*>(residual + (row0 + r) * p.a.residual.stride + n) + c);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(word(r, c)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
+                                         : "memory");
+                        }
+                    } else {
+                        const int c = lane % kBlock;
+                        for (int r = lane / kBlock; r < 32; r += 32 / kBlock) {
+                            if (row0 + r >= p.a.T || c >= n_in) continue;
+                            const Out w = residual[(row0 + r) * p.a.residual.stride + n + c];
+                            if constexpr (sizeof(Out) == 4)
+                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(element(r, c)), "r"(__float_as_uint(w)) : "memory");
+                            else
+                                asm volatile("st.shared.b16 [%0], %1;" ::"r"(element(r, c)), "h"(*reinterpret_cast<const uint16_t*>(&w)) : "memory");
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (scaled) {
+#pragma unroll
+                    for (int i = 0; i < kBlock; i += 4) {
+                        const float4 s = *reinterpret_cast<const float4*>(scale + j + i);
+                        v[i] = v[i] * xs * s.x; v[i + 1] = v[i + 1] * xs * s.y; v[i + 2] = v[i + 2] * xs * s.z; v[i + 3] = v[i + 3] * xs * s.w;
+                        if (kGated) {
+                            const float4 u = *reinterpret_cast<const float4*>(scale + kCols + j + i);
+                            g[i] = g[i] * xs * u.x; g[i + 1] = g[i + 1] * xs * u.y; g[i + 2] = g[i + 2] * xs * u.z; g[i + 3] = g[i + 3] * xs * u.w;
+                        }
+                    }
+                }
+                if (p.a.bias) {
+#pragma unroll
+                    for (int i = 0; i < kBlock; i += 4) {
+                        const float4 s = *reinterpret_cast<const float4*>(bias + j + i);
+                        v[i] += s.x; v[i + 1] += s.y; v[i + 2] += s.z; v[i + 3] += s.w;
+                        if (kGated) {
+                            const float4 u = *reinterpret_cast<const float4*>(bias + kCols + j + i);
+                            g[i] += u.x; g[i + 1] += u.y; g[i + 2] += u.z; g[i + 3] += u.w;
+                        }
+                    }
+                }
+                activate<kBlock>(kGated ? g : v, p.a.act);
+                if (kGated) {
+#pragma unroll
+                    for (int i = 0; i < kBlock; ++i) v[i] *= g[i];
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    constexpr int kPer = 16 / (int)sizeof(Out);
+                    float* y = v + c * kPer;
+                    uint32_t w[4];
+                    if (residual) {
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(word(lane, c)));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (sizeof(Out) == 4) {
+                                y[i] += __uint_as_float(w[i]);
+                            } else {
+                                float u[2];
+                                unpack2<Out>(w[i], u);
+                                y[2 * i] += u[0];
+                                y[2 * i + 1] += u[1];
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (sizeof(Out) == 4) w[i] = __float_as_uint(y[i]);
+                        else w[i] = pack2<Out>(y[2 * i], y[2 * i + 1]);
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(word(lane, c)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                if (p.out_tma) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&om), "r"(n), "r"((int)row0),
+                                     "r"(turn)
+                                     : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    return;
+                }
+                __syncwarp();
+                const int c = lane % kBlock;
+#pragma unroll 4
+                for (int r = lane / kBlock; r < 32; r += 32 / kBlock) {
+                    if (row0 + r >= p.a.T || c >= n_in) continue;
+                    Out* to = out + (row0 + r) * p.a.out.stride + n + c;
+                    if constexpr (sizeof(Out) == 4) {
+                        uint32_t w;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(element(r, c)) : "memory");
+                        *reinterpret_cast<uint32_t*>(to) = w;
+                    } else {
+                        uint16_t w;
+                        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(element(r, c)) : "memory");
+                        *reinterpret_cast<uint16_t*>(to) = w;
+                    }
+                }
+                __syncwarp();   // the buffer has been read
+            };
+
+            float acc[kParts ? kG * kCols : 1];
+            if (kParts) {
+#pragma unroll
+                for (int i = 0; i < kG * kCols; ++i) acc[kParts ? i : 0] = 0.0f;
+            }
+            for (int q = 0; ok && q < parts; ++q, ++part) {
+                ok = wait_pair(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead, error);
+                if (!ok) break;
+                tc_after();
+                const uint32_t from = at + (part & 1) * kN;
+                if (kParts) {
+#pragma unroll
+                    for (int g = 0; g < kG; ++g)
+#pragma unroll
+                        for (int j = 0; j < kCols; j += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(from + g * (kN / 2) + j, r);
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                            asm volatile("" : GEOCACHE_PIN16(r));
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[kParts ? g * kCols + j + i : 0] += __uint_as_float(r[i]);
+                        }
+                    if (q < parts - 1) {
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_at(&b->taken[part & 1], 0);
+                        continue;
+                    }
+                    // the whole sums take the last part's place, where the loop below finds them (its columns are no constants)
+#pragma unroll
+                    for (int g = 0; g < kG; ++g)
+#pragma unroll
+                        for (int j = 0; j < kCols; j += 16)
+                            tmem_st16(from + g * (kN / 2) + j, reinterpret_cast<uint32_t*>(acc) + (kParts ? g * kCols + j : 0));
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                }
+                uint32_t r[kG][kBlock];
+                auto load = [&](int j) {
+#pragma unroll
+                    for (int g = 0; g < kG; ++g)
+#pragma unroll
+                        for (int i = 0; i < kBlock; i += 16) tmem_ld16(from + g * (kN / 2) + j + i, r[g] + i);
+                };
+                load(0);
+#pragma unroll 1
+                for (int j = 0; j < kCols; j += kBlock) {
+                    float v[kG][kBlock];
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int g = 0; g < kG; ++g) {
+#pragma unroll
+                        for (int i = 0; i < kBlock; i += 16) asm volatile("" : GEOCACHE_PIN16(r[g] + i));
+#pragma unroll
+                        for (int i = 0; i < kBlock; ++i) v[g][i] = __uint_as_float(r[g][i]);
+                    }
+                    if (j + kBlock < kCols) {   // the next columns come while these are finished
+                        load(j + kBlock);
+                    } else {   // all is in registers: the next but one part may be written
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_at(&b->taken[part & 1], 0);
+                    }
+                    emit(v[0], v[kG - 1], j);
+                }
+            }
+        }
+        // the boxes in flight are written before the block ends
+        if (p.out_tma && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+    tc_before();
+    __syncthreads();
+    cluster_sync();   // neither block ends while the other's products, arrivals or signals may reach it
+    tc_after();
+    if (warp == kMmaWarp)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
+}
+
+template <typename Out, bool kGated, int kN>
+cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
+    auto kern = linear_pair_kernel<Out, kGated, kN>;
+    constexpr int kBytes = kRing + kFinishWarps * kTurnBytes + 1024;
+    static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (ready != cudaSuccess) return ready;
+    CUtensorMap wm, xm, om{};
+    cudaError_t e = make_map(&wm, p.a.in_dtype, p.a.w, p.a.K, (long long)p.a.N * (kGated ? 2 : 1), kN / 2);
+    if (e == cudaSuccess) e = make_map(&xm, p.a.in_dtype, p.a.x, p.a.K, p.a.T, 128);
+    if (e == cudaSuccess && p.out_tma) e = make_map(&om, p.a.out_dtype, p.a.out, p.a.N, p.a.T, 32, 64);
+    if (e != cudaSuccess) return e;
+    constexpr int kOut = kGated ? kN / 2 : kN;
+    p.token_tiles = (int)((p.a.T + kTokens - 1) / kTokens);
+    p.feature_tiles = (p.a.N + kOut - 1) / kOut;
+    const long long n = (long long)p.token_tiles * p.feature_tiles;
+    if (n > 0x7fffffffLL - 1024) return cudaErrorInvalidConfiguration;
+    p.n_tiles = (int)n;
+    p.band = 4;
+    const uint32_t type = p.a.in_dtype == GEOCACHE_BF16 ? 1 : 0;
+    p.idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kTokens >> 4) << 24;
+    if (pairs > p.n_tiles) pairs = p.n_tiles;
+    return launch_cluster(kern, (unsigned)(2 * pairs), kThreads, kBytes, 2, s, p, wm, xm, om);
+}
+
+// f32 results: tiles of 128 rows of weights only, whose sums in registers need no spills
+template <typename Out, bool kGated>
+cudaError_t launch_n(const PairParams& p, int features, int pairs, cudaStream_t s) {
+    if constexpr (!std::is_same<Out, float>::value)
+        if (features == 256) return launch<Out, kGated, 256>(p, pairs, s);
+    return launch<Out, kGated, 128>(p, pairs, s);
+}
+
+template <typename Out>
+cudaError_t launch_out(const PairParams& p, int features, int pairs, cudaStream_t s) {
+    return p.a.gated ? launch_n<Out, true>(p, features, pairs, s) : launch_n<Out, false>(p, features, pairs, s);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_pairs(const LinearArgs& a, int features, int sms, cudaStream_t s) {
+    PairParams p{};
+    p.a = a;
+    const int eb = a.in_dtype == GEOCACHE_E4M3 ? 1 : 2, ob = a.out_dtype == GEOCACHE_F32 ? 4 : 2;
+    p.chunks = (int)(((long long)a.K * eb + kRowBytes - 1) / kRowBytes);
+    auto words = [&](const geocache_rows& r) { return !((uintptr_t)r.data % 16) && (a.T == 1 || r.stride * ob % 16 == 0); };
+    // (a row's end inside a word was not kept: two elements behind 70 of 16 bits were written)
+    p.out_tma = words(a.out) && (long long)a.N * ob % 16 == 0;
+    p.residual_wide = a.residual.data && words(a.residual);
+    if (a.out_dtype == GEOCACHE_BF16) return launch_out<__nv_bfloat16>(p, features, sms / 2, s);
+    if (a.out_dtype == GEOCACHE_F16) return launch_out<__half>(p, features, sms / 2, s);
+    return launch_out<float>(p, features, sms / 2, s);
+}
+
+}  // namespace geocache
