@@ -101,7 +101,7 @@ __device__ __forceinline__ void store4(Out* p, bool wide, int n, const float* v)
 // the blocks of a cluster.  The blocks' sums meet in shared memory: each sends every other one the sums of the tokens
 // that the other finishes, which adds them in the order of the blocks (no atomics: every call gives the same bits).
 // kParts: f32 results, whose sums leave tensor memory every kPartChunks chunks and are added up in registers, rounded to
-// nearest; the tensor cores' own additions cut off (a chain of 128 was 2.1e-6 from the definition, with parts 4e-7).
+// nearest; the tensor cores' own additions cut off (a chain of 128 was 2.1e-6 from the definition, with parts 2.4e-7).
 constexpr int kTileWarps = 8, kTileThreads = 32 * kTileWarps, kTileLoadWarp = 4, kTileMmaWarp = 5;
 constexpr int kTileStages = 12;
 constexpr int kPartChunks = 4;

@@ -4,6 +4,9 @@
 //     y = h w r,  scale = max(max |y| / 448, 2^-126),  q = e4m3(y / scale).
 // One pass: a row stays in the registers of the threads that read it, and its two statistics, sum h^2 and max |h w|, are
 // taken in one round: max |y| = r max |h w|, since r does not depend on the element.  Sums are binary32.
+//
+// Bound by memory on paper (bf16 with residual into 8 bits: 7 bytes and some 10 instructions an element), and by the
+// instructions in a first form with 40 an element (95 us for 24576 rows of 2048 in bf16 with residual into 8 bits).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -22,208 +25,322 @@ namespace {
 constexpr int kThreads = 256;   // of a block, or as many as a wide row takes
 constexpr float kLargest = 448.0f, kTiny = 0x1p-126f;  // of e4m3; the least scale (the least normal number)
 
-__device__ __forceinline__ void unpack2(uint32_t w, float* v, __nv_bfloat16) {
-    v[0] = __uint_as_float(w << 16);
-    v[1] = __uint_as_float(w & 0xffff0000u);
+// ------------------------------------------------------- pairs of floats --
+__device__ __forceinline__ uint64_t bits(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
+__device__ __forceinline__ float2 floats(uint64_t b) { return make_float2(__uint_as_float((uint32_t)b), __uint_as_float((uint32_t)(b >> 32))); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+    return floats(d);
 }
-__device__ __forceinline__ void unpack2(uint32_t w, float* v, __half) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    v[0] = f.x;
-    v[1] = f.y;
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+    return floats(d);
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return floats(d);
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+// the larger of a and |b|; a NaN stays
+__device__ __forceinline__ float max_abs(float a, float b) {
+    float d;
+    asm("{\n .reg .f32 t;\n abs.f32 t, %2;\n max.NaN.f32 %0, %1, t;\n}\n" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 template <typename T>
-__device__ __forceinline__ T rounded(float x) {
-    if constexpr (std::is_same<T, float>::value) return x;
-    else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
-    else return __float2bfloat16_rn(x);
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+    if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-
-// 8 elements of a row, n of them inside it (the others are zero)
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool aligned, float* v) {
-    if (aligned && n == 8) {
-        if constexpr (std::is_same<T, float>::value) {
-            const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-            unpack2(w.x, v, T());
-            unpack2(w.y, v + 2, T());
-            unpack2(w.z, v + 4, T());
-            unpack2(w.w, v + 6, T());
-        }
+__device__ __forceinline__ uint32_t pack2(float2 v) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(v.x, v.y);
+        return *reinterpret_cast<const uint32_t*>(&h);
     } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < n ? to_float(p[e]) : 0.0f;
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+        return *reinterpret_cast<const uint32_t*>(&h);
     }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, bool aligned, const float* v) {
-    if (aligned && n == 8) {
-        if constexpr (std::is_same<T, float>::value) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            *reinterpret_cast<uint4*>(p) =
-                make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = rounded<T>(v[e]);
-    }
-}
-// two floats as e4m3, `lo` in the low byte, values over 448 as 448
-__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// four floats as e4m3, values over 448 as 448
+__device__ __forceinline__ uint32_t pack_e4m3(float2 a, float2 b) {
+    uint32_t r;
+    asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n mov.b32 %0, {l, h};\n}\n"
+        : "=r"(r)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
 
-// The rows of a block: `lanes` threads (a power of two) each, kWords words of 8 elements a thread, the words of a row
-// side by side over its threads.
-template <typename X, bool kNorm, bool kQuant, int kWords>
-__global__ void __launch_bounds__(1024) norm_rows_kernel(const __grid_constant__ NormRowsArgs a) {
-    __shared__ float2 shared[32];
-    const int lane = threadIdx.x & (a.lanes - 1), row_in = threadIdx.x / a.lanes;
-    const long long row = (long long)blockIdx.x * (blockDim.x / a.lanes) + row_in;
-    const bool active = row < a.T;
-    pdl_wait();
-    float v[kWords][8];
-    const X* x = static_cast<const X*>(a.x.data) + row * a.x.stride;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        const int at = 8 * (lane + i * a.lanes), n = active ? min(8, a.C - at) : 0;
-        load8(x + at, n, a.x_aligned, v[i]);
-    }
-    if (kNorm && a.residual.data) {
-        float r[kWords][8];
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const int at = 8 * (lane + i * a.lanes), n = active ? min(8, a.C - at) : 0;
-            if (std::is_same<X, float>::value || a.residual_f32)
-                load8(static_cast<const float*>(a.residual.data) + row * a.residual.stride + at, n, a.residual_aligned, r[i]);
-            else
-                load8(static_cast<const X*>(a.residual.data) + row * a.residual.stride + at, n, a.residual_aligned, r[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const int at = 8 * (lane + i * a.lanes), n = active ? min(8, a.C - at) : 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[i][e] += r[i][e];
-                if (!a.residual_f32) v[i][e] = to_float(rounded<X>(v[i][e]));
-            }
-            if (std::is_same<X, float>::value || a.residual_f32)
-                store8(static_cast<float*>(a.residual_out.data) + row * a.residual_out.stride + at, n, a.residual_aligned, v[i]);
-            else
-                store8(static_cast<X*>(a.residual_out.data) + row * a.residual_out.stride + at, n, a.residual_aligned, v[i]);
-        }
-    }
-    // sum h^2, and the bits of max |h w| (as whole numbers: a NaN is above all others)
-    float sum = 0.0f;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        const int at = 8 * (lane + i * a.lanes), n = active ? min(8, a.C - at) : 0;
-        if (kNorm) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(v[i][e], v[i][e], sum);
-            if (a.weight) {
-                float w[8];
-                if (n == 8 && a.weight_aligned) {
-                    const float4 p = __ldca(reinterpret_cast<const float4*>(a.weight + at)), q = __ldca(reinterpret_cast<const float4*>(a.weight + at) + 1);
-                    w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
-                    w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = e < n ? __ldca(a.weight + at + e) : 0.0f;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
+// ----------------------------------------------------------------- words --
+// 8 elements of a row as they lie in memory
+template <typename T>
+struct Raw {
+    uint32_t w[2 * sizeof(T)];
+};
+enum { kElements, kWords16, kWords32 };   // rows of whole words of that many bytes
+// n of them inside the row (the others are zero)
+template <typename T>
+__device__ __forceinline__ void load8(Raw<T>& r, const T* p, int n, int words) {
+    if (words && n == 8) {
+        if constexpr (sizeof(T) == 4) {
+            if (words == kWords32) {
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+                             : "l"(p)
+                             : "memory");
+                return;
             }
         }
-        if (kQuant) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+            r.w[4 * i] = w.x; r.w[4 * i + 1] = w.y; r.w[4 * i + 2] = w.z; r.w[4 * i + 3] = w.w;
         }
-    }
-    for (int d = min(16, a.lanes / 2); d > 0; d >>= 1) {
-        if (kNorm) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (kQuant) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-    }
-    if (a.lanes > 32) {
-        const int warps = a.lanes / 32, warp = threadIdx.x / 32, first = row_in * warps;
-        if ((threadIdx.x & 31) == 0) shared[warp] = make_float2(sum, __uint_as_float(top));
-        __syncthreads();
-        sum = 0.0f;
-        top = 0;
-        for (int i = 0; i < warps; ++i) {  // in one order for all threads of the row
-            const float2 s = shared[first + i];
-            sum += s.x;
-            top = max(top, __float_as_uint(s.y));
-        }
-    }
-    if (!active) return;
-    const float f = kNorm ? rsqrtf(sum / (float)a.C + a.eps) : 1.0f;
-    float inv = 1.0f;
-    if (kQuant) {
-        const float most = __uint_as_float(top) * f, s = most / kLargest;
-        const float scale = s < kTiny ? kTiny : s;  // (a NaN stays)
-        if (lane == 0) a.scale[row] = scale;
-        inv = 1.0f / scale;  // (times f only after the element: both may be large where a row is nearly zero)
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        const int at = 8 * (lane + i * a.lanes), n = min(8, a.C - at);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (kNorm) v[i][e] *= f;
-            if (kQuant) v[i][e] *= inv;
-        }
-        if constexpr (kQuant) {
-            uint8_t* out = static_cast<uint8_t*>(a.out.data) + row * a.out.stride + at;
-            const uint32_t lo = pack_e4m3(v[i][0], v[i][1]) | pack_e4m3(v[i][2], v[i][3]) << 16;
-            const uint32_t hi = pack_e4m3(v[i][4], v[i][5]) | pack_e4m3(v[i][6], v[i][7]) << 16;
-            if (n == 8 && a.out_aligned) {
-                *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+            if constexpr (sizeof(T) == 4) {
+                r.w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0;
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < n) out[e] = (uint8_t)((e < 4 ? lo : hi) >> 8 * (e & 3));
+                const uint32_t lo = 2 * i < n ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0;
+                const uint32_t hi = 2 * i + 1 < n ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0;
+                r.w[i] = lo | hi << 16;
             }
-        } else {
-            store8(static_cast<X*>(a.out.data) + row * a.out.stride + at, n, a.out_aligned, v[i]);
         }
     }
 }
-
-template <typename X, bool kNorm, bool kQuant>
-cudaError_t launch_words(const NormRowsArgs& a, int words, int threads, unsigned blocks, cudaStream_t s) {
-    switch (words) {
-        case 1: return launch_pdl(norm_rows_kernel<X, kNorm, kQuant, 1>, dim3(blocks), threads, 0, s, a);
-        case 2: return launch_pdl(norm_rows_kernel<X, kNorm, kQuant, 2>, dim3(blocks), threads, 0, s, a);
-        case 4: return launch_pdl(norm_rows_kernel<X, kNorm, kQuant, 4>, dim3(blocks), threads, 0, s, a);
-        default: return launch_pdl(norm_rows_kernel<X, kNorm, kQuant, 8>, dim3(blocks), threads, 0, s, a);
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, int words, const Raw<T>& r) {
+    if (words && n == 8) {
+        if constexpr (sizeof(T) == 4) {
+            if (words == kWords32) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]),
+                             "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7])
+                             : "memory");
+                return;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+            if constexpr (sizeof(T) == 4) {
+                if (i < n) reinterpret_cast<uint32_t*>(p)[i] = r.w[i];
+            } else {
+                if (2 * i < n) reinterpret_cast<uint16_t*>(p)[2 * i] = (uint16_t)r.w[i];
+                if (2 * i + 1 < n) reinterpret_cast<uint16_t*>(p)[2 * i + 1] = (uint16_t)(r.w[i] >> 16);
+            }
+        }
     }
+}
+template <typename T>
+__device__ __forceinline__ float2 pair(const Raw<T>& r, int i) {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+    else return unpack2<T>(r.w[i]);
+}
+template <typename T>
+__device__ __forceinline__ void set_pair(Raw<T>& r, int i, float2 v) {
+    if constexpr (sizeof(T) == 4) {
+        r.w[2 * i] = __float_as_uint(v.x);
+        r.w[2 * i + 1] = __float_as_uint(v.y);
+    } else {
+        r.w[i] = pack2<T>(v);
+    }
+}
+
+// ------------------------------------------------------------------ rows --
+// A row has `lanes` threads (a power of two) and kPieces pieces of 8 elements a thread, its pieces side by side over its
+// threads; a block has threads / lanes rows at a time, and stays.  Up to two pieces, a thread asks for those of its next
+// row before it finishes this one.
+enum { kNone, kSame, kF32 };
+constexpr int most_threads(int pieces) { return pieces == 8 ? 1024 : 512; }
+
+template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
+__global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const __grid_constant__ NormRowsArgs a) {
+    using R = typename std::conditional<kResidual == kF32, float, X>::type;
+    constexpr bool kAhead = kPieces <= 2;
+    constexpr int kRes = kResidual == kNone ? 1 : kPieces;
+    __shared__ float2 shared[2][32];
+    const int lane = threadIdx.x & (a.lanes - 1), row_in = threadIdx.x / a.lanes, rows = blockDim.x / a.lanes;
+    const long long step = (long long)gridDim.x * rows;
+    long long row = (long long)blockIdx.x * rows + row_in;
+    int n_of[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) n_of[i] = min(8, max(0, a.C - 8 * (lane + i * a.lanes)));
+    const X* from = static_cast<const X*>(a.x.data) + row * a.x.stride + 8 * lane;
+    const R* from_res = static_cast<const R*>(a.residual.data) + row * a.residual.stride + 8 * lane;
+    R* to_res = static_cast<R*>(a.residual_out.data) + row * a.residual_out.stride + 8 * lane;
+    X* to = static_cast<X*>(a.out.data) + row * a.out.stride + 8 * lane;
+    uint8_t* to_q = static_cast<uint8_t*>(a.out.data) + row * a.out.stride + 8 * lane;
+    const int apart = 8 * a.lanes;   // from one piece of a thread to its next
+    Raw<X> x[kPieces];
+    Raw<R> res[kRes];
+    auto load = [&](bool inside) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int n = inside ? n_of[i] : 0;
+            load8(x[i], from + i * apart, n, a.x_words);
+            if constexpr (kResidual != kNone) load8(res[i], from_res + i * apart, n, a.residual_words);
+        }
+        from += step * a.x.stride;
+        if (kResidual != kNone) from_res += step * a.residual.stride;
+    };
+    pdl_wait();
+    if (kAhead) load(row < a.T);
+    for (int turn = 0; row - row_in < a.T; row += step, turn ^= 1) {
+        const bool active = row < a.T;
+        if (!kAhead) load(active);
+        float2 v[kPieces][4];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[i][e] = pair(x[i], e);
+                if constexpr (kResidual != kNone) {
+                    set_pair(res[i], e, add2(v[i][e], pair(res[i], e)));
+                    v[i][e] = pair(res[i], e);   // (what is stored)
+                }
+            }
+            if constexpr (kResidual != kNone) {
+                if (active) store8(to_res + i * apart, n_of[i], a.residual_words, res[i]);
+            }
+        }
+        if (kAhead) load(row + step < a.T);
+        float2 sums = make_float2(0.0f, 0.0f);
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            if (kNorm) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums = fma2(v[i][e], v[i][e], sums);
+                if (a.weight) {
+                    const float* at = a.weight + 8 * lane + i * apart;
+                    if (n_of[i] == 8 && a.weight_words) {
+                        const float4 p = __ldca(reinterpret_cast<const float4*>(at)), q = __ldca(reinterpret_cast<const float4*>(at) + 1);
+                        v[i][0] = mul2(v[i][0], make_float2(p.x, p.y));
+                        v[i][1] = mul2(v[i][1], make_float2(p.z, p.w));
+                        v[i][2] = mul2(v[i][2], make_float2(q.x, q.y));
+                        v[i][3] = mul2(v[i][3], make_float2(q.z, q.w));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (2 * e < n_of[i]) v[i][e].x *= __ldca(at + 2 * e);
+                            if (2 * e + 1 < n_of[i]) v[i][e].y *= __ldca(at + 2 * e + 1);
+                        }
+                    }
+                }
+            }
+            if (kQuant) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = max_abs(max_abs(top, v[i][e].x), v[i][e].y);
+            }
+        }
+        float sum = sums.x + sums.y;
+        auto join = [&](int from) {
+            for (int d = from; d > 0; d >>= 1) {
+                if (kNorm) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if (kQuant) top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, d));
+            }
+        };
+        join(min(16, a.lanes / 2));
+        if (a.lanes > 32) {
+            const int warps = a.lanes / 32, warp = threadIdx.x / 32;   // (a power of two)
+            if ((threadIdx.x & 31) == 0) shared[turn][warp] = make_float2(sum, top);
+            __syncthreads();   // (once a row: the row after next finds this half read)
+            const float2 s = shared[turn][row_in * warps + (threadIdx.x & (warps - 1))];
+            sum = s.x;
+            top = s.y;
+            join(warps / 2);   // in one order for all threads of the row
+        }
+        const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
+        float g = f;   // what an element is multiplied by
+        if (kQuant) {
+            const float s = top * f * (1.0f / kLargest);
+            const float scale = s < kTiny ? kTiny : s;  // (a NaN stays)
+            if (lane == 0 && active) a.scale[row] = scale;
+            const float inv = __fdividef(1.0f, scale);  // (scale < 2^126)
+            g = f * inv;
+            if (kNorm && isinf(g)) {   // a row that is nearly zero
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], make_float2(f, f));
+                g = inv;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], make_float2(g, g));
+            const int n = active ? n_of[i] : 0;
+            if constexpr (kQuant) {
+                const uint32_t lo = pack_e4m3(v[i][0], v[i][1]), hi = pack_e4m3(v[i][2], v[i][3]);
+                if (n == 8 && a.out_words) {
+                    *reinterpret_cast<uint2*>(to_q + i * apart) = make_uint2(lo, hi);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < n) to_q[i * apart + e] = (uint8_t)((e < 4 ? lo : hi) >> 8 * (e & 3));
+                }
+            } else {
+                Raw<X> y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) set_pair(y, e, v[i][e]);
+                if (n) store8(to + i * apart, n, a.out_words, y);
+            }
+        }
+        to += step * a.out.stride;
+        to_q += step * a.out.stride;
+        to_res += step * a.residual_out.stride;
+    }
+}
+
+template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
+cudaError_t launch(const NormRowsArgs& a, int threads, cudaStream_t s) {
+    auto kern = norm_rows_kernel<X, kResidual, kNorm, kQuant, kPieces>;
+    static int resident[3];   // blocks of 256, 512 and 1024 threads that the device holds
+    static const cudaError_t ready = [&] {
+        int device = 0, sms = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+        for (int i = 0; i < 3 && e == cudaSuccess && kThreads << i <= most_threads(kPieces); ++i) {
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[i], kern, kThreads << i, 0);
+            resident[i] *= sms;
+        }
+        return e;
+    }();
+    if (ready != cudaSuccess) return ready;
+    const long long rows = threads / a.lanes, blocks = (a.T + rows - 1) / rows, most = resident[threads / kThreads / 2];
+    return launch_pdl(kern, dim3((unsigned)(blocks < most ? blocks : most)), threads, 0, s, a);
+}
+
+template <typename X, int kResidual, bool kNorm, bool kQuant>
+cudaError_t launch_pieces(const NormRowsArgs& a, int pieces, int threads, cudaStream_t s) {
+    switch (pieces) {
+        case 1: return launch<X, kResidual, kNorm, kQuant, 1>(a, threads, s);
+        case 2: return launch<X, kResidual, kNorm, kQuant, 2>(a, threads, s);
+        case 4: return launch<X, kResidual, kNorm, kQuant, 4>(a, threads, s);
+        default: return launch<X, kResidual, kNorm, kQuant, 8>(a, threads, s);
+    }
+}
+
+template <typename X, int kResidual>
+cudaError_t launch_norm(const NormRowsArgs& a, int pieces, int threads, cudaStream_t s) {
+    return a.scale ? launch_pieces<X, kResidual, true, true>(a, pieces, threads, s)
+                   : launch_pieces<X, kResidual, true, false>(a, pieces, threads, s);
 }
 
 template <typename X>
-cudaError_t launch_type(const NormRowsArgs& a, int words, int threads, unsigned blocks, cudaStream_t s) {
-    if (!a.norm) return launch_words<X, false, true>(a, words, threads, blocks, s);
-    return a.scale ? launch_words<X, true, true>(a, words, threads, blocks, s) : launch_words<X, true, false>(a, words, threads, blocks, s);
+cudaError_t launch_type(const NormRowsArgs& a, int pieces, int threads, cudaStream_t s) {
+    if (!a.norm) return launch_pieces<X, kNone, false, true>(a, pieces, threads, s);
+    if (!a.residual.data) return launch_norm<X, kNone>(a, pieces, threads, s);
+    if constexpr (!std::is_same<X, float>::value)
+        if (a.residual_f32) return launch_norm<X, kF32>(a, pieces, threads, s);
+    return launch_norm<X, kSame>(a, pieces, threads, s);
 }
 
 }  // namespace
@@ -231,27 +348,31 @@ cudaError_t launch_type(const NormRowsArgs& a, int words, int threads, unsigned 
 cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
     NormRowsArgs a = given;
     if (a.T == 0 || a.C == 0) return cudaSuccess;
-    const int eb = a.dtype == GEOCACHE_F32 ? 4 : 2, rb = a.residual_f32 ? 4 : eb, ob = a.scale ? 1 : eb;
-    auto aligned = [](const geocache_rows& r, int size, int bytes) {
-        return !((uintptr_t)r.data % bytes) && !(r.stride * size % bytes);
+    const int eb = a.dtype == GEOCACHE_F32 ? 4 : 2, rb = a.residual_f32 ? 4 : eb;
+    auto words = [](const geocache_rows& r, int size) {
+        const uintptr_t at = (uintptr_t)r.data | (uintptr_t)(r.stride * size);
+        return size == 1 ? at % 8 ? kElements : kWords16 : at % 16 ? kElements : at % 32 ? kWords16 : kWords32;
     };
-    a.x_aligned = aligned(a.x, eb, 16);
-    a.residual_aligned = a.residual.data && aligned(a.residual, rb, 16) && aligned(a.residual_out, rb, 16);
-    a.out_aligned = aligned(a.out, ob, 8 * ob < 16 ? 8 : 16);
-    a.weight_aligned = !((uintptr_t)a.weight % 16);
-    const int pieces = (a.C + 7) / 8;
-    int words = 1, lanes = 1;
-    while (lanes < 32 && lanes < pieces) lanes *= 2;
-    while (lanes * words < pieces) {
-        if (words < 2 || lanes == 1024) words *= 2;
+    a.x_words = words(a.x, eb);
+    if (a.residual.data) {
+        const int in = words(a.residual, rb), out = words(a.residual_out, rb);
+        a.residual_words = in < out ? in : out;
+    }
+    a.out_words = words(a.out, a.scale ? 1 : eb);   // (8-bit rows: whole words of 8)
+    a.weight_words = !((uintptr_t)a.weight % 16);
+    a.inv_C = 1.0f / (float)a.C;
+    const int n = (a.C + 7) / 8;
+    int pieces = 1, lanes = 1;
+    while (lanes < 32 && lanes < n) lanes *= 2;
+    while (lanes * pieces < n) {
+        if (pieces < 2 || lanes == most_threads(pieces)) pieces *= 2;
         else lanes *= 2;
     }
     a.lanes = lanes;
     const int threads = lanes > kThreads ? lanes : kThreads;
-    const long long rows = threads / lanes, blocks = (a.T + rows - 1) / rows;
-    if (a.dtype == GEOCACHE_BF16) return launch_type<__nv_bfloat16>(a, words, threads, (unsigned)blocks, s);
-    if (a.dtype == GEOCACHE_F16) return launch_type<__half>(a, words, threads, (unsigned)blocks, s);
-    return launch_type<float>(a, words, threads, (unsigned)blocks, s);
+    if (a.dtype == GEOCACHE_BF16) return launch_type<__nv_bfloat16>(a, pieces, threads, s);
+    if (a.dtype == GEOCACHE_F16) return launch_type<__half>(a, pieces, threads, s);
+    return launch_type<float>(a, pieces, threads, s);
 }
 
 }  // namespace geocache
