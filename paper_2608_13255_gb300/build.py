@@ -2,7 +2,9 @@
 
 The library is compiled from ``csrc/*.cu`` with one ``-gencode`` for sm_103a,
 each translation unit in parallel, and linked with the static CUDA runtime so
-that the shared object only needs the driver at run time.
+that the shared object only needs the driver at run time.  Beside it stands
+``geocache_rows_binding.so``, a module of the running interpreter (g++, torch's
+headers) through which Python calls the operators on rows.
 """
 from __future__ import annotations
 
@@ -11,6 +13,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libgeocache.so")
+BINDING = os.path.join(LIBDIR, "geocache_rows_binding.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2", "--expt-relaxed-constexpr"]
@@ -34,8 +38,12 @@ def _sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def _binding_source():
+    return os.path.join(CSRC, "geocache_rows_binding.cpp")
+
+
 def _deps():
-    return (_sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh"))
+    return (_sources() + [_binding_source()] + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh"))
             + glob.glob(os.path.join(INCLUDE, "*.h")) + [os.path.abspath(__file__)])
 
 
@@ -54,9 +62,9 @@ def source_hash() -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return any(os.path.getmtime(d) > t for d in _deps())
 
 
@@ -75,6 +83,11 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return _build_locked(verbose, extra_flags)
 
 
+def _torch_dir() -> str:
+    import importlib.util
+    return os.path.dirname(importlib.util.find_spec("torch").origin)
+
+
 def _build_locked(verbose, extra_flags) -> str:
     cc = nvcc()
     objs, procs = [], []
@@ -85,6 +98,12 @@ def _build_locked(verbose, extra_flags) -> str:
             cmd.insert(1, "-Xptxas=-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
         objs.append(obj)
+    torch_dir = _torch_dir()
+    binding_obj = os.path.join(LIBDIR, "geocache_rows_binding.o")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE, "-I", os.path.join(torch_dir, "include"),
+           "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], "-c", _binding_source(), "-o", binding_obj]
+    procs.append((_binding_source(), subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -93,10 +112,14 @@ def _build_locked(verbose, extra_flags) -> str:
         if p.returncode:
             failed.append(src)
     if failed:
-        raise RuntimeError("nvcc failed on: " + ", ".join(failed))
+        raise RuntimeError("compiling failed on: " + ", ".join(failed))
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([cc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs])
     os.replace(tmp, LIB)
+    tmp = BINDING + ".tmp%d" % os.getpid()
+    subprocess.check_call(["g++", "-shared", "-o", tmp, binding_obj, "-L", LIBDIR, "-lgeocache", "-Wl,-rpath,$ORIGIN",
+                           "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, BINDING)
     return LIB
 
 

@@ -12,6 +12,8 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import importlib.machinery
+import importlib.util
 import operator
 import os
 
@@ -730,34 +732,41 @@ def attention(plan: AttentionPlan, q, k, v, out=None, lse=None, scale=None, work
 
 # ------------------------------------ around the attention of a block --
 _E4M3 = torch.float8_e4m3fn
-_ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, _E4M3: E4M3}
 _ACTIVATIONS = {None: ACT_NONE, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
-_ROWS_SIZE = ctypes.sizeof(Rows)
+_ROWS = None
 
 
-def _rows_of(t, dtype, T, C, name):
-    """(address, stride) of a [T, C] view whose rows' elements are consecutive."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == (T, C):
-        rs, es = t.stride()
-        if es == 1 or C == 1:
-            return t.data_ptr(), rs
-        raise ValueError("the elements of a row of %s must be consecutive" % name)
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("%s must be a torch tensor" % name)
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s (got %s)" % (name, dtype, t.dtype))
-    if not t.is_cuda:
-        raise ValueError("%s must be on a CUDA device" % name)
-    raise ValueError("%s must be [%d, %d] (got %s)" % (name, T, C, list(t.shape)))
+def _rows_binding():
+    """The module that checks and marshals the tensors of the calls on rows
+    (csrc/geocache_rows_binding.cpp)."""
+    global _ROWS
+    if _ROWS is None:
+        load()
+        if not os.path.exists(_build.BINDING):
+            raise RuntimeError("%s is not built; run __graft_entry__.build()" % _build.BINDING)
+        loader = importlib.machinery.ExtensionFileLoader("geocache_rows_binding", _build.BINDING)
+        spec = importlib.util.spec_from_file_location("geocache_rows_binding", _build.BINDING, loader=loader)
+        _ROWS = importlib.util.module_from_spec(spec)
+        loader.exec_module(_ROWS)
+    return _ROWS
 
 
-def _norm_input(x):
+def _handle(stream):
+    """A stream's handle as an integer."""
+    if stream is None and torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        # (without a device the call is refused for its tensors)
+        return 0 if stream is None else stream.cuda_stream
+    return int(stream)
+
+
+def _tensor(x, name):
     if not isinstance(x, torch.Tensor):
-        raise TypeError("x must be a torch tensor")
-    if x.dtype is _E4M3 or x.dtype not in _ROW_DTYPES:
-        raise TypeError("x must be float32, bfloat16 or float16 (got %s)" % x.dtype)
-    T, C = x.shape
-    return T, C, x.dtype
+        raise TypeError("%s must be a torch tensor" % name)
+    if x.dim() != 2:
+        raise ValueError("%s must have two axes (has %d)" % (name, x.dim()))
+    return x
 
 
 def add_rms_norm(x, residual=None, weight=None, eps=1e-6, out=None, scale=None, residual_out=None, quantize=False,
@@ -770,32 +779,14 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, out=None, scale=None, 
     None (on the call's stream); residual_out may be the residual itself.  Forward
     only: results carry no gradient.  Returns (out, scale or None, residual_out or
     None)."""
-    T, C, dt = _norm_input(x)
-    if scale is not None or (out is not None and out.dtype is _E4M3):
-        quantize = True
     if out is None:
-        out = _empty((T, C), _E4M3 if quantize else dt, x.device, stream)
-    if quantize and scale is None:
-        scale = _empty((T,), torch.float32, x.device, stream)
-    at_r = at_o = 0
-    f32 = torch.float32
-    rd, rows = dt, _rows_of(x, dt, T, C, "x") + _rows_of(out, _E4M3 if quantize else dt, T, C, "out")
-    if residual is not None:
-        rd = residual.dtype
-        if rd is not dt and rd is not f32:
-            raise TypeError("residual must be %s or float32 (got %s)" % (dt, rd))
-        if residual_out is None:
-            residual_out = _empty((T, C), rd, x.device, stream)
-        rows += _rows_of(residual, rd, T, C, "residual") + _rows_of(residual_out, rd, T, C, "residual_out")
-    elif residual_out is not None:
-        raise ValueError("residual_out without residual")
-    held = array.array("q", rows)
-    at = held.buffer_info()[0]
-    if residual is not None:
-        at_r, at_o = at + 2 * _ROWS_SIZE, at + 3 * _ROWS_SIZE
-    _check(load().geocache_add_rms_norm(at, at_r, at_o, at + _ROWS_SIZE, T, C, _ROW_DTYPES[dt], _ROW_DTYPES[rd],
-                                        _dev(weight, f32, C, "weight"), float(eps), _dev(scale, f32, T, "scale"),
-                                        _stream(stream)))
+        quantize = quantize or scale is not None
+        out = _empty(_tensor(x, "x").shape, _E4M3 if quantize else x.dtype, x.device, stream)
+    if scale is None and (quantize or out.dtype is _E4M3):
+        scale = _empty((_tensor(x, "x").shape[0],), torch.float32, x.device, stream)
+    if residual is not None and residual_out is None:
+        residual_out = _empty(_tensor(x, "x").shape, _tensor(residual, "residual").dtype, x.device, stream)
+    _check((_ROWS or _rows_binding()).add_rms_norm(x, residual, weight, eps, out, scale, residual_out, _handle(stream)))
     return out, scale, residual_out
 
 
@@ -803,15 +794,11 @@ def quantize_rows(x, out=None, scale=None, stream=None):
     """geocache_quantize_rows: the rows of x [T, C] (f32, bf16 or f16; any stride
     between rows) in 8 bits (float8_e4m3fn) with a scale each (device f32 [T]).
     Outputs are allocated when None (on the call's stream).  Returns (out, scale)."""
-    T, C, dt = _norm_input(x)
     if out is None:
-        out = _empty((T, C), _E4M3, x.device, stream)
+        out = _empty(_tensor(x, "x").shape, _E4M3, x.device, stream)
     if scale is None:
-        scale = _empty((T,), torch.float32, x.device, stream)
-    held = array.array("q", _rows_of(x, dt, T, C, "x") + _rows_of(out, _E4M3, T, C, "out"))
-    at = held.buffer_info()[0]
-    _check(load().geocache_quantize_rows(at, at + _ROWS_SIZE, T, C, _ROW_DTYPES[dt], _dev(scale, torch.float32, T, "scale"),
-                                         _stream(stream)))
+        scale = _empty((_tensor(x, "x").shape[0],), torch.float32, x.device, stream)
+    _check((_ROWS or _rows_binding()).quantize_rows(x, out, scale, _handle(stream)))
     return out, scale
 
 
@@ -827,30 +814,15 @@ def linear(x, weight, bias=None, activation=None, gated=False, residual=None, x_
     operands: bf16, f16 or f32); it is allocated on the call's stream when None, as
     `out_dtype` (None: x's type, or bf16).  Forward only: the result carries no
     gradient.  Returns out."""
-    T, K = x.shape
-    rows = weight.shape[0]
-    if gated and rows % 2:
-        raise ValueError("a gated product has an even number of weight rows (got %d)" % rows)
-    N = rows // 2 if gated else rows
-    dt = x.dtype
     if out is None:
         if out_dtype is None:
-            out_dtype = torch.bfloat16 if dt is _E4M3 else dt
-        out = _empty((T, N), out_dtype, x.device, stream)
+            out_dtype = torch.bfloat16 if _tensor(x, "x").dtype is _E4M3 else x.dtype
+        N = _tensor(weight, "weight").shape[0]
+        out = _empty((_tensor(x, "x").shape[0], N // 2 if gated else N), out_dtype, x.device, stream)
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise TypeError("out must be %s (got %s)" % (out_dtype, out.dtype))
-    od = out.dtype
-    if dt not in _ROW_DTYPES or od not in _ROW_DTYPES:
-        raise TypeError("x and out cannot be %s and %s" % (dt, od))
-    held = array.array("q", _rows_of(x, dt, T, K, "x") + _rows_of(weight, dt, rows, K, "weight") +
-                       _rows_of(out, od, T, N, "out") +
-                       ((0, 0) if residual is None else _rows_of(residual, od, T, N, "residual")))
-    at = held.buffer_info()[0]
-    f32 = torch.float32
-    _check(load().geocache_linear(
-        at, at + _ROWS_SIZE, 0 if residual is None else at + 3 * _ROWS_SIZE, at + 2 * _ROWS_SIZE, T, K, N, _ROW_DTYPES[dt],
-        _ROW_DTYPES[od], _ACTIVATIONS[activation], 1 if gated else 0, _dev(bias, f32, rows, "bias"),
-        _dev(x_scale, f32, T, "x_scale"), _dev(weight_scale, f32, rows, "weight_scale"), _stream(stream)))
+    _check((_ROWS or _rows_binding()).linear(x, weight, bias, _ACTIVATIONS[activation], gated, residual, x_scale,
+                                             weight_scale, out, _handle(stream)))
     return out
 
 
