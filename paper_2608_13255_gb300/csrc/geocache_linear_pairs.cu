@@ -127,6 +127,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         b->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == kLoadWarp && elect()) {
+        prefetch_map(&wm);
+        prefetch_map(&xm);
+        if (p.out_tma) prefetch_map(&om);
+    }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(2 * kN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
