@@ -171,57 +171,59 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     const int unit_f = threadIdx.x % kUnits * 4;
 
     if (warp == kTileLoadWarp) {
-        uint32_t stage = 0, phase = 0, armed = 0;
-        bool drop = p.a.drop_first_copy && blockIdx.x == 0;
-        const int step = eight ? kRowBytes : kRowBytes / 2;
-        for (int c = c0; c < c1; ++c) {
-            if (!mbar_wait(&b->empty[stage], phase ^ 1, limit, &b->dead)) break;
-            if (!drop) {
-                if (elect()) {
+        if (elect()) {
+            uint32_t stage = 0, phase = 0, armed = 0;
+            bool drop = p.a.drop_first_copy && blockIdx.x == 0;
+            const int step = eight ? kRowBytes : kRowBytes / 2, second = kGated ? p.a.N + first : first + kFeatures / 2;
+            for (int c = c0; c < c1; ++c) {
+                if (!wait_one(&b->empty[stage], phase ^ 1, limit, &b->dead, &g_linear_error)) break;
+                if (!drop) {
                     const uint32_t at = smem + stage * stage_bytes;
                     mbar_expect(&b->full[stage], stage_bytes);
                     tma_2d(at, &wm, c * step, first, &b->full[stage]);
-                    tma_2d(at + w_bytes / 2, &wm, c * step, kGated ? p.a.N + first : first + kFeatures / 2, &b->full[stage]);
+                    tma_2d(at + w_bytes / 2, &wm, c * step, second, &b->full[stage]);
                     tma_2d(at + w_bytes, &xm, c * step, (int)first_token, &b->full[stage]);
+                    armed |= 1u << stage;
                 }
-                __syncwarp();
-                armed |= 1u << stage;
+                drop = false;
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
-            drop = false;
-            if (++stage == p.stages) { stage = 0; phase ^= 1; }
-        }
-        // the copies in flight land before the block goes on
-        const unsigned long long t0 = globaltimer();
-        for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
-            const uint32_t parity = s < stage ? phase : phase ^ 1;
-            while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
+            // the copies in flight land before the block goes on
+            const unsigned long long t0 = globaltimer();
+            for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+                const uint32_t parity = s < stage ? phase : phase ^ 1;
+                while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
+            }
         }
     } else if (warp == kTileMmaWarp) {
-        uint32_t stage = 0, phase = 0;
-        for (int c = c0; c < c1; ++c) {
-            const int i = c - c0, part = kParts ? i / kPartChunks : 0;
-            const bool begin = kParts ? i % kPartChunks == 0 : i == 0;
-            const bool end = c == c1 - 1 || (kParts && i % kPartChunks == kPartChunks - 1);
-            if (kParts && begin && part >= 2 && !mbar_wait(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead)) break;
-            if (!mbar_wait(&b->full[stage], phase, limit, &b->dead)) break;
-            tc_after();
-            if (elect()) {
+        if (elect()) {
+            uint32_t stage = 0, phase = 0;
+            bool ready = false;   // the stage has been seen full
+            for (int c = c0; c < c1; ++c) {
+                const int i = c - c0, part = kParts ? i / kPartChunks : 0;
+                const bool begin = kParts ? i % kPartChunks == 0 : i == 0;
+                const bool end = c == c1 - 1 || (kParts && i % kPartChunks == kPartChunks - 1);
+                if (kParts && begin && part >= 2 &&
+                    !wait_one(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, &g_linear_error))
+                    break;
+                if (!ready && !wait_one(&b->full[stage], phase, limit, &b->dead, &g_linear_error)) break;
+                tc_after();
                 const uint32_t at = smem + stage * stage_bytes;
+                uint64_t* const empty = &b->empty[stage];
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+                ready = mbar_test(&b->full[stage], phase);   // (looked at behind the products)
                 const uint64_t w = smem_desc(at, 16), x = smem_desc(at + w_bytes, 16);
 #pragma unroll
                 for (int k = 0; k < kRowBytes / 32; ++k)
                     mma(tmem + (part & 1) * p.tokens, w + k * 2, x + k * 2, p.idesc, eight, !begin || k > 0);
-                tc_commit(&b->empty[stage]);
+                tc_commit(empty);
                 if (end) tc_commit(&b->sums[part & 1]);
             }
-            __syncwarp();
-            if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            // every product is done before the block goes on, those too that were issued before a wait ran out
+            tc_commit(&b->done);
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
         }
-        // every product is done before the block goes on, those too that were issued before a wait ran out
-        if (elect()) tc_commit(&b->done);
-        __syncwarp();
-        const unsigned long long t0 = globaltimer();
-        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
     } else if (warp < 4) {
         const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
         float acc[kParts ? kMostTokens : 1];
@@ -277,6 +279,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         }
         tc_before();
     }
+    __syncwarp();
     Epilogue e;
     load_epilogue<kGated>(e, p.a, first + unit_f);
     // Tensor memory is given back before the block waits for its cluster: blocks of two clusters that held it while they

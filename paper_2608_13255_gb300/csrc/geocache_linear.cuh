@@ -19,6 +19,33 @@ __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int
         "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
         : "memory");
 }
+// Waits of a single thread.  The loops that issue copies and products run in one elected thread each: with a vote, an
+// election and two barriers a step, the whole warp needed 530 to 650 cycles for one whose products take 256 to 512.
+static __device__ __noinline__ bool wait_late(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
+    const unsigned long long t0 = globaltimer();
+    while (!mbar_try(bar, parity)) {
+        if (*(volatile uint32_t*)dead) return false;
+        if (globaltimer() - t0 > limit_ns) {
+            *(volatile uint32_t*)dead = 1;
+            atomicOr(error, 1u);
+            return false;
+        }
+    }
+    return true;
+}
+static __device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
+    return mbar_try(bar, parity) || wait_late(bar, parity, limit_ns, dead, error);
+}
+// whether a phase is over, without a wait
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // D (tensor memory) = A B (+ D), A and B in shared memory, 32 bytes of a row of each
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool eight, uint32_t accumulate) {

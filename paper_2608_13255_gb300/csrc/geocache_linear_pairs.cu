@@ -32,26 +32,41 @@ struct PairParams {
 };
 
 struct PairBarriers {
-    uint64_t full[kMostStages], peer[kMostStages], empty[kMostStages], sums[2], taken[2], done;
+    uint64_t full[kMostStages], empty[kMostStages], sums[2], taken[2], done;
     uint32_t tmem, dead;
+    uint32_t copies[2];   // steps whose copies each block has issued (in the first block)
 };
 
-// As mbar_wait_slow, for arrivals from both blocks; the block that gives up tells the other one.
-__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
-    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+// A block that gives up tells the other one as well.
+__device__ __noinline__ bool pair_late(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
     const unsigned long long t0 = globaltimer();
-    while (!__all_sync(0xffffffffu, mbar_try(bar, parity))) {
-        const bool late = globaltimer() - t0 > limit_ns;
-        if (__any_sync(0xffffffffu, late || *(volatile uint32_t*)dead)) {
-            if (late) {
-                for (uint32_t r = 0; r < 2; ++r)
-                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(dead), r)), "r"(1u) : "memory");
-                atomicOr(error, 1u);
-            }
+    while (!mbar_try(bar, parity)) {
+        if (*(volatile uint32_t*)dead) return false;
+        if (globaltimer() - t0 > limit_ns) {
+            for (uint32_t r = 0; r < 2; ++r)
+                asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(dead), r)), "r"(1u) : "memory");
+            atomicOr(error, 1u);
             return false;
         }
     }
     return true;
+}
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
+    return mbar_try(bar, parity) || pair_late(bar, parity, limit_ns, dead, error);
+}
+// the lanes of a warp together and all with one answer
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
+    return __all_sync(0xffffffffu, wait_pair(bar, parity, limit_ns, dead, error));
+}
+// a copy into this block's memory that signals to a barrier of either block (its address in the cluster)
+__device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_cluster(smem_u32(bar), rank)) : "memory");
@@ -115,8 +130,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned int* const error = p.a.error;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&b->full[s], 1);
-            mbar_init(&b->peer[s], 1);
+            mbar_init(&b->full[s], 2);   // (the first block's: both blocks' copies)
             mbar_init(&b->empty[s], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -125,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(&b->done, 1);
         b->dead = 0;
+        b->copies[0] = b->copies[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kLoadWarp && elect()) {
@@ -147,77 +162,72 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool eight = p.a.in_dtype == GEOCACHE_E4M3;
 
     if (warp == kLoadWarp) {
-        uint32_t stage = 0, phase = 0, armed = 0;
-        bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
-        const int step = eight ? kRowBytes : kRowBytes / 2;
-        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
-            int token_tile, feature_tile;
-            tile_at(p, tile, token_tile, feature_tile);
-            const int token = token_tile * kTokens + (int)rank * 128;
-            const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
-            for (int c = 0; c < p.chunks; ++c) {
-                ok = wait_pair(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
-                if (!ok) break;
-                if (!drop) {
-                    if (elect()) {
-                        const uint32_t at = smem + stage * kStage;
-                        mbar_expect(&b->full[stage], kStage);
-                        tma_2d(at, &xm, c * step, token, &b->full[stage]);
-                        tma_2d(at + 128 * kRowBytes, &wm, c * step, row, &b->full[stage]);
+        if (elect()) {
+            uint32_t stage = 0, phase = 0, n = 0;
+            bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
+            const int step = eight ? kRowBytes : kRowBytes / 2;
+            const uint32_t full = in_cluster(smem_u32(&b->full[0]), 0);
+            for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+                int token_tile, feature_tile;
+                tile_at(p, tile, token_tile, feature_tile);
+                const int token = token_tile * kTokens + (int)rank * 128;
+                const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
+                for (int c = 0; c < p.chunks; ++c) {
+                    ok = wait_pair(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
+                    if (!ok) break;
+                    if (!drop) {
+                        const uint32_t at = smem + stage * kStage, bar = full + stage * 8;
+                        expect_at(bar, kStage);
+                        tma_pair(at, &xm, c * step, token, bar);
+                        tma_pair(at + 128 * kRowBytes, &wm, c * step, row, bar);
                     }
-                    __syncwarp();
-                    armed |= 1u << stage;
+                    drop = false;
+                    ++n;
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
-                drop = false;
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(&b->copies[rank]), 0)), "r"(n) : "memory");
+            // the products that read the copies have signalled before the block goes on
+            const unsigned long long t0 = globaltimer();
+            for (uint32_t s = 0; ok && s < (uint32_t)kStages && s < n; ++s) {
+                const uint32_t parity = s < stage ? phase : phase ^ 1;
+                while (!mbar_try(&b->empty[s], parity) && !*(volatile uint32_t*)&b->dead && globaltimer() - t0 < kDrainLimitNs) {}
             }
         }
-        // the copies in flight land before the block goes on, and the products that read them signal
-        const unsigned long long t0 = globaltimer();
-        for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
-            const uint32_t parity = s < stage ? phase : phase ^ 1;
-            while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
-            while (ok && (armed >> s & 1) && !mbar_try(&b->empty[s], parity) && !*(volatile uint32_t*)&b->dead &&
-                   globaltimer() - t0 < kDrainLimitNs) {}
-        }
     } else if (warp == kMmaWarp) {
-        uint32_t stage = 0, phase = 0, part = 0;   // parts are counted over all tiles
-        bool ok = true;
-        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
-            for (int c = 0; c < p.chunks; ++c) {
-                const bool begin = kParts ? c % kPartChunks == 0 : c == 0;
-                const bool end = c == p.chunks - 1 || (kParts && c % kPartChunks == kPartChunks - 1);
-                if (rank == 0) {
-                    if (begin && part >= 2) ok = wait_pair(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
-                    ok = ok && wait_pair(&b->full[stage], phase, limit, &b->dead, error) &&
-                         wait_pair(&b->peer[stage], phase, limit, &b->dead, error);
-                    if (!ok) break;
-                    tc_after();
-                    if (elect()) {
+        if (elect()) {
+            if (rank == 0) {
+                uint32_t stage = 0, phase = 0, part = 0;   // parts are counted over all tiles
+                bool ok = true, ready = false;             // ready: the stage has been seen full
+                for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+                    for (int c = 0; c < p.chunks; ++c) {
+                        const bool begin = kParts ? c % kPartChunks == 0 : c == 0;
+                        const bool end = c == p.chunks - 1 || (kParts && c % kPartChunks == kPartChunks - 1);
+                        if (begin && part >= 2) ok = wait_pair(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
+                        if (ok && !ready) ok = wait_pair(&b->full[stage], phase, limit, &b->dead, error);
+                        if (!ok) break;
+                        tc_after();
                         const uint32_t at = smem + stage * kStage;
+                        uint64_t* const empty = &b->empty[stage];
+                        if (++stage == kStages) { stage = 0; phase ^= 1; }
+                        ready = mbar_test(&b->full[stage], phase);   // (looked at behind the products)
                         const uint64_t x = smem_desc(at, 16), w = smem_desc(at + 128 * kRowBytes, 16);
 #pragma unroll
                         for (int k = 0; k < kRowBytes / 32; ++k)
                             mma_pair(tmem + (part & 1) * kN, x + k * 2, w + k * 2, p.idesc, eight, !begin || k > 0);
-                        commit_pair(&b->empty[stage]);
-                        if (end) commit_pair(&b->sums[part & 1]);
+                        commit_pair(empty);
+                        if (end) {
+                            commit_pair(&b->sums[part & 1]);
+                            ++part;
+                        }
                     }
-                    __syncwarp();
-                } else {
-                    ok = wait_pair(&b->full[stage], phase, limit, &b->dead, error);
-                    if (!ok) break;
-                    if (elect()) arrive_at(&b->peer[stage], 0);
-                    __syncwarp();
                 }
-                part += end;
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+                // every product is done before the blocks go on, those too that were issued before a wait ran out
+                commit_pair(&b->done);
             }
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
         }
-        // every product is done before the blocks go on, those too that were issued before a wait ran out
-        if (rank == 0 && elect()) commit_pair(&b->done);
-        __syncwarp();
-        const unsigned long long t0 = globaltimer();
-        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
     } else {
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + half * kCols;
@@ -372,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = 0; i < kG * kCols; ++i) acc[kParts ? i : 0] = 0.0f;
             }
             for (int q = 0; ok && q < parts; ++q, ++part) {
-                ok = wait_pair(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead, error);
+                ok = wait_warp(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead, error);
                 if (!ok) break;
                 tc_after();
                 const uint32_t from = at + (part & 1) * kN;
@@ -436,9 +446,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (p.out_tma && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
     }
+    __syncwarp();
     tc_before();
     __syncthreads();
     cluster_sync();   // neither block ends while the other's products, arrivals or signals may reach it
+    if (*(volatile uint32_t*)&b->dead) {   // (in both blocks)
+        // Copies that no product has waited for land before the blocks end.  A stage for which only one block has issued
+        // them lacks an arrival.
+        if (rank == 0 && threadIdx.x == 0) {
+            const unsigned long long t0 = globaltimer();
+            for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
+                uint32_t arrivals = 0;
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t n = *(volatile uint32_t*)&b->copies[r];
+                    arrivals += n > s ? (n - s + kStages - 1) / kStages : 0;
+                }
+                if (s == 0 && p.a.drop_first_copy && blockIdx.x == 0 && b->copies[0]) --arrivals;
+                if (arrivals & 1) mbar_arrive(&b->full[s]);
+                const uint32_t phases = (arrivals + 1) / 2;
+                while (phases && !mbar_try(&b->full[s], (phases - 1) & 1) && globaltimer() - t0 < kDrainLimitNs) {}
+            }
+        }
+        __syncwarp();
+        cluster_sync();
+    }
     tc_after();
     if (warp == kMmaWarp)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
