@@ -16,8 +16,9 @@ __device__ unsigned int g_linear_error = 0;
 
 constexpr int kFeatures = 128;   // rows of weights in a tile (gated: 64 of values and 64 of gates)
 
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead) {
-    return __all_sync(0xffffffffu, mbar_try(bar, parity)) || mbar_wait_slow(bar, parity, limit_ns, dead, &g_linear_error);
+// the lanes of a warp together and all with one answer
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead) {
+    return __all_sync(0xffffffffu, wait_one(bar, parity, limit_ns, dead, &g_linear_error));
 }
 
 struct Params {
@@ -112,7 +113,7 @@ struct TileBarriers {
     uint32_t tmem, dead;
 };
 
-template <typename Out, bool kGated>
+template <typename Out, bool kEight, bool kGated>
 __global__ void __launch_bounds__(kTileThreads, 2)
     linear_tile_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm) {
     constexpr bool kParts = std::is_same<Out, float>::value;
@@ -163,7 +164,6 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     constexpr int kPart = kGated ? kFeatures / 2 : kFeatures;   // output features of a tile
     const int first = feature_tile * kPart;
     const int c0 = (int)((long long)p.chunks * rank / p.splits), c1 = (int)((long long)p.chunks * (rank + 1) / p.splits);
-    const bool eight = p.a.in_dtype == GEOCACHE_E4M3;
     const uint32_t w_bytes = kFeatures * kRowBytes, stage_bytes = w_bytes + p.tokens * kRowBytes;
     // [block][token][feature] f32; with one block over its stages, whose last products have read them
     const uint32_t sums = p.splits > 1 ? smem + p.stages * stage_bytes : smem;
@@ -173,19 +173,20 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     if (warp == kTileLoadWarp) {
         if (elect()) {
             uint32_t stage = 0, phase = 0, armed = 0;
-            bool drop = p.a.drop_first_copy && blockIdx.x == 0;
-            const int step = eight ? kRowBytes : kRowBytes / 2, second = kGated ? p.a.N + first : first + kFeatures / 2;
-            for (int c = c0; c < c1; ++c) {
+            const int step = kEight ? kRowBytes : kRowBytes / 2, second = kGated ? p.a.N + first : first + kFeatures / 2;
+            int c = c0;
+            if (p.a.drop_first_copy && blockIdx.x == 0) {
+                ++c;
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            }
+            for (; c < c1; ++c) {
                 if (!wait_one(&b->empty[stage], phase ^ 1, limit, &b->dead, &g_linear_error)) break;
-                if (!drop) {
-                    const uint32_t at = smem + stage * stage_bytes;
-                    mbar_expect(&b->full[stage], stage_bytes);
-                    tma_2d(at, &wm, c * step, first, &b->full[stage]);
-                    tma_2d(at + w_bytes / 2, &wm, c * step, second, &b->full[stage]);
-                    tma_2d(at + w_bytes, &xm, c * step, (int)first_token, &b->full[stage]);
-                    armed |= 1u << stage;
-                }
-                drop = false;
+                const uint32_t at = smem + stage * stage_bytes;
+                mbar_expect(&b->full[stage], stage_bytes);
+                tma_2d(at, &wm, c * step, first, &b->full[stage]);
+                tma_2d(at + w_bytes / 2, &wm, c * step, second, &b->full[stage]);
+                tma_2d(at + w_bytes, &xm, c * step, (int)first_token, &b->full[stage]);
+                armed |= 1u << stage;
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
             // the copies in flight land before the block goes on
@@ -196,34 +197,32 @@ __global__ void __launch_bounds__(kTileThreads, 2)
             }
         }
     } else if (warp == kTileMmaWarp) {
-        if (elect()) {
-            uint32_t stage = 0, phase = 0;
-            bool ready = false;   // the stage has been seen full
-            for (int c = c0; c < c1; ++c) {
-                const int i = c - c0, part = kParts ? i / kPartChunks : 0;
-                const bool begin = kParts ? i % kPartChunks == 0 : i == 0;
-                const bool end = c == c1 - 1 || (kParts && i % kPartChunks == kPartChunks - 1);
-                if (kParts && begin && part >= 2 &&
-                    !wait_one(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, &g_linear_error))
-                    break;
-                if (!ready && !wait_one(&b->full[stage], phase, limit, &b->dead, &g_linear_error)) break;
-                tc_after();
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        for (int c = c0, part = 0; ok && c < c1; ++part) {
+            if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead);
+            tc_after();   // (what was read from tensor memory)
+            const int end = kParts ? min(c + kPartChunks, c1) : c1;
+            uint32_t accumulate = 0;
+            for (; ok && c < end; ++c) {
+                ok = wait_warp(&b->full[stage], phase, limit, &b->dead);
+                if (!ok) break;
                 const uint32_t at = smem + stage * stage_bytes;
-                uint64_t* const empty = &b->empty[stage];
+                if (elect())
+                    stage_products<kEight>(tmem + (part & 1) * p.tokens, desc_low(at), desc_low(at + w_bytes), p.idesc, accumulate,
+                                           smem_u32(&b->empty[stage]));
+                __syncwarp();
+                accumulate = 1;
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
-                ready = mbar_test(&b->full[stage], phase);   // (looked at behind the products)
-                const uint64_t w = smem_desc(at, 16), x = smem_desc(at + w_bytes, 16);
-#pragma unroll
-                for (int k = 0; k < kRowBytes / 32; ++k)
-                    mma(tmem + (part & 1) * p.tokens, w + k * 2, x + k * 2, p.idesc, eight, !begin || k > 0);
-                tc_commit(empty);
-                if (end) tc_commit(&b->sums[part & 1]);
             }
-            // every product is done before the block goes on, those too that were issued before a wait ran out
-            tc_commit(&b->done);
-            const unsigned long long t0 = globaltimer();
-            while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+            if (ok && elect()) tc_commit(&b->sums[part & 1]);
+            __syncwarp();
         }
+        // every product is done before the block goes on, those too that were issued before a wait ran out
+        if (elect()) tc_commit(&b->done);
+        __syncwarp();
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
     } else if (warp < 4) {
         const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
         float acc[kParts ? kMostTokens : 1];
@@ -234,7 +233,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
             for (int t = 0; t < kMostTokens; ++t) acc[kParts ? t : 0] = 0.0f;
         }
         for (int part = 0; ok && part < parts; ++part) {
-            ok = mbar_wait(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead);
+            ok = wait_warp(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead);
             tc_after();
             if (kParts && ok) {
 #pragma unroll
@@ -330,9 +329,9 @@ __global__ void __launch_bounds__(kTileThreads, 2)
 // ----------------------------------------------------------------- host --
 constexpr int kTileSmem = 112 * 1024;   // two blocks an SM
 
-template <typename Out, bool kGated>
+template <typename Out, bool kEight, bool kGated>
 cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
-    auto kern = linear_tile_kernel<Out, kGated>;
+    auto kern = linear_tile_kernel<Out, kEight, kGated>;
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem);
     if (ready != cudaSuccess) return ready;
     CUtensorMap wm, xm;
@@ -359,7 +358,8 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
 
 template <typename Out>
 cudaError_t launch_out(const Params& p, int sms, cudaStream_t s) {
-    return p.a.gated ? launch_tiles<Out, true>(p, sms, s) : launch_tiles<Out, false>(p, sms, s);
+    if (p.a.in_dtype == GEOCACHE_E4M3) return p.a.gated ? launch_tiles<Out, true, true>(p, sms, s) : launch_tiles<Out, true, false>(p, sms, s);
+    return p.a.gated ? launch_tiles<Out, false, true>(p, sms, s) : launch_tiles<Out, false, false>(p, sms, s);
 }
 
 // Which kernel and tile a product takes: the least estimate in us.  The terms were fitted to sweeps over tokens 1 to 5391,

@@ -36,31 +36,37 @@ static __device__ __noinline__ bool wait_late(uint64_t* bar, uint32_t parity, un
 static __device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
     return mbar_try(bar, parity) || wait_late(bar, parity, limit_ns, dead, error);
 }
-// whether a phase is over, without a wait
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-// D (tensor memory) = A B (+ D), A and B in shared memory, 32 bytes of a row of each
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool eight, uint32_t accumulate) {
-    if (eight)
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
+// The products of one stage, D (tensor memory) = A B (+ D), and the signal that its operands have been read.  a and b are
+// the low words of the operands' descriptors; a product takes 32 bytes of a row of each.  One statement, for few
+// instructions: the loop around it is fetched again and again beside the other warps' code, and at some 400 cycles a stage
+// it was what the tensor cores waited for.
+#define GEOCACHE_STAGE(group, kind, commit, tail)                                                                        \
+    asm volatile(                                                                                                        \
+        "{\n .reg .pred p, t;\n .reg .b64 a, b;\n .reg .b32 x, y;\n .reg .b16 m;\n mov.b16 m, 3;\n setp.ne.u32 p, %4, 0;\n setp.eq.u32 t, 0, 0;\n"         \
+        " mov.b64 a, {%1, %6};\n mov.b64 b, {%2, %6};\n tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, p;\n"       \
+        " add.u32 x, %1, 2;\n add.u32 y, %2, 2;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
+        " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
+        " add.u32 x, %1, 4;\n add.u32 y, %2, 4;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
+        " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
+        " add.u32 x, %1, 6;\n add.u32 y, %2, 6;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
+        " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
+        " tcgen05.commit." group ".mbarrier::arrive::one.shared::cluster" commit ".b64 [%5]" tail ";\n}\n" ::"r"(d),       \
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(empty), "n"(kDescHigh)                                          \
+        : "memory")
+static_assert(kRowBytes == 4 * 32, "four products a stage");
+constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;   // high word of smem_desc
+__device__ __forceinline__ uint32_t desc_low(uint32_t at) { return at >> 4 | 1u << 16; }
+template <bool kEight>
+__device__ __forceinline__ void stage_products(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate, uint32_t empty) {
+    if constexpr (kEight) GEOCACHE_STAGE("cta_group::1", "f8f6f4", "", "");
+    else GEOCACHE_STAGE("cta_group::1", "f16", "", "");
+}
+// on both blocks of a pair, whose barriers are both told
+template <bool kEight>
+__device__ __forceinline__ void stage_products_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate, uint32_t empty) {
+    if constexpr (kEight) GEOCACHE_STAGE("cta_group::2", "f8f6f4", ".multicast::cluster", ", m");
+    else GEOCACHE_STAGE("cta_group::2", "f16", ".multicast::cluster", ", m");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t* r) {
     asm volatile(

@@ -77,21 +77,6 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
                  "h"((uint16_t)3)
                  : "memory");
 }
-__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool eight, uint32_t accumulate) {
-    if (eight)
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
-}
-
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
@@ -108,7 +93,7 @@ __device__ __forceinline__ void tile_at(const PairParams& p, int tile, int& toke
     token_tile = b * p.band + in - feature_tile * rows;
 }
 
-template <typename Out, bool kGated, int kN>
+template <typename Out, bool kEight, bool kGated, int kN>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_pair_kernel(const __grid_constant__ PairParams p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm,
                        const __grid_constant__ CUtensorMap om) {
@@ -159,29 +144,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_wait();
 
     const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
-    const bool eight = p.a.in_dtype == GEOCACHE_E4M3;
 
     if (warp == kLoadWarp) {
         if (elect()) {
+            constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
             uint32_t stage = 0, phase = 0, n = 0;
-            bool drop = p.a.drop_first_copy && blockIdx.x == 0, ok = true;
-            const int step = eight ? kRowBytes : kRowBytes / 2;
+            bool ok = true, drop = p.a.drop_first_copy && blockIdx.x == 0;
             const uint32_t full = in_cluster(smem_u32(&b->full[0]), 0);
             for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
                 int token_tile, feature_tile;
                 tile_at(p, tile, token_tile, feature_tile);
                 const int token = token_tile * kTokens + (int)rank * 128;
                 const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
-                for (int c = 0; c < p.chunks; ++c) {
+                int x = 0;
+                const int end = p.chunks * kStep;
+                if (drop) {
+                    drop = false;
+                    x = kStep;
+                    n = stage = 1;
+                }
+                for (; x < end; x += kStep) {
                     ok = wait_pair(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
                     if (!ok) break;
-                    if (!drop) {
-                        const uint32_t at = smem + stage * kStage, bar = full + stage * 8;
-                        expect_at(bar, kStage);
-                        tma_pair(at, &xm, c * step, token, bar);
-                        tma_pair(at + 128 * kRowBytes, &wm, c * step, row, bar);
-                    }
-                    drop = false;
+                    const uint32_t at = smem + stage * kStage, bar = full + stage * 8;
+                    expect_at(bar, kStage);
+                    tma_pair(at, &xm, x, token, bar);
+                    tma_pair(at + 128 * kRowBytes, &wm, x, row, bar);
                     ++n;
                     if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
@@ -195,39 +183,36 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
     } else if (warp == kMmaWarp) {
-        if (elect()) {
-            if (rank == 0) {
-                uint32_t stage = 0, phase = 0, part = 0;   // parts are counted over all tiles
-                bool ok = true, ready = false;             // ready: the stage has been seen full
-                for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
-                    for (int c = 0; c < p.chunks; ++c) {
-                        const bool begin = kParts ? c % kPartChunks == 0 : c == 0;
-                        const bool end = c == p.chunks - 1 || (kParts && c % kPartChunks == kPartChunks - 1);
-                        if (begin && part >= 2) ok = wait_pair(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
-                        if (ok && !ready) ok = wait_pair(&b->full[stage], phase, limit, &b->dead, error);
+        if (rank == 0) {
+            uint32_t stage = 0, phase = 0, part = 0;   // parts are counted over all tiles
+            bool ok = true;
+            for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+                for (int c = 0; ok && c < p.chunks; ++part) {
+                    if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
+                    tc_after();   // (what was read from tensor memory)
+                    const int end = kParts ? min(c + kPartChunks, p.chunks) : p.chunks;
+                    uint32_t accumulate = 0;
+                    for (; ok && c < end; ++c) {
+                        ok = wait_warp(&b->full[stage], phase, limit, &b->dead, error);
                         if (!ok) break;
-                        tc_after();
-                        const uint32_t at = smem + stage * kStage;
-                        uint64_t* const empty = &b->empty[stage];
+                        const uint32_t at = desc_low(smem + stage * kStage);
+                        if (elect())
+                            stage_products_pair<kEight>(tmem + (part & 1) * kN, at, at + (128 * kRowBytes >> 4), p.idesc, accumulate,
+                                                        smem_u32(&b->empty[stage]));
+                        __syncwarp();
+                        accumulate = 1;
                         if (++stage == kStages) { stage = 0; phase ^= 1; }
-                        ready = mbar_test(&b->full[stage], phase);   // (looked at behind the products)
-                        const uint64_t x = smem_desc(at, 16), w = smem_desc(at + 128 * kRowBytes, 16);
-#pragma unroll
-                        for (int k = 0; k < kRowBytes / 32; ++k)
-                            mma_pair(tmem + (part & 1) * kN, x + k * 2, w + k * 2, p.idesc, eight, !begin || k > 0);
-                        commit_pair(empty);
-                        if (end) {
-                            commit_pair(&b->sums[part & 1]);
-                            ++part;
-                        }
                     }
+                    if (ok && elect()) commit_pair(&b->sums[part & 1]);
+                    __syncwarp();
                 }
-                // every product is done before the blocks go on, those too that were issued before a wait ran out
-                commit_pair(&b->done);
             }
-            const unsigned long long t0 = globaltimer();
-            while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+            // every product is done before the blocks go on, those too that were issued before a wait ran out
+            if (elect()) commit_pair(&b->done);
+            __syncwarp();
         }
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
     } else {
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + half * kCols;
@@ -475,9 +460,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
 }
 
-template <typename Out, bool kGated, int kN>
+template <typename Out, bool kEight, bool kGated, int kN>
 cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
-    auto kern = linear_pair_kernel<Out, kGated, kN>;
+    auto kern = linear_pair_kernel<Out, kEight, kGated, kN>;
     constexpr int kBytes = kRing + kFinishWarps * kTurnBytes + 1024;
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (ready != cudaSuccess) return ready;
@@ -500,16 +485,18 @@ cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
 }
 
 // f32 results: tiles of 128 rows of weights only, whose sums in registers need no spills
-template <typename Out, bool kGated>
+template <typename Out, bool kEight, bool kGated>
 cudaError_t launch_n(const PairParams& p, int features, int pairs, cudaStream_t s) {
     if constexpr (!std::is_same<Out, float>::value)
-        if (features == 256) return launch<Out, kGated, 256>(p, pairs, s);
-    return launch<Out, kGated, 128>(p, pairs, s);
+        if (features == 256) return launch<Out, kEight, kGated, 256>(p, pairs, s);
+    return launch<Out, kEight, kGated, 128>(p, pairs, s);
 }
 
 template <typename Out>
 cudaError_t launch_out(const PairParams& p, int features, int pairs, cudaStream_t s) {
-    return p.a.gated ? launch_n<Out, true>(p, features, pairs, s) : launch_n<Out, false>(p, features, pairs, s);
+    if (p.a.in_dtype == GEOCACHE_E4M3)
+        return p.a.gated ? launch_n<Out, true, true>(p, features, pairs, s) : launch_n<Out, true, false>(p, features, pairs, s);
+    return p.a.gated ? launch_n<Out, false, true>(p, features, pairs, s) : launch_n<Out, false, false>(p, features, pairs, s);
 }
 
 }  // namespace
