@@ -52,20 +52,19 @@ __device__ __forceinline__ void load_epilogue(Epilogue& e, const LinearArgs& a, 
 }
 // v: the sums, and then the results
 template <bool kGated>
-__device__ __forceinline__ void finish(float* v, float* gate, const Epilogue& e, float xs, bool scaled, int act) {
+__device__ __forceinline__ void finish(float2* v, float2* gate, const Epilogue& e, float xs, bool scaled, int act) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (scaled) v[i] = v[i] * xs * e.scale[0][i];
-        v[i] += e.bias[0][i];
-        if (kGated) {
-            if (scaled) gate[i] = gate[i] * xs * e.scale[1][i];
-            gate[i] += e.bias[1][i];
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int g = 0; g < (kGated ? 2 : 1); ++g) {
+            float2& z = g ? gate[i] : v[i];
+            const float2 bias = make_float2(e.bias[g][2 * i], e.bias[g][2 * i + 1]);
+            z = scaled ? fma2(mul2(z, both(xs)), make_float2(e.scale[g][2 * i], e.scale[g][2 * i + 1]), bias) : add2(z, bias);
         }
-    }
-    activate<4>(kGated ? gate : v, act);
+    activate<2>(kGated ? gate : v, act);
     if (kGated) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= gate[i];
+        v[0] = mul2(v[0], gate[0]);
+        v[1] = mul2(v[1], gate[1]);
     }
 }
 template <typename Out>
@@ -171,30 +170,29 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     const int unit_f = threadIdx.x % kUnits * 4;
 
     if (warp == kTileLoadWarp) {
-        if (elect()) {
-            uint32_t stage = 0, phase = 0, armed = 0;
-            const int step = kEight ? kRowBytes : kRowBytes / 2, second = kGated ? p.a.N + first : first + kFeatures / 2;
-            int c = c0;
-            if (p.a.drop_first_copy && blockIdx.x == 0) {
-                ++c;
-                if (++stage == p.stages) { stage = 0; phase ^= 1; }
-            }
-            for (; c < c1; ++c) {
-                if (!wait_one(&b->empty[stage], phase ^ 1, limit, &b->dead, &g_linear_error)) break;
-                const uint32_t at = smem + stage * stage_bytes;
-                mbar_expect(&b->full[stage], stage_bytes);
-                tma_2d(at, &wm, c * step, first, &b->full[stage]);
-                tma_2d(at + w_bytes / 2, &wm, c * step, second, &b->full[stage]);
-                tma_2d(at + w_bytes, &xm, c * step, (int)first_token, &b->full[stage]);
-                armed |= 1u << stage;
-                if (++stage == p.stages) { stage = 0; phase ^= 1; }
-            }
-            // the copies in flight land before the block goes on
-            const unsigned long long t0 = globaltimer();
-            for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
-                const uint32_t parity = s < stage ? phase : phase ^ 1;
-                while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
-            }
+        uint32_t stage = 0, phase = 0, armed = 0;
+        constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
+        const int second = kGated ? p.a.N + first : first + kFeatures / 2;
+        int c = c0;
+        if (p.a.drop_first_copy && blockIdx.x == 0) {
+            ++c;
+            if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        }
+        for (; c < c1; ++c) {
+            if (!wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead)) break;
+            const uint32_t at = smem + stage * stage_bytes;
+            if (elect())
+                stage_copies(at, at + w_bytes / 2, at + w_bytes, &wm, &xm, c * kStep, first, second, (int)first_token, smem_u32(&b->full[stage]),
+                             stage_bytes);
+            __syncwarp();
+            armed |= 1u << stage;
+            if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        }
+        // the copies in flight land before the block goes on
+        const unsigned long long t0 = globaltimer();
+        for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+            const uint32_t parity = s < stage ? phase : phase ^ 1;
+            while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
         }
     } else if (warp == kTileMmaWarp) {
         uint32_t stage = 0, phase = 0;
@@ -306,7 +304,8 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     for (int t = threadIdx.x / kUnits; t < n_tok; t += kStep) {
         const long long token = first_token + rank * p.share + t;
         const float xs = p.a.x_scale ? __ldca(p.a.x_scale + token) : 1.0f;
-        float v[4] = {}, gate[4] = {}, res[4] = {};
+        float res[4] = {};
+        float2 v[2] = {}, gate[2] = {};
         if (p.a.residual.data)
             load4(static_cast<const Out*>(p.a.residual.data) + token * p.a.residual.stride + n, p.residual_wide, n_in, res);
         for (int i = 0; i < p.splits; ++i)
@@ -316,13 +315,13 @@ __global__ void __launch_bounds__(kTileThreads, 2)
                 asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                              : "=f"(s.x), "=f"(s.y), "=f"(s.z), "=f"(s.w)
                              : "r"(sums + ((i * p.share + t) * kFeatures + g * kPart + unit_f) * 4));
-                float* w = g ? gate : v;
-                w[0] += s.x; w[1] += s.y; w[2] += s.z; w[3] += s.w;
+                float2* w = g ? gate : v;
+                w[0] = add2(w[0], make_float2(s.x, s.y));
+                w[1] = add2(w[1], make_float2(s.z, s.w));
             }
         finish<kGated>(v, gate, e, xs, p.a.x_scale != nullptr, p.a.act);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += res[i];
-        store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, v);
+        const float y[4] = {v[0].x + res[0], v[0].y + res[1], v[1].x + res[2], v[1].y + res[3]};
+        store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, y);
     }
 }
 

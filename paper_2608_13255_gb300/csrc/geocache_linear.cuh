@@ -6,6 +6,7 @@
 
 #include "geocache.h"
 #include "geocache_device.cuh"
+#include "geocache_float2.cuh"
 #include "geocache_internal.h"
 #include "geocache_tcgen05.cuh"
 
@@ -13,14 +14,28 @@ namespace geocache {
 
 constexpr int kRowBytes = 128;   // of an operand's row in a stage: 64 16-bit elements or 128 of 8 bits (one swizzle row)
 
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+// A stage's copies with the expectation of their bytes, one statement each for the same reason as its products below.
+// Two boxes of weights and one of tokens:
+__device__ __forceinline__ void stage_copies(uint32_t w_at, uint32_t w2_at, uint32_t x_at, const CUtensorMap* wm, const CUtensorMap* xm, int x, int w_row,
+                                             int w2_row, int token, uint32_t bar, uint32_t bytes) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+        "{\n mbarrier.arrive.expect_tx.shared::cta.b64 _, [%9], %10;\n"
+        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%3, {%5, %6}], [%9];\n"
+        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%1], [%3, {%5, %7}], [%9];\n"
+        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%2], [%4, {%5, %8}], [%9];\n}\n" ::"r"(w_at),
+        "r"(w2_at), "r"(x_at), "l"(wm), "l"(xm), "r"(x), "r"(w_row), "r"(w2_row), "r"(token), "r"(bar), "r"(bytes)
         : "memory");
 }
-// Waits of a single thread.  The loops that issue copies and products run in one elected thread each: with a vote, an
-// election and two barriers a step, the whole warp needed 530 to 650 cycles for one whose products take 256 to 512.
+// and of a pair's block, one box each, which signal to a barrier of either block (its address in the cluster)
+__device__ __forceinline__ void stage_copies_pair(uint32_t x_at, uint32_t w_at, const CUtensorMap* xm, const CUtensorMap* wm, int x, int token, int w_row,
+                                                  uint32_t bar, uint32_t bytes) {
+    asm volatile(
+        "{\n mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%7], %8;\n"
+        " cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%2, {%4, %5}], [%7];\n"
+        " cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%1], [%3, {%4, %6}], [%7];\n}\n" ::"r"(x_at),
+        "r"(w_at), "l"(xm), "l"(wm), "r"(x), "r"(token), "r"(w_row), "r"(bar), "r"(bytes)
+        : "memory");
+}
 static __device__ __noinline__ bool wait_late(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
     const unsigned long long t0 = globaltimer();
     while (!mbar_try(bar, parity)) {
@@ -85,22 +100,56 @@ __device__ __forceinline__ uint32_t in_cluster(uint32_t at, uint32_t rank) {
 }
 
 // ------------------------------------------------------------- epilogue --
-// exp(-x) overflows to infinity below -88, where the quotient is -0 as it should be
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
-// The branch stands around the elements: inside the loop it made the code so long that its fetching took most of a small
-// call's time.
-template <int kCount>
-__device__ __forceinline__ void activate(float* x, int act) {
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float one_over(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// x / (1 + 2^u), and 0 where 2^u is infinite
+__device__ __forceinline__ float2 damped(float2 x, float2 u) {
+    const float2 d = add2(make_float2(exp2_of(u.x), exp2_of(u.y)), both(1.0f));
+    return mul2(x, make_float2(one_over(d.x), one_over(d.y)));
+}
+// kPairs pairs.  The branch stands around the elements: inside their loop it made the code so long that its fetching took
+// most of a small call's time.
+template <int kPairs>
+__device__ __forceinline__ void activate(float2* x, int act) {
+    constexpr float kLog2e = 1.4426950408889634f;
     if (act == GEOCACHE_ACT_GELU) {
+        // x (1 + erf(x / sqrt 2)) / 2 = max(x, 0) - |x| erfc(|x| / sqrt 2) / 2, with erfc(s) = e^(-s^2) (a1 t + ... + a5 t^5),
+        // t = 1 / (1 + p s), by formula 7.1.26 of Abramowitz and Stegun's handbook (within 1.5e-7; no cancellation where x
+        // is negative).  Beyond 30 the second term is zero, infinities too.
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) x[i] = 0.5f * x[i] * (1.0f + erff(x[i] * 0.70710678118654752f));
-    } else if (act != GEOCACHE_ACT_NONE) {
-        const bool tanh = act == GEOCACHE_ACT_GELU_TANH;   // (1 + tanh u) / 2 = sigmoid(2 u)
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            const float u = 1.5957691216057308f * x[i] * fmaf(0.044715f * x[i], x[i], 1.0f);
-            x[i] *= sigmoid(tanh ? u : x[i]);
+        for (int i = 0; i < kPairs; ++i) {
+            float2 m;
+            float top, bottom;
+            asm("{\n .reg .f32 t;\n abs.f32 t, %1;\n min.NaN.f32 %0, t, 0f41F00000;\n}\n" : "=f"(m.x) : "f"(x[i].x));
+            asm("{\n .reg .f32 t;\n abs.f32 t, %1;\n min.NaN.f32 %0, t, 0f41F00000;\n}\n" : "=f"(m.y) : "f"(x[i].y));
+            asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(top) : "f"(x[i].x));
+            asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(bottom) : "f"(x[i].y));
+            const float2 d = fma2(m, both(0.3275911f * 0.70710678f), both(1.0f)), t = make_float2(one_over(d.x), one_over(d.y));
+            float2 q = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+            q = fma2(q, t, both(0.5f * 1.421413741f));
+            q = fma2(q, t, both(0.5f * -0.284496736f));
+            q = fma2(q, t, both(0.5f * 0.254829592f));
+            const float2 u = mul2(mul2(m, both(-0.5f * kLog2e)), m);
+            q = mul2(mul2(q, t), mul2(m, make_float2(exp2_of(u.x), exp2_of(u.y))));
+            x[i] = fma2(q, both(-1.0f), make_float2(top, bottom));
         }
+    } else if (act == GEOCACHE_ACT_GELU_TANH) {   // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z))
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 z = fma2(mul2(x[i], x[i]), both(-1.5957691216057308f * 0.044715f * kLog2e), both(-1.5957691216057308f * kLog2e));
+            x[i] = damped(x[i], mul2(x[i], z));
+        }
+    } else if (act == GEOCACHE_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) x[i] = damped(x[i], mul2(x[i], both(-kLog2e)));
     }
 }
 template <typename T>

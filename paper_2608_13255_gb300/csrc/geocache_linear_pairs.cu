@@ -58,16 +58,6 @@ __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, unsign
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
     return __all_sync(0xffffffffu, wait_pair(bar, parity, limit_ns, dead, error));
 }
-// a copy into this block's memory that signals to a barrier of either block (its address in the cluster)
-__device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_cluster(smem_u32(bar), rank)) : "memory");
 }
@@ -146,41 +136,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
 
     if (warp == kLoadWarp) {
-        if (elect()) {
-            constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
-            uint32_t stage = 0, phase = 0, n = 0;
-            bool ok = true, drop = p.a.drop_first_copy && blockIdx.x == 0;
-            const uint32_t full = in_cluster(smem_u32(&b->full[0]), 0);
-            for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
-                int token_tile, feature_tile;
-                tile_at(p, tile, token_tile, feature_tile);
-                const int token = token_tile * kTokens + (int)rank * 128;
-                const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
-                int x = 0;
-                const int end = p.chunks * kStep;
-                if (drop) {
-                    drop = false;
-                    x = kStep;
-                    n = stage = 1;
-                }
-                for (; x < end; x += kStep) {
-                    ok = wait_pair(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
-                    if (!ok) break;
-                    const uint32_t at = smem + stage * kStage, bar = full + stage * 8;
-                    expect_at(bar, kStage);
-                    tma_pair(at, &xm, x, token, bar);
-                    tma_pair(at + 128 * kRowBytes, &wm, x, row, bar);
-                    ++n;
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
-                }
+        constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
+        uint32_t stage = 0, phase = 0, n = 0;
+        bool ok = true, drop = p.a.drop_first_copy && blockIdx.x == 0;
+        const uint32_t full = in_cluster(smem_u32(&b->full[0]), 0);
+        for (int tile = pair; ok && tile < p.n_tiles; tile += pairs) {
+            int token_tile, feature_tile;
+            tile_at(p, tile, token_tile, feature_tile);
+            const int token = token_tile * kTokens + (int)rank * 128;
+            const int row = kGated ? feature_tile * kOut + (rank ? p.a.N : 0) : feature_tile * kN + (int)rank * (kN / 2);
+            int x = 0;
+            const int end = p.chunks * kStep;
+            if (drop) {
+                drop = false;
+                x = kStep;
+                n = stage = 1;
             }
-            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(&b->copies[rank]), 0)), "r"(n) : "memory");
-            // the products that read the copies have signalled before the block goes on
-            const unsigned long long t0 = globaltimer();
-            for (uint32_t s = 0; ok && s < (uint32_t)kStages && s < n; ++s) {
-                const uint32_t parity = s < stage ? phase : phase ^ 1;
-                while (!mbar_try(&b->empty[s], parity) && !*(volatile uint32_t*)&b->dead && globaltimer() - t0 < kDrainLimitNs) {}
+            for (; x < end; x += kStep) {
+                ok = wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
+                if (!ok) break;
+                const uint32_t at = smem + stage * kStage;
+                if (elect()) stage_copies_pair(at, at + 128 * kRowBytes, &xm, &wm, x, token, row, full + stage * 8, kStage);
+                __syncwarp();
+                ++n;
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
+        }
+        if (lane == 0) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(&b->copies[rank]), 0)), "r"(n) : "memory");
+        // the products that read the copies have signalled before the block goes on
+        const unsigned long long t0 = globaltimer();
+        for (uint32_t s = 0; ok && s < (uint32_t)kStages && s < n; ++s) {
+            const uint32_t parity = s < stage ? phase : phase ^ 1;
+            while (!mbar_try(&b->empty[s], parity) && !*(volatile uint32_t*)&b->dead && globaltimer() - t0 < kDrainLimitNs) {}
         }
     } else if (warp == kMmaWarp) {
         if (rank == 0) {
@@ -246,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // cycles that shared memory has for a tile's operands at a summed axis of 2048.
             auto word = [&](int r, int c) { return turn + r * 64 + ((c ^ (r >> 1 & 3)) << 4); };   // 16 bytes
             auto element = [&](int r, int c) { return word(r, c * (int)sizeof(Out) >> 4) + (c * (int)sizeof(Out) & 15); };
-            auto emit = [&](float* v, float* g, int j) {
+            auto emit = [&](float2* v, float2* g, int j) {
                 const int n = n0 + j;
                 if (n >= p.a.N) return;
                 const int n_in = min(kBlock, p.a.N - n);
@@ -278,56 +265,54 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     __syncwarp();
                 }
-                if (scaled) {
+                if (scaled || p.a.bias) {
 #pragma unroll
-                    for (int i = 0; i < kBlock; i += 4) {
-                        const float4 s = *reinterpret_cast<const float4*>(scale + j + i);
-                        v[i] = v[i] * xs * s.x; v[i + 1] = v[i + 1] * xs * s.y; v[i + 2] = v[i + 2] * xs * s.z; v[i + 3] = v[i + 3] * xs * s.w;
-                        if (kGated) {
-                            const float4 u = *reinterpret_cast<const float4*>(scale + kCols + j + i);
-                            g[i] = g[i] * xs * u.x; g[i + 1] = g[i + 1] * xs * u.y; g[i + 2] = g[i + 2] * xs * u.z; g[i + 3] = g[i + 3] * xs * u.w;
-                        }
-                    }
-                }
-                if (p.a.bias) {
+                    for (int i = 0; i < kBlock; i += 4)
 #pragma unroll
-                    for (int i = 0; i < kBlock; i += 4) {
-                        const float4 s = *reinterpret_cast<const float4*>(bias + j + i);
-                        v[i] += s.x; v[i + 1] += s.y; v[i + 2] += s.z; v[i + 3] += s.w;
-                        if (kGated) {
-                            const float4 u = *reinterpret_cast<const float4*>(bias + kCols + j + i);
-                            g[i] += u.x; g[i + 1] += u.y; g[i + 2] += u.z; g[i + 3] += u.w;
+                        for (int k = 0; k < kG; ++k) {
+                            float2* z = (k ? g : v) + i / 2;
+                            const float4 b4 = *reinterpret_cast<const float4*>(bias + k * kCols + j + i);
+                            if (scaled) {
+                                const float4 s4 = *reinterpret_cast<const float4*>(scale + k * kCols + j + i);
+                                z[0] = fma2(mul2(z[0], both(xs)), make_float2(s4.x, s4.y), make_float2(b4.x, b4.y));
+                                z[1] = fma2(mul2(z[1], both(xs)), make_float2(s4.z, s4.w), make_float2(b4.z, b4.w));
+                            } else {
+                                z[0] = add2(z[0], make_float2(b4.x, b4.y));
+                                z[1] = add2(z[1], make_float2(b4.z, b4.w));
+                            }
                         }
-                    }
                 }
-                activate<kBlock>(kGated ? g : v, p.a.act);
+                activate<kBlock / 2>(kGated ? g : v, p.a.act);
                 if (kGated) {
 #pragma unroll
-                    for (int i = 0; i < kBlock; ++i) v[i] *= g[i];
+                    for (int i = 0; i < kBlock / 2; ++i) v[i] = mul2(v[i], g[i]);
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    constexpr int kPer = 16 / (int)sizeof(Out);
-                    float* y = v + c * kPer;
+                    constexpr int kPer = 8 / (int)sizeof(Out);   // pairs of a word
+                    float2* y = v + c * kPer;
                     uint32_t w[4];
                     if (residual) {
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(word(lane, c)));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < kPer; ++i) {
                             if constexpr (sizeof(Out) == 4) {
-                                y[i] += __uint_as_float(w[i]);
+                                y[i] = add2(y[i], make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])));
                             } else {
                                 float u[2];
                                 unpack2<Out>(w[i], u);
-                                y[2 * i] += u[0];
-                                y[2 * i + 1] += u[1];
+                                y[i] = add2(y[i], make_float2(u[0], u[1]));
                             }
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (sizeof(Out) == 4) w[i] = __float_as_uint(y[i]);
-                        else w[i] = pack2<Out>(y[2 * i], y[2 * i + 1]);
+                    for (int i = 0; i < kPer; ++i) {
+                        if constexpr (sizeof(Out) == 4) {
+                            w[2 * i] = __float_as_uint(y[i].x);
+                            w[2 * i + 1] = __float_as_uint(y[i].y);
+                        } else {
+                            w[i] = pack2<Out>(y[i].x, y[i].y);
+                        }
                     }
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(word(lane, c)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                 }
@@ -407,14 +392,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 load(0);
 #pragma unroll 1
                 for (int j = 0; j < kCols; j += kBlock) {
-                    float v[kG][kBlock];
+                    float2 v[kG][kBlock / 2];
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                     for (int g = 0; g < kG; ++g) {
 #pragma unroll
                         for (int i = 0; i < kBlock; i += 16) asm volatile("" : GEOCACHE_PIN16(r[g] + i));
 #pragma unroll
-                        for (int i = 0; i < kBlock; ++i) v[g][i] = __uint_as_float(r[g][i]);
+                        for (int i = 0; i < kBlock / 2; ++i) v[g][i] = make_float2(__uint_as_float(r[g][2 * i]), __uint_as_float(r[g][2 * i + 1]));
                     }
                     if (j + kBlock < kCols) {   // the next columns come while these are finished
                         load(j + kBlock);

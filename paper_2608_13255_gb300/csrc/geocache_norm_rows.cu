@@ -16,6 +16,7 @@
 
 #include "geocache.h"
 #include "geocache_device.cuh"
+#include "geocache_float2.cuh"
 #include "geocache_internal.h"
 
 namespace geocache {
@@ -25,24 +26,6 @@ namespace {
 constexpr int kThreads = 256;   // of a block, or as many as a wide row takes
 constexpr float kLargest = 448.0f, kTiny = 0x1p-126f;  // of e4m3; the least scale (the least normal number)
 
-// ------------------------------------------------------- pairs of floats --
-__device__ __forceinline__ uint64_t bits(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
-__device__ __forceinline__ float2 floats(uint64_t b) { return make_float2(__uint_as_float((uint32_t)b), __uint_as_float((uint32_t)(b >> 32))); }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
-    return floats(d);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
-    return floats(d);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
-    return floats(d);
-}
 // the larger of a and |b|; a NaN stays
 __device__ __forceinline__ float max_abs(float a, float b) {
     float d;
@@ -268,14 +251,14 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], make_float2(f, f));
+                    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(f));
                 g = inv;
             }
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], make_float2(g, g));
+            for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(g));
             const int n = active ? n_of[i] : 0;
             if constexpr (kQuant) {
                 const uint32_t lo = pack_e4m3(v[i][0], v[i][1]), hi = pack_e4m3(v[i][2], v[i][3]);
