@@ -27,7 +27,7 @@ struct Params {
     int splits;        // blocks of a cluster, which share a tile's summed axis
     int share;         // tokens that each of them finishes
     int chunks;        // of kRowBytes of a row
-    int stages;
+    int stages, deep;  // a stage holds one or two chunks
     int feature_tiles;
     uint32_t columns;  // of tensor memory
     uint32_t idesc;
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     constexpr int kPart = kGated ? kFeatures / 2 : kFeatures;   // output features of a tile
     const int first = feature_tile * kPart;
     const int c0 = (int)((long long)p.chunks * rank / p.splits), c1 = (int)((long long)p.chunks * (rank + 1) / p.splits);
-    const uint32_t w_bytes = kFeatures * kRowBytes, stage_bytes = w_bytes + p.tokens * kRowBytes;
+    const uint32_t w_bytes = kFeatures * kRowBytes, chunk_bytes = w_bytes + p.tokens * kRowBytes, stage_bytes = p.deep * chunk_bytes;
     // [block][token][feature] f32; with one block over its stages, whose last products have read them
     const uint32_t sums = p.splits > 1 ? smem + p.stages * stage_bytes : smem;
     constexpr int kUnits = kPart / 4;   // of four features, in a token; a thread has those of one column
@@ -172,18 +172,26 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     if (warp == kTileLoadWarp) {
         uint32_t stage = 0, phase = 0, armed = 0;
         constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
-        const int second = kGated ? p.a.N + first : first + kFeatures / 2;
         int c = c0;
         if (p.a.drop_first_copy && blockIdx.x == 0) {
-            ++c;
+            c += p.deep;
             if (++stage == p.stages) { stage = 0; phase ^= 1; }
         }
-        for (; c < c1; ++c) {
+        for (; c < c1; c += p.deep) {
             if (!wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead)) break;
-            const uint32_t at = smem + stage * stage_bytes;
-            if (elect())
-                stage_copies(at, at + w_bytes / 2, at + w_bytes, &wm, &xm, c * kStep, first, second, (int)first_token, smem_u32(&b->full[stage]),
-                             stage_bytes);
+            const uint32_t at = smem + stage * stage_bytes, bar = smem_u32(&b->full[stage]);
+            const int n = min(p.deep, c1 - c);
+            if (elect()) {
+                mbar_expect(&b->full[stage], n * chunk_bytes);
+                tma_2d(at, &wm, c * kStep, first, bar);
+                if (kGated) tma_2d(at + w_bytes / 2, &wm, c * kStep, p.a.N + first, bar);
+                tma_2d(at + w_bytes, &xm, c * kStep, (int)first_token, bar);
+                if (n > 1) {
+                    tma_2d(at + chunk_bytes, &wm, (c + 1) * kStep, first, bar);
+                    if (kGated) tma_2d(at + chunk_bytes + w_bytes / 2, &wm, (c + 1) * kStep, p.a.N + first, bar);
+                    tma_2d(at + chunk_bytes + w_bytes, &xm, (c + 1) * kStep, (int)first_token, bar);
+                }
+            }
             __syncwarp();
             armed |= 1u << stage;
             if (++stage == p.stages) { stage = 0; phase ^= 1; }
@@ -202,13 +210,15 @@ __global__ void __launch_bounds__(kTileThreads, 2)
             tc_after();   // (what was read from tensor memory)
             const int end = kParts ? min(c + kPartChunks, c1) : c1;
             uint32_t accumulate = 0;
-            for (; ok && c < end; ++c) {
+            for (; ok && c < end; c += p.deep) {
                 ok = wait_warp(&b->full[stage], phase, limit, &b->dead);
                 if (!ok) break;
-                const uint32_t at = smem + stage * stage_bytes;
-                if (elect())
-                    stage_products<kEight>(tmem + (part & 1) * p.tokens, desc_low(at), desc_low(at + w_bytes), p.idesc, accumulate,
-                                           smem_u32(&b->empty[stage]));
+                const uint32_t w = desc_low(smem + stage * stage_bytes), x = w + (w_bytes >> 4), d = tmem + (part & 1) * p.tokens;
+                if (elect()) {
+                    products<kEight, false>(d, w, x, p.idesc, accumulate);
+                    if (c + 1 < end && p.deep > 1) products<kEight, false>(d, w + (chunk_bytes >> 4), x + (chunk_bytes >> 4), p.idesc, 1);
+                    tc_commit(&b->empty[stage]);
+                }
                 __syncwarp();
                 accumulate = 1;
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
@@ -334,16 +344,17 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem);
     if (ready != cudaSuccess) return ready;
     CUtensorMap wm, xm;
-    cudaError_t e = make_map(&wm, p.a.in_dtype, p.a.w, p.a.K, (long long)p.a.N * (kGated ? 2 : 1), kFeatures / 2);
+    cudaError_t e = make_map(&wm, p.a.in_dtype, p.a.w, p.a.K, (long long)p.a.N * (kGated ? 2 : 1), kGated ? kFeatures / 2 : kFeatures);
     if (e == cudaSuccess) e = make_map(&xm, p.a.in_dtype, p.a.x, p.a.K, p.a.T, p.tokens);
     if (e != cudaSuccess) return e;
-    const int stage = (kFeatures + p.tokens) * kRowBytes;
     const int per = (p.chunks + p.splits - 1) / p.splits;
+    p.deep = per > 1 && p.tokens <= 32 ? 2 : 1;   // (more tokens leave too few stages)
+    const int stage = p.deep * (kFeatures + p.tokens) * kRowBytes;
     p.share = (p.tokens + p.splits - 1) / p.splits;
     const int sums = p.splits * p.share * kFeatures * 4, beside = p.splits > 1 ? sums : 0;
     p.stages = (kTileSmem - 1024 - beside) / stage;
     p.stages = p.stages > kTileStages ? kTileStages : p.stages;
-    if (p.stages > per) p.stages = per;
+    if (p.stages > (per + p.deep - 1) / p.deep) p.stages = (per + p.deep - 1) / p.deep;
     int bytes = p.stages * stage + beside;
     if (bytes < sums) bytes = sums;
     p.columns = 32;

@@ -14,27 +14,21 @@ namespace geocache {
 
 constexpr int kRowBytes = 128;   // of an operand's row in a stage: 64 16-bit elements or 128 of 8 bits (one swizzle row)
 
-// A stage's copies with the expectation of their bytes, one statement each for the same reason as its products below.
-// Two boxes of weights and one of tokens:
-__device__ __forceinline__ void stage_copies(uint32_t w_at, uint32_t w2_at, uint32_t x_at, const CUtensorMap* wm, const CUtensorMap* xm, int x, int w_row,
-                                             int w2_row, int token, uint32_t bar, uint32_t bytes) {
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile(
-        "{\n mbarrier.arrive.expect_tx.shared::cta.b64 _, [%9], %10;\n"
-        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%3, {%5, %6}], [%9];\n"
-        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%1], [%3, {%5, %7}], [%9];\n"
-        " cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%2], [%4, {%5, %8}], [%9];\n}\n" ::"r"(w_at),
-        "r"(w2_at), "r"(x_at), "l"(wm), "l"(xm), "r"(x), "r"(w_row), "r"(w2_row), "r"(token), "r"(bar), "r"(bytes)
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
-// and of a pair's block, one box each, which signal to a barrier of either block (its address in the cluster)
-__device__ __forceinline__ void stage_copies_pair(uint32_t x_at, uint32_t w_at, const CUtensorMap* xm, const CUtensorMap* wm, int x, int token, int w_row,
-                                                  uint32_t bar, uint32_t bytes) {
+// a box of a pair's block, which signals to a barrier of either block (its address in the cluster)
+__device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile(
-        "{\n mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%7], %8;\n"
-        " cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%2, {%4, %5}], [%7];\n"
-        " cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%1], [%3, {%4, %6}], [%7];\n}\n" ::"r"(x_at),
-        "r"(w_at), "l"(xm), "l"(wm), "r"(x), "r"(token), "r"(w_row), "r"(bar), "r"(bytes)
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
+}
+__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 static __device__ __noinline__ bool wait_late(uint64_t* bar, uint32_t parity, unsigned long long limit_ns, uint32_t* dead, unsigned int* error) {
     const unsigned long long t0 = globaltimer();
@@ -52,36 +46,33 @@ static __device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, 
     return mbar_try(bar, parity) || wait_late(bar, parity, limit_ns, dead, error);
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-// The products of one stage, D (tensor memory) = A B (+ D), and the signal that its operands have been read.  a and b are
-// the low words of the operands' descriptors; a product takes 32 bytes of a row of each.  One statement, for few
-// instructions: the loop around it is fetched again and again beside the other warps' code, and at some 400 cycles a stage
-// it was what the tensor cores waited for.
-#define GEOCACHE_STAGE(group, kind, commit, tail)                                                                        \
+// The products of one chunk (128 bytes of a row of each operand), D (tensor memory) = A B (+ D); a and b are the low words
+// of the operands' descriptors.  One statement, for few instructions: the loop around it is fetched again and again beside
+// the other warps' code, and at some 400 cycles a turn it was what the tensor cores waited for.
+#define GEOCACHE_PRODUCTS(group, kind)                                                                                   \
     asm volatile(                                                                                                        \
-        "{\n .reg .pred p, t;\n .reg .b64 a, b;\n .reg .b32 x, y;\n .reg .b16 m;\n mov.b16 m, 3;\n setp.ne.u32 p, %4, 0;\n setp.eq.u32 t, 0, 0;\n"         \
-        " mov.b64 a, {%1, %6};\n mov.b64 b, {%2, %6};\n tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, p;\n"       \
-        " add.u32 x, %1, 2;\n add.u32 y, %2, 2;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
+        "{\n .reg .pred p, t;\n .reg .b64 a, b;\n .reg .b32 x, y;\n setp.ne.u32 p, %4, 0;\n setp.eq.u32 t, 0, 0;\n"         \
+        " mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, p;\n"       \
+        " add.u32 x, %1, 2;\n add.u32 y, %2, 2;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"                           \
         " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
-        " add.u32 x, %1, 4;\n add.u32 y, %2, 4;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
+        " add.u32 x, %1, 4;\n add.u32 y, %2, 4;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"                           \
         " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
-        " add.u32 x, %1, 6;\n add.u32 y, %2, 6;\n mov.b64 a, {x, %6};\n mov.b64 b, {y, %6};\n"                           \
-        " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n"                                                      \
-        " tcgen05.commit." group ".mbarrier::arrive::one.shared::cluster" commit ".b64 [%5]" tail ";\n}\n" ::"r"(d),       \
-        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(empty), "n"(kDescHigh)                                          \
+        " add.u32 x, %1, 6;\n add.u32 y, %2, 6;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"                           \
+        " tcgen05.mma." group ".kind::" kind " [%0], a, b, %3, t;\n}\n" ::"r"(d),                                          \
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)                                                      \
         : "memory")
-static_assert(kRowBytes == 4 * 32, "four products a stage");
+static_assert(kRowBytes == 4 * 32, "four products a chunk");
 constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;   // high word of smem_desc
 __device__ __forceinline__ uint32_t desc_low(uint32_t at) { return at >> 4 | 1u << 16; }
-template <bool kEight>
-__device__ __forceinline__ void stage_products(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate, uint32_t empty) {
-    if constexpr (kEight) GEOCACHE_STAGE("cta_group::1", "f8f6f4", "", "");
-    else GEOCACHE_STAGE("cta_group::1", "f16", "", "");
-}
-// on both blocks of a pair, whose barriers are both told
-template <bool kEight>
-__device__ __forceinline__ void stage_products_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate, uint32_t empty) {
-    if constexpr (kEight) GEOCACHE_STAGE("cta_group::2", "f8f6f4", ".multicast::cluster", ", m");
-    else GEOCACHE_STAGE("cta_group::2", "f16", ".multicast::cluster", ", m");
+template <bool kEight, bool kPair>
+__device__ __forceinline__ void products(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (kPair) {
+        if constexpr (kEight) GEOCACHE_PRODUCTS("cta_group::2", "f8f6f4");
+        else GEOCACHE_PRODUCTS("cta_group::2", "f16");
+    } else {
+        if constexpr (kEight) GEOCACHE_PRODUCTS("cta_group::1", "f8f6f4");
+        else GEOCACHE_PRODUCTS("cta_group::1", "f16");
+    }
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t* r) {
     asm volatile(

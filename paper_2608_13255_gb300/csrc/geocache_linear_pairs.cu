@@ -16,7 +16,7 @@ namespace {
 // the other half of tensor memory.  Tokens are the lanes of tensor memory: a thread finishes a token's columns.
 constexpr int kTokens = 256;               // of a tile: 128 of each block
 constexpr int kFinishWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 32 * 10;
-constexpr int kMostStages = 8;
+constexpr int kMostStages = 6;
 constexpr int kRing = 6 * 32 * 1024;       // bytes of the stages
 constexpr int kPartChunks = 4;             // as in the tile kernel: f32 results leave tensor memory in parts
 constexpr int kTurnBytes = 32 * 64;        // of a finishing warp's buffer: 64 bytes of 32 tokens, in swizzled words of 16
@@ -29,6 +29,7 @@ struct PairParams {
     int n_tiles;
     uint32_t idesc;
     int out_tma, residual_wide;      // rows of whole 16-byte words
+    int out_four, residual_four;     // else: of whole 4-byte words
 };
 
 struct PairBarriers {
@@ -83,6 +84,57 @@ __device__ __forceinline__ void tile_at(const PairParams& p, int tile, int& toke
     token_tile = b * p.band + in - feature_tile * rows;
 }
 
+// words of 4 or 2 bytes
+template <int kSize>
+__device__ __forceinline__ uint32_t load_word(const char* p) {
+    if constexpr (kSize == 4) return __ldca(reinterpret_cast<const uint32_t*>(p));
+    else return __ldca(reinterpret_cast<const unsigned short*>(p));
+}
+template <int kSize>
+__device__ __forceinline__ void store_word(char* p, uint32_t w) {
+    if constexpr (kSize == 4) *reinterpret_cast<uint32_t*>(p) = w;
+    else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
+}
+template <int kSize>
+__device__ __forceinline__ uint32_t load_shared(uint32_t at) {
+    uint32_t w;
+    if constexpr (kSize == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+    else asm volatile("{\n .reg .b16 t;\n ld.shared.b16 t, [%1];\n cvt.u32.u16 %0, t;\n}\n" : "=r"(w) : "r"(at) : "memory");
+    return w;
+}
+template <int kSize>
+__device__ __forceinline__ void store_shared(uint32_t at, uint32_t w) {
+    if constexpr (kSize == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(w) : "memory");
+    else asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((uint16_t)w) : "memory");
+}
+// Between the first `bytes` of a buffer's up to 32 rows of 64 bytes (swizzled words of 16) and rows of global memory that
+// are no whole words of 16 bytes, with a warp's lanes along the rows.
+__device__ __forceinline__ uint32_t turned(uint32_t buffer, int r, int at) { return buffer + r * 64 + (((at >> 4) ^ (r >> 1 & 3)) << 4) + (at & 15); }
+template <int kSize>
+__device__ __forceinline__ void turn_out(uint32_t buffer, char* rows, long long stride, int n_rows, int bytes, int lane) {
+    constexpr int kLanes = 64 / kSize, kStep = 32 / kLanes;   // lanes of a row; rows at a time
+    const int at = lane % kLanes * kSize;
+    if (at >= bytes) return;
+#pragma unroll 4
+    for (int r = lane / kLanes; r < n_rows; r += kStep) store_word<kSize>(rows + r * stride + at, load_shared<kSize>(turned(buffer, r, at)));
+}
+template <int kSize>
+__device__ __forceinline__ void turn_in(uint32_t buffer, const char* rows, long long stride, int n_rows, int bytes, int lane) {
+    constexpr int kLanes = 64 / kSize, kStep = 32 / kLanes;
+    const int at = lane % kLanes * kSize;
+    if (at >= bytes) return;
+#pragma unroll 1
+    for (int r0 = lane / kLanes; r0 < n_rows; r0 += 8 * kStep) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + i * kStep < n_rows) w[i] = load_word<kSize>(rows + (r0 + i * kStep) * stride + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + i * kStep < n_rows) store_shared<kSize>(turned(buffer, r0 + i * kStep, at), w[i]);
+    }
+}
+
 template <typename Out, bool kEight, bool kGated, int kN>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_pair_kernel(const __grid_constant__ PairParams p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm,
@@ -90,8 +142,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr bool kParts = std::is_same<Out, float>::value;
     constexpr int kOut = kGated ? kN / 2 : kN;          // output features of a tile
     constexpr int kCols = kOut / 2;                     // of them, those of a finishing warp
-    constexpr uint32_t kStage = (128 + kN / 2) * kRowBytes;
-    constexpr int kStages = kRing / kStage < kMostStages ? kRing / kStage : kMostStages;
+    // A turn of the loop that issues the products takes some 400 cycles, a chunk's products 512, or 256 with 128 rows of
+    // weights, whose stages hold two chunks (24576 x 2048 x 6144 bf16: 420 -> 357 us; with 256 rows 133 -> 139 for the gated
+    // 5391 x 1600 x 6400, as three stages are less even than six).
+    constexpr int kDeep = kN == 256 ? 1 : 2;
+    constexpr uint32_t kChunk = (128 + kN / 2) * kRowBytes, kStage = kDeep * kChunk;
+    constexpr int kStages = kRing / kStage;
+    static_assert(kStages <= kMostStages, "barriers");
     constexpr int kG = kGated ? 2 : 1;
     constexpr int kBlock = 64 / (int)sizeof(Out);       // columns that are finished at a time
     extern __shared__ uint8_t raw[];
@@ -149,14 +206,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int end = p.chunks * kStep;
             if (drop) {
                 drop = false;
-                x = kStep;
+                x = kDeep * kStep;
                 n = stage = 1;
             }
-            for (; x < end; x += kStep) {
+            for (; x < end; x += kDeep * kStep) {
                 ok = wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead, error);
                 if (!ok) break;
-                const uint32_t at = smem + stage * kStage;
-                if (elect()) stage_copies_pair(at, at + 128 * kRowBytes, &xm, &wm, x, token, row, full + stage * 8, kStage);
+                const uint32_t at = smem + stage * kStage, bar = full + stage * 8;
+                const bool two = kDeep > 1 && x + kStep < end;
+                if (elect()) {
+                    expect_at(bar, two ? 2 * kChunk : kChunk);
+                    tma_pair(at, &xm, x, token, bar);
+                    tma_pair(at + 128 * kRowBytes, &wm, x, row, bar);
+                    if (two) {
+                        tma_pair(at + kChunk, &xm, x + kStep, token, bar);
+                        tma_pair(at + kChunk + 128 * kRowBytes, &wm, x + kStep, row, bar);
+                    }
+                }
                 __syncwarp();
                 ++n;
                 if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -179,13 +245,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc_after();   // (what was read from tensor memory)
                     const int end = kParts ? min(c + kPartChunks, p.chunks) : p.chunks;
                     uint32_t accumulate = 0;
-                    for (; ok && c < end; ++c) {
+                    for (; ok && c < end; c += kDeep) {
                         ok = wait_warp(&b->full[stage], phase, limit, &b->dead, error);
                         if (!ok) break;
-                        const uint32_t at = desc_low(smem + stage * kStage);
-                        if (elect())
-                            stage_products_pair<kEight>(tmem + (part & 1) * kN, at, at + (128 * kRowBytes >> 4), p.idesc, accumulate,
-                                                        smem_u32(&b->empty[stage]));
+                        const uint32_t x = desc_low(smem + stage * kStage), w = x + (128 * kRowBytes >> 4), d = tmem + (part & 1) * kN;
+                        if (elect()) {
+                            products<kEight, true>(d, x, w, p.idesc, accumulate);
+                            if (kDeep > 1 && c + 1 < end) products<kEight, true>(d, x + (kChunk >> 4), w + (kChunk >> 4), p.idesc, 1);
+                            commit_pair(&b->empty[stage]);
+                        }
                         __syncwarp();
                         accumulate = 1;
                         if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -232,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // the rows).  Straight from the registers, 32 rows an instruction, the stores alone took 2,000 of the 16,400
             // cycles that shared memory has for a tile's operands at a summed axis of 2048.
             auto word = [&](int r, int c) { return turn + r * 64 + ((c ^ (r >> 1 & 3)) << 4); };   // 16 bytes
-            auto element = [&](int r, int c) { return word(r, c * (int)sizeof(Out) >> 4) + (c * (int)sizeof(Out) & 15); };
+            const int n_rows = (int)max(0LL, min(32LL, p.a.T - row0));
             auto emit = [&](float2* v, float2* g, int j) {
                 const int n = n0 + j;
                 if (n >= p.a.N) return;
@@ -253,15 +321,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                                          : "memory");
                         }
                     } else {
-                        const int c = lane % kBlock;
-                        for (int r = lane / kBlock; r < 32; r += 32 / kBlock) {
-                            if (row0 + r >= p.a.T || c >= n_in) continue;
-                            const Out w = residual[(row0 + r) * p.a.residual.stride + n + c];
-                            if constexpr (sizeof(Out) == 4)
-                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(element(r, c)), "r"(__float_as_uint(w)) : "memory");
-                            else
-                                asm volatile("st.shared.b16 [%0], %1;" ::"r"(element(r, c)), "h"(*reinterpret_cast<const uint16_t*>(&w)) : "memory");
-                        }
+                        const char* rows = (const char*)(residual + row0 * p.a.residual.stride + n);
+                        const long long stride = p.a.residual.stride * (int)sizeof(Out);
+                        if (sizeof(Out) == 4 || p.residual_four) turn_in<4>(turn, rows, stride, n_rows, n_in * (int)sizeof(Out), lane);
+                        else turn_in<2>(turn, rows, stride, n_rows, n_in * (int)sizeof(Out), lane);
                     }
                     __syncwarp();
                 }
@@ -328,21 +391,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     return;
                 }
                 __syncwarp();
-                const int c = lane % kBlock;
-#pragma unroll 4
-                for (int r = lane / kBlock; r < 32; r += 32 / kBlock) {
-                    if (row0 + r >= p.a.T || c >= n_in) continue;
-                    Out* to = out + (row0 + r) * p.a.out.stride + n + c;
-                    if constexpr (sizeof(Out) == 4) {
-                        uint32_t w;
-                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(element(r, c)) : "memory");
-                        *reinterpret_cast<uint32_t*>(to) = w;
-                    } else {
-                        uint16_t w;
-                        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(element(r, c)) : "memory");
-                        *reinterpret_cast<uint16_t*>(to) = w;
-                    }
-                }
+                char* rows = (char*)(out + row0 * p.a.out.stride + n);
+                const long long stride = p.a.out.stride * (int)sizeof(Out);
+                if (sizeof(Out) == 4 || p.out_four) turn_out<4>(turn, rows, stride, n_rows, n_in * (int)sizeof(Out), lane);
+                else turn_out<2>(turn, rows, stride, n_rows, n_in * (int)sizeof(Out), lane);
                 __syncwarp();   // the buffer has been read
             };
 
@@ -495,6 +547,9 @@ cudaError_t launch_linear_pairs(const LinearArgs& a, int features, int sms, cuda
     // (a row's end inside a word was not kept: two elements behind 70 of 16 bits were written)
     p.out_tma = words(a.out) && (long long)a.N * ob % 16 == 0;
     p.residual_wide = a.residual.data && words(a.residual);
+    auto fours = [&](const geocache_rows& r) { return !((uintptr_t)r.data % 4) && (long long)a.N * ob % 4 == 0 && r.stride * ob % 4 == 0; };
+    p.out_four = fours(a.out);
+    p.residual_four = fours(a.residual);
     if (a.out_dtype == GEOCACHE_BF16) return launch_out<__nv_bfloat16>(p, features, sms / 2, s);
     if (a.out_dtype == GEOCACHE_F16) return launch_out<__half>(p, features, sms / 2, s);
     return launch_out<float>(p, features, sms / 2, s);
