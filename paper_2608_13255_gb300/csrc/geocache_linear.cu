@@ -26,7 +26,7 @@ struct Params {
     int tokens;        // of a tile (a multiple of 16)
     int splits;        // blocks of a cluster, which share a tile's summed axis
     int share;         // tokens that each of them finishes
-    int chunks;        // of kRowBytes of a row
+    int chunks, per;   // of kRowBytes of a row; of a block
     int stages, deep;  // a stage holds one or two chunks
     int feature_tiles;
     uint32_t columns;  // of tensor memory
@@ -108,100 +108,120 @@ constexpr int kTileStages = 12;
 constexpr int kPartChunks = 4;
 
 struct TileBarriers {
-    uint64_t full[kTileStages], empty[kTileStages], sums[2], taken[2], done;
+    uint64_t full[kTileStages], empty[kTileStages], sums[2], taken[2], done, here;
     uint32_t tmem, dead;
 };
+
+__device__ __forceinline__ uint32_t cluster_id() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
 
 template <typename Out, bool kEight, bool kGated>
 __global__ void __launch_bounds__(kTileThreads, 2)
     linear_tile_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm) {
     constexpr bool kParts = std::is_same<Out, float>::value;
     constexpr int kMostTokens = kParts ? 64 : 128;
+    constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;   // elements of a chunk
     extern __shared__ uint8_t raw[];
     __shared__ TileBarriers bars;
     TileBarriers* b = &bars;
     const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const unsigned long long limit = p.a.wait_limit_ns;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&b->full[s], 1);
-            mbar_init(&b->empty[s], 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&b->sums[i], 1);
-            mbar_init(&b->taken[i], 4);
-        }
-        mbar_init(&b->done, 1);
-        b->dead = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == kTileLoadWarp && elect()) {
-        prefetch_map(&wm);
-        prefetch_map(&xm);
-    }
-    if (warp == kTileMmaWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(p.columns)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    tc_before();
-    __syncthreads();
-    tc_after();
-    if (p.splits > 1) cluster_sync();   // all blocks are there before one writes into another
-    const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
-    // Few blocks let the next kernel's begin beside them (12 x 320 x 15: 4.4 -> 3.7 us).  Where they take more than half of
-    // the SMs, blocks that come early double up on the first SMs that are free (116 x 1280 x 990: 5.4 -> 5.8).  What the
-    // next kernel holds before its own wait, this one has by now.
-    if (p.few) pdl_launch_dependents();
-    pdl_wait();
 
-    const int rank = (int)(blockIdx.x % p.splits);
-    const long long tile = blockIdx.x / p.splits;
-    const int feature_tile = (int)(tile % p.feature_tiles);
-    const long long first_token = tile / p.feature_tiles * p.tokens;
+    const int rank = (int)cluster_rank();
+    const long long first_token = (long long)cluster_id() * p.tokens;
     constexpr int kPart = kGated ? kFeatures / 2 : kFeatures;   // output features of a tile
-    const int first = feature_tile * kPart;
-    const int c0 = (int)((long long)p.chunks * rank / p.splits), c1 = (int)((long long)p.chunks * (rank + 1) / p.splits);
+    const int first = (int)blockIdx.y * kPart;
+    const int c0 = rank * p.per, c1 = min(p.chunks, c0 + p.per);
     const uint32_t w_bytes = kFeatures * kRowBytes, chunk_bytes = w_bytes + p.tokens * kRowBytes, stage_bytes = p.deep * chunk_bytes;
     // [block][token][feature] f32; with one block over its stages, whose last products have read them
     const uint32_t sums = p.splits > 1 ? smem + p.stages * stage_bytes : smem;
     constexpr int kUnits = kPart / 4;   // of four features, in a token; a thread has those of one column
     const int unit_f = threadIdx.x % kUnits * 4;
+    const int tile_tokens = max(0, min(p.tokens - rank * p.share, p.share));   // that this block finishes
 
+    uint32_t stage = 0, phase = 0, armed = 0;   // of the loads
+    int c = c0;
+    auto copies = [&]() {
+        const uint32_t at = smem + stage * stage_bytes, bar = smem_u32(&b->full[stage]);
+        const int n = min(p.deep, c1 - c);
+        if (elect()) {
+            mbar_expect(&b->full[stage], n * chunk_bytes);
+            tma_2d(at, &wm, c * kStep, first, bar);
+            if (kGated) tma_2d(at + w_bytes / 2, &wm, c * kStep, p.a.N + first, bar);
+            tma_2d(at + w_bytes, &xm, c * kStep, (int)first_token, bar);
+            if (n > 1) {
+                tma_2d(at + chunk_bytes, &wm, (c + 1) * kStep, first, bar);
+                if (kGated) tma_2d(at + chunk_bytes + w_bytes / 2, &wm, (c + 1) * kStep, p.a.N + first, bar);
+                tma_2d(at + chunk_bytes + w_bytes, &xm, (c + 1) * kStep, (int)first_token, bar);
+            }
+        }
+        __syncwarp();
+        armed |= 1u << stage;
+        c += p.deep;
+        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+    };
     if (warp == kTileLoadWarp) {
-        uint32_t stage = 0, phase = 0, armed = 0;
-        constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;
-        int c = c0;
-        if (p.a.drop_first_copy && blockIdx.x == 0) {
+        // The first copies leave as soon as their barriers are there, before the block waits for its tensor memory and its
+        // cluster (with divisions by the grid's shape after both, they left 2,200 cycles after the block's start; now 600).
+        if (lane < p.stages) {
+            mbar_init(&b->full[lane], 1);
+            mbar_init(&b->empty[lane], 1);
+        } else if (lane >= 24 && lane < 26) {
+            mbar_init(&b->sums[lane - 24], 1);
+            mbar_init(&b->taken[lane - 24], 4);
+        } else if (lane == 26) {
+            mbar_init(&b->done, 1);
+            b->dead = 0;
+        } else if (lane == 27) {
+            mbar_init(&b->here, 1);
+            if (p.splits > 1) mbar_expect(&b->here, p.splits * tile_tokens * kFeatures * 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;\n fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        pdl_wait();
+        if (p.a.drop_first_copy && blockIdx.x == 0 && blockIdx.y == 0) {
             c += p.deep;
             if (++stage == p.stages) { stage = 0; phase ^= 1; }
         }
-        for (; c < c1; c += p.deep) {
-            if (!wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead)) break;
-            const uint32_t at = smem + stage * stage_bytes, bar = smem_u32(&b->full[stage]);
-            const int n = min(p.deep, c1 - c);
-            if (elect()) {
-                mbar_expect(&b->full[stage], n * chunk_bytes);
-                tma_2d(at, &wm, c * kStep, first, bar);
-                if (kGated) tma_2d(at + w_bytes / 2, &wm, c * kStep, p.a.N + first, bar);
-                tma_2d(at + w_bytes, &xm, c * kStep, (int)first_token, bar);
-                if (n > 1) {
-                    tma_2d(at + chunk_bytes, &wm, (c + 1) * kStep, first, bar);
-                    if (kGated) tma_2d(at + chunk_bytes + w_bytes / 2, &wm, (c + 1) * kStep, p.a.N + first, bar);
-                    tma_2d(at + chunk_bytes + w_bytes, &xm, (c + 1) * kStep, (int)first_token, bar);
-                }
-            }
-            __syncwarp();
-            armed |= 1u << stage;
-            if (++stage == p.stages) { stage = 0; phase ^= 1; }
-        }
+        for (int i = (int)stage; i < p.stages && phase == 0 && c < c1; ++i) copies();
+    } else if (warp == kTileMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(p.columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    Epilogue e;
+    load_epilogue<kGated>(e, p.a, first + unit_f);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    // (all blocks of the cluster are there before one writes into another)
+    if (p.splits > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
+    // Few blocks let the next kernel's begin beside them (12 x 320 x 15: 4.4 -> 3.7 us).  Where they take more than half of
+    // the SMs, blocks that come early double up on the first SMs that are free (116 x 1280 x 990: 5.4 -> 5.8).  What the
+    // next kernel holds before its own wait, this one has by now.
+    if (p.few) pdl_launch_dependents();
+
+    if (warp == kTileLoadWarp) {
+        while (c < c1 && wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead)) copies();
         // the copies in flight land before the block goes on
         const unsigned long long t0 = globaltimer();
         for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
             const uint32_t parity = s < stage ? phase : phase ^ 1;
             while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
         }
+        __syncwarp();
+        if (p.splits > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     } else if (warp == kTileMmaWarp) {
         uint32_t stage = 0, phase = 0;
         bool ok = true;
@@ -231,6 +251,8 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         __syncwarp();
         const unsigned long long t0 = globaltimer();
         while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+        __syncwarp();
+        if (p.splits > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     } else if (warp < 4) {
         const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
         float acc[kParts ? kMostTokens : 1];
@@ -259,11 +281,18 @@ __global__ void __launch_bounds__(kTileThreads, 2)
                 if (lane == 0) mbar_arrive(&b->taken[part & 1]);
             }
         }
+        __syncwarp();
+        if (p.splits > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         // with one block the stages are overwritten: the loads have landed, as the products that wait for them are done
-        ok = ok && !*(volatile uint32_t*)&b->dead;
+        ok = __all_sync(0xffffffffu, ok && !*(volatile uint32_t*)&b->dead);
         if (ok) {
             int to = 0, in = 0;   // the block that finishes token t, and t's place there
-            uint32_t row = in_cluster(sums + ((rank * p.share) * kFeatures + warp * 32 + lane) * 4, 0);
+            const uint32_t mine = sums + (rank * p.share * kFeatures + warp * 32 + lane) * 4, here = smem_u32(&b->here);
+            uint32_t row = mine, bar = here;
+            if (p.splits > 1) {
+                row = in_cluster(mine, 0);
+                bar = in_cluster(here, 0);
+            }
 #pragma unroll
             for (int t = 0; t < kMostTokens; t += 16)
                 if (t < p.tokens) {
@@ -272,46 +301,67 @@ __global__ void __launch_bounds__(kTileThreads, 2)
                         tmem_ld16(at + t, r);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                         asm volatile("" : GEOCACHE_PIN16(r));
-                    }
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t v = kParts ? __float_as_uint(acc[kParts ? t + i : 0]) : r[i];
-                        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(row + in * (kFeatures * 4)), "r"(v) : "memory");
-                        if (++in == p.share && to + 1 < p.splits) {
-                            in = 0;
-                            row = in_cluster(sums + ((rank * p.share) * kFeatures + warp * 32 + lane) * 4, ++to);
+                        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(acc[kParts ? t + i : 0]);
+                    }
+                    if (p.splits == 1) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(mine + (t + i) * (kFeatures * 4)), "r"(r[i]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(row + in * (kFeatures * 4)),
+                                         "r"(r[i]), "r"(bar)
+                                         : "memory");
+                            if (++in == p.share && to + 1 < p.splits) {
+                                in = 0;
+                                ++to;
+                                row = in_cluster(mine, to);
+                                bar = in_cluster(here, to);
+                            }
                         }
                     }
                 }
         }
         tc_before();
+    } else if (p.splits > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
-    __syncwarp();
-    Epilogue e;
-    load_epilogue<kGated>(e, p.a, first + unit_f);
-    // Tensor memory is given back before the block waits for its cluster: blocks of two clusters that held it while they
-    // waited for each other's second block would never end.
+    // Tensor memory is given back before the block waits for others: blocks of two clusters that held it while they waited
+    // for each other's second block would never end.
     __syncthreads();
     if (warp == kTileMmaWarp) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.columns) : "memory");
     }
+    bool ok = __all_sync(0xffffffffu, !*(volatile uint32_t*)&b->dead);
     if (p.splits > 1) {
-        if ((int)threadIdx.x < p.splits && *(volatile uint32_t*)&b->dead)
+        // No block ends before the others have sent what they send; what it needs itself it waits for on its own barrier.
+        if (!ok && (int)threadIdx.x < p.splits)
             asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cluster(smem_u32(&b->dead), threadIdx.x)), "r"(1u) : "memory");
         __syncwarp();
-        cluster_sync();
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        ok = ok && (tile_tokens == 0 || wait_warp(&b->here, 0, limit, &b->dead));
     }
-    if (*(volatile uint32_t*)&b->dead) return;
+    auto leave = [&]() {
+        if (p.splits == 1) return;
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        if (!ok)   // sums on their way to a block that did not wait for all of them
+            for (const unsigned long long t0 = globaltimer(); globaltimer() - t0 < 20000;) {}
+    };
+    if (!ok) {
+        leave();
+        return;
+    }
 
     const long long left = p.a.T - first_token - (long long)rank * p.share;
-    int n_tok = min(p.tokens - rank * p.share, p.share);
-    n_tok = left < n_tok ? (int)left : n_tok;
-    const int n = first + unit_f, n_in = min(4, p.a.N - n);
-    if (n_in <= 0) return;
-    constexpr int kStep = kTileThreads / kUnits;
+    const int n = first + unit_f, n_in = min(4, p.a.N - n), n_tok = n_in <= 0 ? 0 : (int)min((long long)tile_tokens, left);
+    constexpr int kRows = kTileThreads / kUnits;
 #pragma unroll 2
-    for (int t = threadIdx.x / kUnits; t < n_tok; t += kStep) {
+    for (int t = threadIdx.x / kUnits; t < n_tok; t += kRows) {
         const long long token = first_token + rank * p.share + t;
         const float xs = p.a.x_scale ? __ldca(p.a.x_scale + token) : 1.0f;
         float res[4] = {};
@@ -333,6 +383,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         const float y[4] = {v[0].x + res[0], v[0].y + res[1], v[1].x + res[2], v[1].y + res[3]};
         store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, y);
     }
+    leave();
 }
 
 // ----------------------------------------------------------------- host --
@@ -347,7 +398,8 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
     cudaError_t e = make_map(&wm, p.a.in_dtype, p.a.w, p.a.K, (long long)p.a.N * (kGated ? 2 : 1), kGated ? kFeatures / 2 : kFeatures);
     if (e == cudaSuccess) e = make_map(&xm, p.a.in_dtype, p.a.x, p.a.K, p.a.T, p.tokens);
     if (e != cudaSuccess) return e;
-    const int per = (p.chunks + p.splits - 1) / p.splits;
+    const int per = p.per = (p.chunks + p.splits - 1) / p.splits;
+    p.splits = (p.chunks + per - 1) / per;   // (none is left without a chunk)
     p.deep = per > 1 && p.tokens <= 32 ? 2 : 1;   // (more tokens leave too few stages)
     const int stage = p.deep * (kFeatures + p.tokens) * kRowBytes;
     p.share = (p.tokens + p.splits - 1) / p.splits;
@@ -360,10 +412,10 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
     p.columns = 32;
     const int used = p.tokens * (std::is_same<Out, float>::value ? 2 : 1);
     while ((int)p.columns < used) p.columns *= 2;
-    const long long blocks = (p.a.T + p.tokens - 1) / p.tokens * p.feature_tiles * p.splits;
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    p.few = 2 * blocks <= sms;
-    return launch_cluster(kern, (unsigned)blocks, kTileThreads, bytes + 1024, p.splits, s, p, wm, xm);
+    const long long columns = (p.a.T + p.tokens - 1) / p.tokens * p.splits;
+    if (columns > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    p.few = 2 * columns * p.feature_tiles <= sms;
+    return launch_cluster(kern, dim3((unsigned)columns, (unsigned)p.feature_tiles), kTileThreads, bytes + 1024, p.splits, s, p, wm, xm);
 }
 
 template <typename Out>

@@ -184,9 +184,9 @@ inline cudaError_t make_map(CUtensorMap* map, int dtype, const geocache_rows& x,
 }
 
 template <typename... Params_, typename... Args>
-cudaError_t launch_cluster(void (*kern)(Params_...), unsigned blocks, int threads, size_t smem, int cluster, cudaStream_t s, Args... args) {
+cudaError_t launch_cluster(void (*kern)(Params_...), dim3 blocks, int threads, size_t smem, int cluster, cudaStream_t s, Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks);
+    cfg.gridDim = blocks;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;

@@ -518,7 +518,7 @@ cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
     const uint32_t type = p.a.in_dtype == GEOCACHE_BF16 ? 1 : 0;
     p.idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kTokens >> 4) << 24;
     if (pairs > p.n_tiles) pairs = p.n_tiles;
-    return launch_cluster(kern, (unsigned)(2 * pairs), kThreads, kBytes, 2, s, p, wm, xm, om);
+    return launch_cluster(kern, dim3((unsigned)(2 * pairs)), kThreads, kBytes, 2, s, p, wm, xm, om);
 }
 
 // f32 results: tiles of 128 rows of weights only, whose sums in registers need no spills
