@@ -424,9 +424,9 @@ cudaError_t launch_out(const Params& p, int sms, cudaStream_t s) {
     return p.a.gated ? launch_tiles<Out, false, true>(p, sms, s) : launch_tiles<Out, false, false>(p, sms, s);
 }
 
-// Which kernel and tile a product takes: the least estimate in us.  The terms were fitted to sweeps over tokens 1 to 5391,
-// summed axes of 320 to 8192 and 64 to 8192 features in 8 and 16 bits; over these the choice is on average 2% slower
-// than the best one.
+// Which kernel and tile a product takes: the least estimate in us.  The terms were fitted to sweeps over tokens 1 to 24576,
+// summed axes of 64 to 10240 and 56 to 12288 features in 8 and 16 bits, with operands from memory; over these the choice
+// is on average 1.4% slower than the best one.
 struct Choice {
     int pair_features;   // of a tile of the pairs' kernel, 0: the tile kernel
     int tokens, splits;  // of its tiles and clusters
@@ -435,6 +435,8 @@ Choice choose(const LinearArgs& a, int sms) {
     const bool f32 = a.out_dtype == GEOCACHE_F32;
     const int chunks = (int)(((long long)a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) + kRowBytes - 1) / kRowBytes);
     auto tiles = [](long long n, int per) { return (double)((n + per - 1) / per); };
+    // operands in MB, of which the first wait for memory
+    const double mb = 1e-6 * a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) * (double)(a.T + (long long)a.N * (a.gated ? 2 : 1));
     Choice c{};
     double best = 1e30;
     auto take = [&](double us, Choice to) {
@@ -447,21 +449,21 @@ Choice choose(const LinearArgs& a, int sms) {
         if (tokens > 16 && tokens / 2 >= a.T) break;
         for (int splits = 1; splits <= 8; ++splits) {
             if (splits > 1 && (tokens > 64 || splits > chunks)) break;
-            // blocks an SM, of which two run beside each other: the second adds 0.78 of the first's time
+            // blocks an SM, of which two run beside each other: the second adds 0.58 of the first's time
             const double r = tiles(a.T, tokens) * tiles(a.N, a.gated ? kFeatures / 2 : kFeatures) * splits / sms;
-            const double rounds = r <= 1 ? 1 : r <= 2 ? 1 + 0.78 * (r - 1) : 0.89 * r;
+            const double rounds = r <= 1 ? 1 : r <= 2 ? 1 + 0.58 * (r - 1) : 0.79 * r;
             const int per = (chunks + splits - 1) / splits;
-            const double chunk = (kFeatures + tokens) * 0.00163;
-            take(2.5 + (splits > 1 ? 0.63 + 0.042 * splits : 0) +
-                     rounds * (per * (chunk > 0.054 ? chunk : 0.054) + tokens * (0.034 + 0.0045 / splits)),
+            const double chunk = (kFeatures + tokens) * 0.00153;
+            take(1.14 + 0.0925 * mb + (splits > 1 ? 1.2 + 0.08 * splits : 0) +
+                     rounds * (per * (chunk > 0.101 ? chunk : 0.101) + tokens * (0.0391 + 0.0166 / splits)),
                  {0, tokens, splits});
         }
     }
     for (int features = 128; features <= (f32 ? 128 : 256); features += 128) {
         const double n = tiles(a.T, 256) * tiles(a.N, a.gated ? features / 2 : features);
-        const double rounds = tiles((long long)n, sms / 2), finish = features == 256 ? 2.7 : f32 ? 3.0 : 1.5;
-        const double sums = chunks * (features == 256 ? 0.34 : f32 ? 0.27 : 0.235);
-        if (n < 2e9) take(5.5 + rounds * (sums > finish ? sums : finish), {features, 0, 0});
+        const double rounds = tiles((long long)n, sms / 2), finish = features == 256 ? 2.94 : f32 ? 2.62 : 1.48;
+        const double sums = chunks * (features == 256 ? 0.281 : f32 ? 0.182 : 0.169);
+        if (n < 2e9) take(4.73 + 0.0571 * mb + rounds * (sums > finish ? sums : finish), {features, 0, 0});
     }
     return c;
 }
