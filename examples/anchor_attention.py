@@ -3,10 +3,12 @@
 Full steps run the block on all views; cached steps run it on the anchors alone (Sec. 3.2, batch-sliced anchor forward):
 their rows are packed, keep the rotary slots of the N-view layout, and attend to each other inside their asset; the
 library transports their change to the other views.  Background tokens take no part, so each asset is a packed sequence
-of its own length.  The projections are torch products; the norms with the rotation, the attention, the packing, the
-transport and the reconstruction are the library's.
+of its own length.  The projections of the latents are torch products (their few channels are no whole 16-byte words);
+the norms with the rotation, the attention, the packing, the transport and the reconstruction are the library's.  With
+--ff a gated feed-forward stands behind the attention: the library's norm and products, with --eight-bit on 8-bit rows.
 
     python examples/anchor_attention.py [--workload hunyuan64] [--assets 2] [--heads 8] [--dim 64] [--steps 10]
+                                        [--ff 2048 [--eight-bit]]
 """
 import argparse
 import os
@@ -36,9 +38,9 @@ def rotary_table(N, H, W, D):
 
 
 class Block:
-    """x0 of the views that are given: latents -> heads -> attention inside each asset -> latents."""
+    """x0 of the views that are given: latents -> heads -> attention inside each asset (-> feed-forward) -> latents."""
 
-    def __init__(self, w, heads, kv_heads, D, seed=0):
+    def __init__(self, w, heads, kv_heads, D, seed=0, ff=0, eight_bit=False):
         self.w, self.Hq, self.Hk, self.D = w, heads, kv_heads, D
         g = torch.Generator(device="cuda").manual_seed(seed)
         r = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
@@ -48,6 +50,16 @@ class Block:
         self.table = rotary_table(w.N, w.H, w.W, D)
         self.pos = torch.from_numpy(w.pos).cuda()
         self.valid = torch.from_numpy(w.valid).cuda()
+        self.ff, self.eight_bit = ff, eight_bit
+        if ff:
+            M = heads * D
+            self.norm_weight = 1 + 0.1 * r(M)
+            self.up = (r(2 * ff, M) / M ** 0.5).to(torch.bfloat16)       # values, then gates
+            self.down = (r(M, ff) / ff ** 0.5).to(torch.bfloat16)
+            self.up_scale = self.down_scale = None
+            if eight_bit:
+                self.up, self.up_scale = gc.quantize_rows(self.up)
+                self.down, self.down_scale = gc.quantize_rows(self.down)
         self.kept = {}  # token lists and plans of the view sets that the rotation comes back to
 
     def rows(self, views):
@@ -77,15 +89,26 @@ class Block:
         qkv = (features @ self.into).view(-1, self.Hq + 2 * self.Hk, self.D)
         return qkv, place, slots, plan
 
+    def feed_forward(self, rows):
+        """rows + down(values * gelu(gates)) for the rows' norm."""
+        normed, scale, _ = gc.add_rms_norm(rows, weight=self.norm_weight, quantize=self.eight_bit)
+        hidden = gc.linear(normed, self.up, activation="gelu", gated=True, x_scale=scale, weight_scale=self.up_scale)
+        scale = None
+        if self.eight_bit:
+            hidden, scale = gc.quantize_rows(hidden)
+        return gc.linear(hidden, self.down, residual=rows, x_scale=scale, weight_scale=self.down_scale)
+
     def __call__(self, x, views):
         views = tuple(views)
         w, Hq, Hk = self.w, self.Hq, self.Hk
         qkv, place, slots, plan = self.qkv(x, views)
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
         gc.qk_norm_rope(q, k, self.table, slots, self.q_weight, self.k_weight, q_out=q, k_out=k)  # in place
-        out = gc.attention(plan, q, k, v)
+        out = gc.attention(plan, q, k, v).reshape(len(place), -1)
+        if self.ff:
+            out = self.feed_forward(out)
         x0 = torch.zeros((w.B * len(views) * w.H * w.W, w.C), device="cuda")
-        x0[place] = (out.reshape(len(place), -1) @ self.back).float()
+        x0[place] = (out @ self.back).float()
         return x0.view(w.B, len(views), w.H, w.W, w.C).permute(0, 1, 4, 2, 3).contiguous()
 
 
@@ -120,9 +143,11 @@ def main():
     ap.add_argument("--kv-heads", type=int, default=0, help="default: --heads")
     ap.add_argument("--dim", type=int, default=64)
     ap.add_argument("--steps", type=int, default=10)
+    ap.add_argument("--ff", type=int, default=0, help="hidden width of a gated feed-forward (0: none)")
+    ap.add_argument("--eight-bit", action="store_true", help="the feed-forward on 8-bit rows and weights")
     o = ap.parse_args()
     w = synth.make_workload(o.workload, B=o.assets)
-    block = Block(w, o.heads, o.kv_heads or o.heads, o.dim)
+    block = Block(w, o.heads, o.kv_heads or o.heads, o.dim, ff=o.ff, eight_bit=o.eight_bit)
     run(block, o.steps)
     gc.device_status()
     torch.cuda.synchronize()
