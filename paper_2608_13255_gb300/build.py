@@ -102,6 +102,7 @@ def _build_locked(verbose, extra_flags) -> str:
     binding_obj = os.path.join(LIBDIR, "geocache_rows_binding.o")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE, "-I", os.path.join(torch_dir, "include"),
            "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(cc))), "include"),
            "-I", sysconfig.get_paths()["include"], "-c", _binding_source(), "-o", binding_obj]
     procs.append((_binding_source(), subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = []
@@ -118,7 +119,7 @@ def _build_locked(verbose, extra_flags) -> str:
     os.replace(tmp, LIB)
     tmp = BINDING + ".tmp%d" % os.getpid()
     subprocess.check_call(["g++", "-shared", "-o", tmp, binding_obj, "-L", LIBDIR, "-lgeocache", "-Wl,-rpath,$ORIGIN",
-                           "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+                           "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
     os.replace(tmp, BINDING)
     return LIB
 

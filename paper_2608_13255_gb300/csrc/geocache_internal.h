@@ -180,8 +180,9 @@ struct NormRowsArgs {
     long long T;
     int C, norm, dtype, residual_f32;
     float eps;
-    // set by the launch: threads of a row, which rows are whole words, 1 / C
-    int lanes, x_words, residual_words, out_words, weight_words;
+    // set by the launch: threads of a row, the first distance of its warps' join, which rows are whole
+    // words, 1 / C
+    int lanes, join, x_words, residual_words, out_words, weight_words;
     float inv_C;
 };
 cudaError_t launch_norm_rows(const NormRowsArgs& a, cudaStream_t s);

@@ -136,7 +136,7 @@ __device__ __forceinline__ void set_pair(Raw<T>& r, int i, float2 v) {
 }
 
 // ------------------------------------------------------------------ rows --
-// A row has `lanes` threads (a power of two) and kPieces pieces of 8 elements a thread, its pieces side by side over its
+// A row has `lanes` threads (a power of two up to 32, then whole warps) and kPieces pieces of 8 elements a thread, its pieces side by side over its
 // threads; a block has threads / lanes rows at a time, and stays.  Up to two pieces, a thread asks for those of its next
 // row before it finishes this one.
 enum { kNone, kSame, kF32 };
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
     constexpr bool kAhead = kPieces <= 2;
     constexpr int kRes = kResidual == kNone ? 1 : kPieces;
     __shared__ float2 shared[2][32];
-    const int lane = threadIdx.x & (a.lanes - 1), row_in = threadIdx.x / a.lanes, rows = blockDim.x / a.lanes;
+    const int row_in = threadIdx.x / a.lanes, lane = threadIdx.x - row_in * a.lanes, rows = blockDim.x / a.lanes;
     const long long step = (long long)gridDim.x * rows;
     long long row = (long long)blockIdx.x * rows + row_in;
     int n_of[kPieces];
@@ -231,13 +231,15 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
         };
         join(min(16, a.lanes / 2));
         if (a.lanes > 32) {
-            const int warps = a.lanes / 32, warp = threadIdx.x / 32;   // (a power of two)
-            if ((threadIdx.x & 31) == 0) shared[turn][warp] = make_float2(sum, top);
+            const int warps = a.lanes / 32, warp = threadIdx.x / 32, own = threadIdx.x & 31;
+            if (own == 0) shared[turn][warp] = make_float2(sum, top);
             __syncthreads();   // (once a row: the row after next finds this half read)
-            const float2 s = shared[turn][row_in * warps + (threadIdx.x & (warps - 1))];
+            const float2 s = own < warps ? shared[turn][row_in * warps + own] : make_float2(0.0f, 0.0f);
             sum = s.x;
             top = s.y;
-            join(warps / 2);   // in one order for all threads of the row
+            join(a.join);   // in one order for all threads of the row
+            sum = __shfl_sync(0xffffffffu, sum, 0);
+            top = __shfl_sync(0xffffffffu, top, 0);
         }
         const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
         float g = f;   // what an element is multiplied by
@@ -285,19 +287,19 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
 template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
 cudaError_t launch(const NormRowsArgs& a, int threads, cudaStream_t s) {
     auto kern = norm_rows_kernel<X, kResidual, kNorm, kQuant, kPieces>;
-    static int resident[3];   // blocks of 256, 512 and 1024 threads that the device holds
+    static int resident[33];   // blocks of that many warps that the device holds
     static const cudaError_t ready = [&] {
         int device = 0, sms = 0;
         cudaError_t e = cudaGetDevice(&device);
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-        for (int i = 0; i < 3 && e == cudaSuccess && kThreads << i <= most_threads(kPieces); ++i) {
-            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[i], kern, kThreads << i, 0);
+        for (int i = 1; e == cudaSuccess && 32 * i <= most_threads(kPieces); ++i) {
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[i], kern, 32 * i, 0);
             resident[i] *= sms;
         }
         return e;
     }();
     if (ready != cudaSuccess) return ready;
-    const long long rows = threads / a.lanes, blocks = (a.T + rows - 1) / rows, most = resident[threads / kThreads / 2];
+    const long long rows = threads / a.lanes, blocks = (a.T + rows - 1) / rows, most = resident[threads / 32];
     return launch_pdl(kern, dim3((unsigned)(blocks < most ? blocks : most)), threads, 0, s, a);
 }
 
@@ -344,15 +346,20 @@ cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
     a.out_words = words(a.out, a.scale ? 1 : eb);   // (8-bit rows: whole words of 8)
     a.weight_words = !((uintptr_t)a.weight % 16);
     a.inv_C = 1.0f / (float)a.C;
+    // Rows over 256 elements have two pieces a thread or more: fewer joins an element (1600 elements in 7 warps of one
+    // piece a thread 20.6 us, in 4 warps of two 19.7, though a fifth of these has no work).
     const int n = (a.C + 7) / 8;
-    int pieces = 1, lanes = 1;
-    while (lanes < 32 && lanes < n) lanes *= 2;
-    while (lanes * pieces < n) {
-        if (pieces < 2 || lanes == most_threads(pieces)) pieces *= 2;
-        else lanes *= 2;
+    int pieces = n <= 32 ? 1 : n <= 2 * most_threads(2) ? 2 : n <= 4 * most_threads(4) ? 4 : 8;
+    int lanes = 1;
+    if (n <= 32) {
+        while (lanes < n) lanes *= 2;
+    } else {
+        lanes = (n + 32 * pieces - 1) / (32 * pieces) * 32;
     }
     a.lanes = lanes;
-    const int threads = lanes > kThreads ? lanes : kThreads;
+    a.join = 1;
+    while (2 * a.join < lanes / 32) a.join *= 2;
+    const int threads = lanes > kThreads ? lanes : kThreads / lanes * lanes;
     if (a.dtype == GEOCACHE_BF16) return launch_type<__nv_bfloat16>(a, pieces, threads, s);
     if (a.dtype == GEOCACHE_F16) return launch_type<__half>(a, pieces, threads, s);
     return launch_type<float>(a, pieces, threads, s);

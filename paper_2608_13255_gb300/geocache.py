@@ -753,12 +753,7 @@ def _rows_binding():
 
 def _handle(stream):
     """A stream's handle as an integer."""
-    if stream is None and torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    if stream is None or isinstance(stream, torch.cuda.Stream):
-        # (without a device the call is refused for its tensors)
-        return 0 if stream is None else stream.cuda_stream
-    return int(stream)
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
 
 def _tensor(x, name):
@@ -786,7 +781,8 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, out=None, scale=None, 
         scale = _empty((_tensor(x, "x").shape[0],), torch.float32, x.device, stream)
     if residual is not None and residual_out is None:
         residual_out = _empty(_tensor(x, "x").shape, _tensor(residual, "residual").dtype, x.device, stream)
-    _check((_ROWS or _rows_binding()).add_rms_norm(x, residual, weight, eps, out, scale, residual_out, _handle(stream)))
+    _check((_ROWS or _rows_binding()).add_rms_norm(x, residual, weight, eps, out, scale, residual_out,
+                                                   None if stream is None else _handle(stream)))
     return out, scale, residual_out
 
 
@@ -798,7 +794,7 @@ def quantize_rows(x, out=None, scale=None, stream=None):
         out = _empty(_tensor(x, "x").shape, _E4M3, x.device, stream)
     if scale is None:
         scale = _empty((_tensor(x, "x").shape[0],), torch.float32, x.device, stream)
-    _check((_ROWS or _rows_binding()).quantize_rows(x, out, scale, _handle(stream)))
+    _check((_ROWS or _rows_binding()).quantize_rows(x, out, scale, None if stream is None else _handle(stream)))
     return out, scale
 
 
@@ -822,7 +818,7 @@ def linear(x, weight, bias=None, activation=None, gated=False, residual=None, x_
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise TypeError("out must be %s (got %s)" % (out_dtype, out.dtype))
     _check((_ROWS or _rows_binding()).linear(x, weight, bias, _ACTIVATIONS[activation], gated, residual, x_scale,
-                                             weight_scale, out, _handle(stream)))
+                                             weight_scale, out, None if stream is None else _handle(stream)))
     return out
 
 
