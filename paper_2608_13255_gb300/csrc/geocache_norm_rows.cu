@@ -137,15 +137,17 @@ __device__ __forceinline__ void set_pair(Raw<T>& r, int i, float2 v) {
 
 // ------------------------------------------------------------------ rows --
 // A row has `lanes` threads (a power of two up to 32, then whole warps) and kPieces pieces of 8 elements a thread, its pieces side by side over its
-// threads; a block has threads / lanes rows at a time, and stays.  Up to two pieces, a thread asks for those of its next
-// row before it finishes this one.
+// threads; a block has threads / lanes rows at a time, and stays.  Up to two pieces (four of norms whose registers hold
+// them), a thread asks for those of its next row before it finishes this one.
 enum { kNone, kSame, kF32 };
+// whether the registers hold four pieces of this row and of the next
+constexpr bool four_ahead(int size, int residual) { return residual == kNone || (size == 2 && residual == kSame); }
 constexpr int most_threads(int pieces) { return pieces == 8 ? 1024 : 512; }
 
 template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
 __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const __grid_constant__ NormRowsArgs a) {
     using R = typename std::conditional<kResidual == kF32, float, X>::type;
-    constexpr bool kAhead = kPieces <= 2;
+    constexpr bool kAhead = kPieces <= 2 || (kPieces == 4 && four_ahead(sizeof(X), kResidual));
     constexpr int kRes = kResidual == kNone ? 1 : kPieces;
     __shared__ float2 shared[2][32];
     const int row_in = threadIdx.x / a.lanes, lane = threadIdx.x - row_in * a.lanes, rows = blockDim.x / a.lanes;
@@ -350,6 +352,11 @@ cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
     // piece a thread 20.6 us, in 4 warps of two 19.7, though a fifth of these has no work).
     const int n = (a.C + 7) / 8;
     int pieces = n <= 32 ? 1 : n <= 2 * most_threads(2) ? 2 : n <= 4 * most_threads(4) ? 4 : 8;
+    // Norms of many rows are bound by instructions, of which four pieces have fewer (44943 x 2048 bf16 with residual into 8
+    // bits 110 -> 103 us, 11772 x 1808 without 21.3 -> 18.6); few rows leave SMs idle (1569 x 592 3.2 -> 3.5), and 8-bit
+    // rows without a norm are bound by memory (8192 x 2048 10.1 -> 11.1).
+    if (pieces == 2 && n > 64 && a.norm && a.T >= 3000 && four_ahead(eb, !a.residual.data ? kNone : eb == 2 && !a.residual_f32 ? kSame : kF32))
+        pieces = 4;
     int lanes = 1;
     if (n <= 32) {
         while (lanes < n) lanes *= 2;

@@ -211,3 +211,21 @@ def test_offsets_past_32_bits(gc):
     want = gc.add_rms_norm(src)[0]
     gc.add_rms_norm(x, out=x)
     assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,C", [(2999, 520), (3001, 520), (3100, 1811), (4000, 8184)])
+def test_many_rows(gc, T, C, dtype):
+    # the division of a row over threads depends on the number of rows
+    x, res, w = _randn((T, C), 1, dtype), _randn((T, C), 2, dtype), 1 + 0.1 * _randn((C,), 3, torch.float32)
+    for residual in (None, res):
+        h = x if residual is None else (x.float() + res.float()).to(dtype)
+        y = _norm(h, w, 1e-5)
+        out, _, ro = gc.add_rms_norm(x, residual, w, 1e-5)
+        _check(out, y, dtype)
+        assert residual is None or torch.equal(ro, h)
+        q, scale, _ = gc.add_rms_norm(x, residual, w, 1e-5, quantize=True)
+        _check_quantised(q, scale, y, F32)
+        # few of the rows by themselves: the other division, sums in another order
+        some = gc.add_rms_norm(x[:50], None if residual is None else residual[:50], w, 1e-5)[0]
+        _check(some, y[:50], dtype)
