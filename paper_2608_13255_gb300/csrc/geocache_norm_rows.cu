@@ -24,6 +24,7 @@ namespace geocache {
 namespace {
 
 constexpr int kThreads = 256;   // of a block, or as many as a wide row takes
+constexpr int kSpread = 152;    // blocks that few rows are spread over: an SM each
 constexpr float kLargest = 448.0f, kTiny = 0x1p-126f;  // of e4m3; the least scale (the least normal number)
 
 // the larger of a and |b|; a NaN stays
@@ -366,7 +367,10 @@ cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
     a.lanes = lanes;
     a.join = 1;
     while (2 * a.join < lanes / 32) a.join *= 2;
-    const int threads = lanes > kThreads ? lanes : kThreads / lanes * lanes;
+    // few rows spread over the SMs
+    const long long spread = (a.T + kSpread - 1) / kSpread;
+    int threads = lanes > kThreads ? lanes : kThreads / lanes * lanes;
+    if (spread * lanes < threads) threads = (int)((spread * lanes + 31) / 32 * 32);
     if (a.dtype == GEOCACHE_BF16) return launch_type<__nv_bfloat16>(a, pieces, threads, s);
     if (a.dtype == GEOCACHE_F16) return launch_type<__half>(a, pieces, threads, s);
     return launch_type<float>(a, pieces, threads, s);
