@@ -145,6 +145,29 @@ enum { kNone, kSame, kF32 };
 constexpr bool four_ahead(int size, int residual) { return residual == kNone || (size == 2 && residual == kSame); }
 constexpr int most_threads(int pieces) { return pieces == 8 ? 1024 : 512; }
 
+// sum h^2 and max |h w| of a row from its threads', in one order for all of them
+template <bool kNorm, bool kQuant>
+__device__ __forceinline__ void join_row(float& sum, float& top, const NormRowsArgs& a, float2* shared, int row_in) {
+    auto join = [&](int from) {
+        for (int d = from; d > 0; d >>= 1) {
+            if (kNorm) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (kQuant) top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, d));
+        }
+    };
+    join(min(16, a.lanes / 2));
+    if (a.lanes > 32) {
+        const int warps = a.lanes / 32, warp = threadIdx.x / 32, own = threadIdx.x & 31;
+        if (own == 0) shared[warp] = make_float2(sum, top);
+        __syncthreads();   // (once a row: the row after next finds this half read)
+        const float2 s = own < warps ? shared[row_in * warps + own] : make_float2(0.0f, 0.0f);
+        sum = s.x;
+        top = s.y;
+        join(a.join);
+        sum = __shfl_sync(0xffffffffu, sum, 0);
+        top = __shfl_sync(0xffffffffu, top, 0);
+    }
+}
+
 template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
 __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const __grid_constant__ NormRowsArgs a) {
     using R = typename std::conditional<kResidual == kF32, float, X>::type;
@@ -226,24 +249,7 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
             }
         }
         float sum = sums.x + sums.y;
-        auto join = [&](int from) {
-            for (int d = from; d > 0; d >>= 1) {
-                if (kNorm) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (kQuant) top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, d));
-            }
-        };
-        join(min(16, a.lanes / 2));
-        if (a.lanes > 32) {
-            const int warps = a.lanes / 32, warp = threadIdx.x / 32, own = threadIdx.x & 31;
-            if (own == 0) shared[turn][warp] = make_float2(sum, top);
-            __syncthreads();   // (once a row: the row after next finds this half read)
-            const float2 s = own < warps ? shared[turn][row_in * warps + own] : make_float2(0.0f, 0.0f);
-            sum = s.x;
-            top = s.y;
-            join(a.join);   // in one order for all threads of the row
-            sum = __shfl_sync(0xffffffffu, sum, 0);
-            top = __shfl_sync(0xffffffffu, top, 0);
-        }
+        join_row<kNorm, kQuant>(sum, top, a, shared[turn], row_in);
         const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
         float g = f;   // what an element is multiplied by
         if (kQuant) {
@@ -287,28 +293,122 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
     }
 }
 
+// The same for rows that are no whole words: a thread has kCount elements `lanes` apart, so that a warp's loads and stores
+// lie along the row.  24576 x 2047 bf16 with residual into 8 bits: 132 us, with eight elements side by side a thread, each
+// moved by itself, 271.  (Narrow rows keep the latter: 20000 x 263 into 8 bits 8.7 us, like this 10.0.)
+constexpr int most_element_threads(int count) { return count == 64 ? 1024 : 512; }
+
+template <typename X, int kResidual, bool kNorm, bool kQuant, int kCount>
+__global__ void __launch_bounds__(most_element_threads(kCount)) norm_elements_kernel(const __grid_constant__ NormRowsArgs a) {
+    using R = typename std::conditional<kResidual == kF32, float, X>::type;
+    constexpr bool kAhead = kCount == 16;
+    constexpr int kRes = kResidual == kNone ? 1 : kCount;
+    __shared__ float2 shared[2][32];
+    const int row_in = threadIdx.x / a.lanes, lane = threadIdx.x - row_in * a.lanes, rows = blockDim.x / a.lanes;
+    const long long step = (long long)gridDim.x * rows;
+    long long row = (long long)blockIdx.x * rows + row_in;
+    const int n = (a.C - lane + a.lanes - 1) / a.lanes;   // elements of this thread (may be below 1)
+    X x[kCount];
+    R res[kRes];
+    const X* from = static_cast<const X*>(a.x.data) + row * a.x.stride + lane;
+    const R* from_res = static_cast<const R*>(a.residual.data) + row * a.residual.stride + lane;
+    auto load = [&](bool inside) {
+        const int in = inside ? n : 0;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            x[i] = i < in ? from[i * a.lanes] : X(0.0f);
+            if constexpr (kResidual != kNone) res[i] = i < in ? from_res[i * a.lanes] : R(0.0f);
+        }
+        from += step * a.x.stride;
+        if (kResidual != kNone) from_res += step * a.residual.stride;
+    };
+    pdl_wait();
+    if (kAhead) load(row < a.T);
+    for (int turn = 0; row - row_in < a.T; row += step, turn ^= 1) {
+        const int in = row < a.T ? n : 0;
+        if (!kAhead) load(in != 0);
+        float v[kCount], sum = 0.0f, top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            v[i] = (float)x[i];
+            if constexpr (kResidual != kNone) {
+                const R stored = (R)(v[i] + (float)res[i]);
+                if (i < in) static_cast<R*>(a.residual_out.data)[row * a.residual_out.stride + lane + i * a.lanes] = stored;
+                v[i] = (float)stored;
+            }
+        }
+        if (kAhead) load(row + step < a.T);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            if (kNorm) {
+                sum = fmaf(v[i], v[i], sum);
+                if (a.weight && i < n) v[i] *= __ldca(a.weight + lane + i * a.lanes);
+            }
+            if (kQuant) top = max_abs(top, v[i]);
+        }
+        join_row<kNorm, kQuant>(sum, top, a, shared[turn], row_in);
+        const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
+        float inv = 1.0f;
+        if (kQuant) {
+            const float s = top * f * (1.0f / kLargest);
+            const float scale = s < kTiny ? kTiny : s;  // (a NaN stays)
+            if (lane == 0 && row < a.T) a.scale[row] = scale;
+            inv = __fdividef(1.0f, scale);  // (scale < 2^126)
+        }
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            if (kNorm) v[i] *= f;
+            if constexpr (kQuant) {
+                const uint32_t q = pack_e4m3(make_float2(v[i] * inv, 0.0f), make_float2(0.0f, 0.0f));
+                if (i < in) static_cast<uint8_t*>(a.out.data)[row * a.out.stride + lane + i * a.lanes] = (uint8_t)q;
+            } else {
+                if (i < in) static_cast<X*>(a.out.data)[row * a.out.stride + lane + i * a.lanes] = (X)v[i];
+            }
+        }
+    }
+}
+
+template <typename... Kernel>
+cudaError_t launch_resident(void (*kern)(Kernel...), const NormRowsArgs& a, int threads, int resident, cudaStream_t s) {
+    const long long rows = threads / a.lanes, blocks = (a.T + rows - 1) / rows;
+    return launch_pdl(kern, dim3((unsigned)(blocks < resident ? blocks : resident)), threads, 0, s, a);
+}
+
+// the blocks of each number of warps that the device holds
+template <typename F>
+cudaError_t residents(F kern, int most, int* resident) {
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    for (int i = 1; e == cudaSuccess && 32 * i <= most; ++i) {
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[i], kern, 32 * i, 0);
+        resident[i] *= sms;
+    }
+    return e;
+}
+
 template <typename X, int kResidual, bool kNorm, bool kQuant, int kPieces>
 cudaError_t launch(const NormRowsArgs& a, int threads, cudaStream_t s) {
     auto kern = norm_rows_kernel<X, kResidual, kNorm, kQuant, kPieces>;
-    static int resident[33];   // blocks of that many warps that the device holds
-    static const cudaError_t ready = [&] {
-        int device = 0, sms = 0;
-        cudaError_t e = cudaGetDevice(&device);
-        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-        for (int i = 1; e == cudaSuccess && 32 * i <= most_threads(kPieces); ++i) {
-            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[i], kern, 32 * i, 0);
-            resident[i] *= sms;
-        }
-        return e;
-    }();
-    if (ready != cudaSuccess) return ready;
-    const long long rows = threads / a.lanes, blocks = (a.T + rows - 1) / rows, most = resident[threads / 32];
-    return launch_pdl(kern, dim3((unsigned)(blocks < most ? blocks : most)), threads, 0, s, a);
+    static int resident[33];
+    static const cudaError_t ready = residents(kern, most_threads(kPieces), resident);
+    return ready != cudaSuccess ? ready : launch_resident(kern, a, threads, resident[threads / 32], s);
+}
+
+template <typename X, int kResidual, bool kNorm, bool kQuant, int kCount>
+cudaError_t launch_elements(const NormRowsArgs& a, int threads, cudaStream_t s) {
+    auto kern = norm_elements_kernel<X, kResidual, kNorm, kQuant, kCount>;
+    static int resident[33];
+    static const cudaError_t ready = residents(kern, most_element_threads(kCount), resident);
+    return ready != cudaSuccess ? ready : launch_resident(kern, a, threads, resident[threads / 32], s);
 }
 
 template <typename X, int kResidual, bool kNorm, bool kQuant>
 cudaError_t launch_pieces(const NormRowsArgs& a, int pieces, int threads, cudaStream_t s) {
     switch (pieces) {
+        case -16: return launch_elements<X, kResidual, kNorm, kQuant, 16>(a, threads, s);
+        case -32: return launch_elements<X, kResidual, kNorm, kQuant, 32>(a, threads, s);
+        case -64: return launch_elements<X, kResidual, kNorm, kQuant, 64>(a, threads, s);
         case 1: return launch<X, kResidual, kNorm, kQuant, 1>(a, threads, s);
         case 2: return launch<X, kResidual, kNorm, kQuant, 2>(a, threads, s);
         case 4: return launch<X, kResidual, kNorm, kQuant, 4>(a, threads, s);
@@ -363,6 +463,12 @@ cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
         while (lanes < n) lanes *= 2;
     } else {
         lanes = (n + 32 * pieces - 1) / (32 * pieces) * 32;
+    }
+    if (a.C > 512 && (!a.x_words || !a.out_words || (a.residual.data && !a.residual_words))) {   // (a negative number: single elements)
+        pieces = a.C <= 16 * most_element_threads(16) ? -16 : a.C <= 32 * most_element_threads(32) ? -32 : -64;
+        lanes = 1;
+        while (lanes < 32 && lanes * -pieces < a.C) lanes *= 2;
+        if (lanes * -pieces < a.C) lanes = (a.C + 32 * -pieces - 1) / (32 * -pieces) * 32;
     }
     a.lanes = lanes;
     a.join = 1;

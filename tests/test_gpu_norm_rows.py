@@ -229,3 +229,24 @@ def test_many_rows(gc, T, C, dtype):
         # few of the rows by themselves: the other division, sums in another order
         some = gc.add_rms_norm(x[:50], None if residual is None else residual[:50], w, 1e-5)[0]
         _check(some, y[:50], dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,C", [(40, 513), (700, 1031), (5, 8191), (9, 8193), (3, 16383), (3, 16385), (2, 65535)])
+def test_rows_that_are_no_whole_words(gc, T, C, dtype):
+    # single elements, from and into rows at every alignment, with a residual in place
+    x = _randn((T, C + 3), 1, dtype)[:, 1:1 + C]
+    res, w = _randn((T, C), 2, dtype), 1 + 0.1 * _randn((C,), 3, torch.float32)
+    for residual in (None, res, res.float() * 1.001):
+        h = x if residual is None else (x.float() + residual.float()).to(residual.dtype)
+        y = _norm(h, w, 1e-5)
+        kept = None if residual is None else residual.clone()
+        out = torch.full((T, C + 5), 7.0, device=DEV, dtype=dtype)
+        gc.add_rms_norm(x, kept, w, 1e-5, out=out[:, 2:2 + C], residual_out=kept)
+        _check(out[:, 2:2 + C], y, dtype)
+        assert (out[:, :2] == 7).all() and (out[:, 2 + C:] == 7).all()
+        assert residual is None or torch.equal(kept, h)
+        q, scale, _ = gc.add_rms_norm(x, residual, w, 1e-5, quantize=True)
+        _check_quantised(q, scale, y, F32)
+    q, scale = gc.quantize_rows(x)
+    _check_quantised(q, scale, x.double(), 0.0)
