@@ -11,9 +11,15 @@ namespace geocache {
 namespace {
 
 // The two blocks of a cluster hold 128 tokens each and half of the tile's weights each; one thread of the first issues
-// products over both (cta_group::2), so an SM reads 3/4 of the operand bytes that a tile of its own would take (and
-// copies half the weights).  A block runs over many tiles: warps 0 to 7 finish a tile while the next one's products fill
-// the other half of tensor memory.  Tokens are the lanes of tensor memory: a thread finishes a token's columns.
+// products over both (cta_group::2), so an SM copies and reads two thirds of the operand bytes that a tile of 128 x 256 of
+// its own would take.  A block runs over many tiles: warps 0 to 7 finish a tile while the next one's products fill the
+// other half of tensor memory.  Tokens are the lanes of tensor memory: a thread finishes a token's columns.
+//
+// Bound by the tensor cores: a chunk of 256 x 256 takes the 512 cycles of its products, whose operands' copies (32 KB an SM)
+// are 870 cycles on their way and six of them in flight.  24576 x 2048 x 6144 bf16 308 us where the card may run at its
+// burst clock (2,010 TFLOP/s; the library's product 313 to 318), 357 back to back under the power cap (1,730).  What did
+// not help: asking L2 for the chunks ahead of the copies (355 -> 385 us), bands of 8 or 16 token tiles instead of 4 (347 ->
+// 369), waits and arrivals with the scope of the cluster (355 -> 888: each flushes).
 constexpr int kTokens = 256;               // of a tile: 128 of each block
 constexpr int kFinishWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 32 * 10;
 constexpr int kMostStages = 6;

@@ -5,8 +5,8 @@
 // One pass: a row stays in the registers of the threads that read it, and its two statistics, sum h^2 and max |h w|, are
 // taken in one round: max |y| = r max |h w|, since r does not depend on the element.  Sums are binary32.
 //
-// Bound by memory on paper (bf16 with residual into 8 bits: 7 bytes and some 10 instructions an element), and by the
-// instructions in a first form with 40 an element (95 us for 24576 rows of 2048 in bf16 with residual into 8 bits).
+// Bound by memory on paper (bf16 with residual into 8 bits: 7 bytes an element), and by the instructions in a first form
+// with 40 an element: 24576 rows of 2048 in bf16 with residual into 8 bits took 95 us, with half as many 59 (5.9 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
