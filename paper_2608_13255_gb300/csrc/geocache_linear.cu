@@ -32,6 +32,7 @@ struct Params {
     uint32_t columns;  // of tensor memory
     uint32_t idesc;
     int few;           // blocks: at most half of the SMs
+    int features;      // of a tile of the kernel for few features
     int out_wide, residual_wide;   // four elements of a row are one aligned word
 };
 
@@ -386,6 +387,183 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     leave();
 }
 
+// --------------------------------------------------------- few features --
+// Many tokens and at most 64 features: the bound is the reading of the tokens' rows, once.  Here the tokens are the lanes
+// of tensor memory and the features its columns, so that no product is of rows that are not there, and up to three blocks
+// an SM, not persistent, keep the memory busy where the tiles are no whole rounds of the SMs: 24576 x 2048 x 64 bf16 (192
+// tiles) into f32 takes 22 us (4.6 TB/s with the launch and its ends), on pairs of SMs 26; 44943 tokens into bf16 34, with
+// two blocks an SM 38.  All blocks read the same weights at the same time, so a chunk of a block alone takes 0.23 us.
+constexpr int kNarrowTokens = 128, kNarrowFeatures = 64, kNarrowStages = 12, kNarrowThreads = 192, kNarrowBlocks = 3;   // (blocks an SM)
+
+struct NarrowBarriers {
+    uint64_t full[kNarrowStages], empty[kNarrowStages], sums[2], taken[2], done;
+    uint32_t tmem, dead;
+};
+
+template <typename Out, bool kEight>
+__global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
+    linear_narrow_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm) {
+    constexpr bool kParts = std::is_same<Out, float>::value;
+    constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;   // elements of a chunk
+    constexpr uint32_t x_bytes = kNarrowTokens * kRowBytes;
+    extern __shared__ uint8_t raw[];
+    __shared__ NarrowBarriers bars;
+    NarrowBarriers* b = &bars;
+    const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const unsigned long long limit = p.a.wait_limit_ns;
+    const long long first_token = (long long)blockIdx.x * kNarrowTokens;
+    const uint32_t stage_bytes = x_bytes + p.features * kRowBytes;
+
+    uint32_t stage = 0, phase = 0, armed = 0;   // of the loads
+    int c = 0;
+    auto next = [&]() {
+        ++c;
+        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+    };
+    auto copies = [&]() {
+        const uint32_t at = smem + stage * stage_bytes, bar = smem_u32(&b->full[stage]);
+        if (elect()) {
+            mbar_expect(&b->full[stage], stage_bytes);
+            tma_2d(at, &xm, c * kStep, (int)first_token, bar);
+            tma_2d(at + x_bytes, &wm, c * kStep, 0, bar);
+        }
+        __syncwarp();
+        armed |= 1u << stage;
+        next();
+    };
+    if (warp == kTileLoadWarp) {   // (the first copies leave before the block has its tensor memory, as above)
+        if (lane < p.stages) {
+            mbar_init(&b->full[lane], 1);
+            mbar_init(&b->empty[lane], 1);
+        } else if (lane >= 24 && lane < 26) {
+            mbar_init(&b->sums[lane - 24], 1);
+            mbar_init(&b->taken[lane - 24], 4);
+        } else if (lane == 26) {
+            mbar_init(&b->done, 1);
+            b->dead = 0;
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;\n fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        pdl_wait();
+        if (p.a.drop_first_copy && blockIdx.x == 0) next();
+        for (int i = (int)stage; i < p.stages && phase == 0 && c < p.chunks; ++i) copies();
+    } else if (warp == kTileMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b->tmem)), "r"(p.columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    const int units = p.features / 4, unit_f = (int)threadIdx.x % units * 4;   // (a power of two)
+    Epilogue e;
+    load_epilogue<false>(e, p.a, unit_f);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = (uint32_t)uniform((int)b->tmem);
+    if (p.few) pdl_launch_dependents();
+
+    if (warp == kTileLoadWarp) {
+        while (c < p.chunks && wait_warp(&b->empty[stage], phase ^ 1, limit, &b->dead)) copies();
+        // the copies in flight land before the block goes on
+        const unsigned long long t0 = globaltimer();
+        for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+            const uint32_t parity = s < stage ? phase : phase ^ 1;
+            while ((armed >> s & 1) && !mbar_try(&b->full[s], parity) && globaltimer() - t0 < kDrainLimitNs) {}
+        }
+    } else if (warp == kTileMmaWarp) {
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        for (int c = 0, part = 0; ok && c < p.chunks; ++part) {
+            if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead);
+            tc_after();   // (what was read from tensor memory)
+            const int end = kParts ? min(c + kPartChunks, p.chunks) : p.chunks;
+            uint32_t accumulate = 0;
+            for (; ok && c < end; ++c) {
+                ok = wait_warp(&b->full[stage], phase, limit, &b->dead);
+                if (!ok) break;
+                const uint32_t x = desc_low(smem + stage * stage_bytes);
+                if (elect()) {
+                    products<kEight, false>(tmem + (part & 1) * p.features, x, x + (x_bytes >> 4), p.idesc, accumulate);
+                    tc_commit(&b->empty[stage]);
+                }
+                __syncwarp();
+                accumulate = 1;
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            }
+            if (ok && elect()) tc_commit(&b->sums[part & 1]);
+            __syncwarp();
+        }
+        // every product is done before the block goes on, those too that were issued before a wait ran out
+        if (elect()) tc_commit(&b->done);
+        __syncwarp();
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try(&b->done, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+    } else if (warp < 4) {
+        const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
+        float acc[kNarrowFeatures] = {};
+        const long long token = first_token + threadIdx.x;
+        const float xs = p.a.x_scale && token < p.a.T ? __ldca(p.a.x_scale + token) : 1.0f;
+        const int parts = kParts ? (p.chunks + kPartChunks - 1) / kPartChunks : 1;
+        bool ok = true;
+        for (int part = 0; ok && part < parts; ++part) {
+            ok = wait_warp(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead);
+            tc_after();
+            if (ok) {
+#pragma unroll
+                for (int f = 0; f < kNarrowFeatures; f += 16)
+                    if (f < p.features) {
+                        uint32_t r[16];
+                        tmem_ld16(at + (part & 1) * p.features + f, r);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        asm volatile("" : GEOCACHE_PIN16(r));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[f + i] = kParts ? acc[f + i] + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+                    }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&b->taken[part & 1]);
+            }
+        }
+        // The stages are overwritten: the loads have landed, as the products that wait for them are done.  Four floats
+        // between the tokens, for other banks.
+        ok = __all_sync(0xffffffffu, ok && !*(volatile uint32_t*)&b->dead);
+        if (ok) {
+            const uint32_t row = smem + (warp * 32 + lane) * (p.features + 4) * 4;
+#pragma unroll
+            for (int f = 0; f < kNarrowFeatures; f += 4)
+                if (f < p.features)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(row + f * 4), "f"(acc[f] * xs), "f"(acc[f + 1] * xs),
+                                 "f"(acc[f + 2] * xs), "f"(acc[f + 3] * xs)
+                                 : "memory");
+        }
+        tc_before();
+    }
+    __syncthreads();
+    if (warp == kTileMmaWarp) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.columns) : "memory");
+    }
+    if (*(volatile uint32_t*)&b->dead) return;
+
+    const int n_in = min(4, p.a.N - unit_f), n_tok = n_in <= 0 ? 0 : (int)min((long long)kNarrowTokens, p.a.T - first_token);
+#pragma unroll 4
+    for (int t = (int)threadIdx.x / units; t < n_tok; t += kNarrowThreads / units) {
+        const long long token = first_token + t;
+        float res[4] = {};
+        if (p.a.residual.data)
+            load4(static_cast<const Out*>(p.a.residual.data) + token * p.a.residual.stride + unit_f, p.residual_wide, n_in, res);
+        float4 s;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(s.x), "=f"(s.y), "=f"(s.z), "=f"(s.w)
+                     : "r"(smem + (t * (p.features + 4) + unit_f) * 4));
+        float2 v[2] = {make_float2(s.x, s.y), make_float2(s.z, s.w)};
+        finish<false>(v, v, e, 1.0f, p.a.x_scale != nullptr, p.a.act);   // (the token's scale is in the sum)
+        const float y[4] = {v[0].x + res[0], v[0].y + res[1], v[1].x + res[2], v[1].y + res[3]};
+        store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + unit_f, p.out_wide, n_in, y);
+    }
+}
+
 // ----------------------------------------------------------------- host --
 constexpr int kTileSmem = 112 * 1024;   // two blocks an SM
 
@@ -418,8 +596,34 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
     return launch_cluster(kern, dim3((unsigned)columns, (unsigned)p.feature_tiles), kTileThreads, bytes + 1024, p.splits, s, p, wm, xm);
 }
 
+constexpr int kNarrowSmem = 227 * 1024;   // of an SM, with 1 KB beside each block's
+template <typename Out, bool kEight>
+cudaError_t launch_narrow(Params p, int sms, cudaStream_t s) {
+    auto kern = linear_narrow_kernel<Out, kEight>;
+    static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowSmem - 1024);
+    if (ready != cudaSuccess) return ready;
+    CUtensorMap wm, xm;
+    cudaError_t e = make_map(&wm, p.a.in_dtype, p.a.w, p.a.K, p.a.N, p.features);
+    if (e == cudaSuccess) e = make_map(&xm, p.a.in_dtype, p.a.x, p.a.K, p.a.T, kNarrowTokens);
+    if (e != cudaSuccess) return e;
+    const int stage = (kNarrowTokens + p.features) * kRowBytes, sums = kNarrowTokens * (p.features + 4) * 4;
+    const long long blocks = (p.a.T + kNarrowTokens - 1) / kNarrowTokens;
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    // as many stages as let the blocks that there are for an SM, up to three, run beside each other
+    const int beside = blocks <= sms ? 1 : blocks <= 2LL * sms ? 2 : kNarrowBlocks;
+    p.stages = (kNarrowSmem / beside - 3 * 1024) / stage;   // (1 KB each: the system's, the barriers, the boxes' alignment)
+    p.stages = p.stages > kNarrowStages ? kNarrowStages : p.stages;
+    if (p.stages > p.chunks) p.stages = p.chunks;
+    const int bytes = p.stages * stage < sums ? sums : p.stages * stage;
+    p.columns = 32;
+    while ((int)p.columns < p.features * (std::is_same<Out, float>::value ? 2 : 1)) p.columns *= 2;
+    p.few = 2 * blocks <= sms;
+    return launch_cluster(kern, dim3((unsigned)blocks), kNarrowThreads, bytes + 1024, 1, s, p, wm, xm);
+}
+
 template <typename Out>
 cudaError_t launch_out(const Params& p, int sms, cudaStream_t s) {
+    if (p.features) return p.a.in_dtype == GEOCACHE_E4M3 ? launch_narrow<Out, true>(p, sms, s) : launch_narrow<Out, false>(p, sms, s);
     if (p.a.in_dtype == GEOCACHE_E4M3) return p.a.gated ? launch_tiles<Out, true, true>(p, sms, s) : launch_tiles<Out, true, false>(p, sms, s);
     return p.a.gated ? launch_tiles<Out, false, true>(p, sms, s) : launch_tiles<Out, false, false>(p, sms, s);
 }
@@ -429,7 +633,7 @@ cudaError_t launch_out(const Params& p, int sms, cudaStream_t s) {
 // is on average 1.4% slower than the best one.
 struct Choice {
     int pair_features;   // of a tile of the pairs' kernel, 0: the tile kernel
-    int tokens, splits;  // of its tiles and clusters
+    int tokens, splits;  // of its tiles and clusters; no tokens: the kernel for few features
 };
 Choice choose(const LinearArgs& a, int sms) {
     const bool f32 = a.out_dtype == GEOCACHE_F32;
@@ -465,6 +669,12 @@ Choice choose(const LinearArgs& a, int sms) {
         const double sums = chunks * (features == 256 ? 0.281 : f32 ? 0.182 : 0.169);
         if (n < 2e9) take(4.73 + 0.0571 * mb + rounds * (sums > finish ? sums : finish), {features, 0, 0});
     }
+    if (a.N <= kNarrowFeatures && !a.gated) {
+        // a block's chain or the memory, and rounds of blocks
+        const double part = (a.N <= 16 ? 16 : a.N <= 32 ? 32 : 64) / 64.0, copies = 3.5 + 0.135 * mb;
+        const double chain = 3 + 1.2 * part + chunks * (0.23 + 0.02 * part), rounds = tiles(a.T, kNarrowTokens * kNarrowBlocks * sms);
+        take((chain > copies ? chain : copies) + 2 * (rounds - 1), {0, 0, 1});
+    }
     return c;
 }
 
@@ -494,7 +704,11 @@ cudaError_t launch_linear(const LinearArgs& given, cudaStream_t s) {
     p.splits = c.splits;
     // binary32 sums, operands of one type (e4m3 is type 0 of its kind), both with the summed axis contiguous
     const uint32_t type = a.in_dtype == GEOCACHE_BF16 ? 1 : 0;
-    p.idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(p.tokens >> 3) << 17 | (uint32_t)(kFeatures >> 4) << 24;
+    if (!p.tokens)
+        for (p.features = 16; p.features < a.N;) p.features *= 2;
+    // the first operand's rows are the lanes, here weights; with few features tokens
+    const int columns = p.features ? p.features : p.tokens, lanes = p.features ? kNarrowTokens : kFeatures;
+    p.idesc = 1u << 4 | type << 7 | type << 10 | (uint32_t)(columns >> 3) << 17 | (uint32_t)(lanes >> 4) << 24;
     p.out_wide = !((uintptr_t)a.out.data % (4 * ob)) && a.out.stride % 4 == 0;
     p.residual_wide = !((uintptr_t)a.residual.data % (4 * ob)) && a.residual.stride % 4 == 0;
     if (a.out_dtype == GEOCACHE_BF16) return launch_out<__nv_bfloat16>(p, sms, s);

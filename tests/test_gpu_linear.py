@@ -131,7 +131,8 @@ EPILOGUES = [dict(), dict(bias=True), dict(act="gelu"), dict(act="gelu_tanh", bi
 
 @pytest.mark.parametrize("dtype,od", [(BF16, BF16), (BF16, F32), (F16, F16), (F16, F32), (E4M3, BF16), (E4M3, F16), (E4M3, F32)],
                          ids=["bf16", "bf16-f32", "f16", "f16-f32", "e4m3-bf16", "e4m3-f16", "e4m3-f32"])
-@pytest.mark.parametrize("T,K,N", [(1, 512, 70), (5, 1600, 512), (130, 640, 200), (700, 768, 900), (2600, 512, 1200)])
+@pytest.mark.parametrize("T,K,N", [(1, 512, 70), (5, 1600, 512), (130, 640, 200), (700, 768, 900), (2600, 512, 1200), (1300, 1024, 1300),
+                                   (5000, 512, 4104)])
 def test_epilogues(gc, T, K, N, dtype, od):
     for i, e in enumerate(EPILOGUES):
         gated = e.get("gated", False)
@@ -163,6 +164,52 @@ def test_epilogues(gc, T, K, N, dtype, od):
             out = gc.linear(x, w, bias, e.get("act"), gated, r, xs, ws, out=wide[:T, shift:shift + N])
             assert torch.equal(out, got)
             assert (wide[T] == 5).all() and (wide[:, :shift] == 5).all() and (wide[:, shift + N:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype,od", [(BF16, BF16), (BF16, F32), (F16, F32), (E4M3, F16), (E4M3, F32)],
+                         ids=["bf16", "bf16-f32", "f16-f32", "e4m3-f16", "e4m3-f32"])
+@pytest.mark.parametrize("T,K,N", [(7999, 320, 1), (9001, 64, 13), (5000, 1000, 16), (20479, 512, 17), (24577, 2048, 64), (24576, 1552, 39),
+                                   (39001, 528, 61), (60001, 256, 64)])
+def test_few_features(gc, T, K, N, dtype, od):
+    # tokens in one, two, three and more rounds of blocks an SM; the last block with one token or all
+    _exact_case(gc, T, K, N, dtype)
+    for i, e in enumerate([dict(), dict(bias=True), dict(act="gelu_tanh", bias=True, residual=True), dict(act="silu", residual=True)]):
+        x, w = _randn((T, K), 10 * i), _randn((N, K), 10 * i + 1) * 2 * K ** -0.5
+        xs = ws = None
+        if dtype is E4M3:
+            x, xs = gc.quantize_rows(x)
+            w, ws = gc.quantize_rows(w)
+        bias = _randn((N,), 10 * i + 2) if e.get("bias") else None
+        residual = _randn((T, N), 10 * i + 3).to(od) if e.get("residual") else None
+        x, w = _rows(x, dtype, K, 32), _rows(w, dtype, K, 16)
+        got = gc.linear(x, w, bias, e.get("act"), False, residual, xs, ws, out_dtype=od)
+        y, dy = _reference(x, w, N, e.get("act"), False, bias, residual, xs, ws)
+        _check(got, y, dy, od, str(e))
+        if residual is not None:
+            r = residual.clone()
+            assert torch.equal(gc.linear(x, w, bias, e.get("act"), False, r, xs, ws, out=r), got)
+        for shift in (1, 4):
+            wide = torch.full((T + 1, N + 17), 5.0, device=DEV, dtype=od)
+            assert torch.equal(gc.linear(x, w, bias, e.get("act"), False, residual, xs, ws, out=wide[:T, shift:shift + N]), got)
+            assert (wide[T] == 5).all() and (wide[:, :shift] == 5).all() and (wide[:, shift + N:] == 5).all()
+
+
+def test_few_features_not_finite(gc):
+    T, K, N = 12001, 128, 33
+    x, w = _whole((T, K), 1), _whole((N, K), 2)
+    x[70, 3] = float("nan")
+    x[300, 3] = float("inf")
+    w[:, 3] = 1.0
+    w[9, 5] = float("nan")
+    ref = gc.linear(torch.nan_to_num(x, 0.0, 0.0).to(BF16), torch.nan_to_num(w, 0.0).to(BF16), out_dtype=F32)
+    got = gc.linear(x.to(BF16), w.to(BF16), out_dtype=F32)
+    nan = torch.zeros((T, N), dtype=torch.bool, device=DEV)
+    nan[70] = True
+    nan[:, 9] = True
+    inf = torch.zeros_like(nan)
+    inf[300] = True
+    inf &= ~nan
+    assert got[nan].isnan().all() and (got[inf] == float("inf")).all() and torch.equal(got[~nan & ~inf], ref[~nan & ~inf])
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3], ids=["bf16", "e4m3"])
@@ -252,7 +299,8 @@ def test_streams_and_graph(gc):
     gc.device_status()
 
 
-@pytest.mark.parametrize("T,K,N", [(4, 4096, 512), (512, 512, 1536), (300, 1024, 256), (2600, 2048, 1200), (6000, 512, 512)])
+@pytest.mark.parametrize("T,K,N", [(4, 4096, 512), (512, 512, 1536), (300, 1024, 256), (2600, 2048, 1200), (6000, 512, 512),
+                                   (30000, 2048, 40)])
 def test_waits_that_run_out(gc, T, K, N):
     x, w = _randn((T, K), 1).to(BF16), _randn((N, K), 2).to(BF16)
     want = gc.linear(x, w)
