@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
 // of tensor memory and the features its columns, so that no product is of rows that are not there, and up to three blocks
 // an SM, not persistent, keep the memory busy where the tiles are no whole rounds of the SMs: 24576 x 2048 x 64 bf16 (192
 // tiles) into f32 takes 22 us (4.6 TB/s with the launch and its ends), on pairs of SMs 26; 44943 tokens into bf16 34, with
-// two blocks an SM 38.  All blocks read the same weights at the same time, so a chunk of a block alone takes 0.23 us.
+// two blocks an SM 38.  Where the tiles are fewer than the SMs a chunk takes 0.23 us, whatever its features and stages.
 constexpr int kNarrowTokens = 128, kNarrowFeatures = 64, kNarrowStages = 12, kNarrowThreads = 192, kNarrowBlocks = 3;   // (blocks an SM)
 
 struct NarrowBarriers {
