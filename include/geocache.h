@@ -583,8 +583,10 @@ typedef struct {
  * and out = y rounded to `dtype` (scale NULL), or 8-bit rows (scale given):
  *     scale = max(max_c |y_c| / 448, 2^-126),  out = e4m3(y / scale),
  * so that out * scale stands for y.  What is rounded to residual_dtype is what
- * is normalised; the mean, y and the scale are binary32 (a row whose h^2 or
- * h * weight overflow binary32 has no useful result).  A NaN or infinity stays
+ * is normalised; the mean, y, the scale and y / scale are binary32, with a
+ * rounding for each operation (a value beside the middle of two e4m3 numbers may
+ * become either; a row whose h^2 or h * weight overflow binary32, or, with eps 0,
+ * underflow, has no useful result).  A NaN or infinity stays
  * in its row.
  *   x                       [T, C] of `dtype` (F32, BF16 or F16).
  *   residual, residual_out  [T, C] of residual_dtype (`dtype` or F32), or NULL both.
@@ -605,7 +607,9 @@ int geocache_add_rms_norm(const geocache_rows* x, const geocache_rows* residual,
 /* --------------------------------------------------------------------------
  * geocache_quantize_rows -- 8-bit rows of what follows no norm (the
  * attention's output, a feed-forward's hidden rows, weights):
- *     scale = max(max_c |x_c| / 448, 2^-126),  out = e4m3(x / scale).
+ *     scale = max(max_c |x_c| / 448, 2^-126),  out = e4m3(x / scale),
+ * the scale rounded to nearest; from 16-bit rows so are the quotients (binary32,
+ * then e4m3), from F32 rows they are within 2^-43 of that before the rounding.
  * x [T, C] of `dtype` (F32, BF16 or F16), out [T, C] E4M3, scale device [T] f32.
  * Sizes, alignment and statuses as geocache_add_rms_norm; no buffers overlap.
  * ------------------------------------------------------------------------ */

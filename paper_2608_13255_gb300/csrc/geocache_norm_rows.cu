@@ -57,6 +57,33 @@ __device__ __forceinline__ uint32_t pack_e4m3(float2 a, float2 b) {
     return r;
 }
 
+// max / 448: an inverse of two terms, the first of which is rounded down.  Rounded correctly, as no quotient by 7 is within
+// 2^-27 of half a step, where no term is subnormal.
+__device__ __forceinline__ float scale_of(float top) {
+    constexpr float kHigh = 0x1.249248p-9f, kLow = (float)(1.0 / 448.0 - (double)kHigh);
+    static_assert(kLow > 0.0f, "rounded down");
+    float s = fmaf(top, kHigh, top * kLow);
+    if (top < 0x1p-60f) s = __fdiv_rn(top, kLargest);
+    return s < kTiny ? kTiny : s;  // (a NaN stays)
+}
+// 1 / scale as the sum of two terms: x hi + x lo is within 2^-43 of x / scale before it is rounded.  With one term a value at
+// the middle of two numbers of e4m3, which 16-bit rows meet often, went either way (0.05% of the elements of 20001 x 8192
+// f16 were a step from e4m3(x / scale); one more instruction a pair: 81.5 -> 82.9 us, 8192 x 2048 bf16 9.1 -> 9.8).  lo is
+// positive, so that a zero keeps its sign.
+struct Inverse {
+    float hi, lo;
+};
+__device__ __forceinline__ Inverse inverse_of(float scale) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(scale));   // (within 2^-23)
+    Inverse i;
+    i.hi = __uint_as_float(__float_as_uint(r) - 2);
+    i.lo = fmaf(-scale, i.hi, 1.0f) * i.hi;
+    return i;
+}
+// Of scales beyond, lo would be subnormal: such rows are brought down first (what becomes zero by that is zero in 8 bits).
+constexpr float kHighScale = 0x1p60f, kDown = 0x1p-64f;
+
 // ----------------------------------------------------------------- words --
 // 8 elements of a row as they lie in memory
 template <typename T>
@@ -253,23 +280,40 @@ __global__ void __launch_bounds__(most_threads(kPieces)) norm_rows_kernel(const 
         const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
         float g = f;   // what an element is multiplied by
         if (kQuant) {
-            const float s = top * f * (1.0f / kLargest);
-            const float scale = s < kTiny ? kTiny : s;  // (a NaN stays)
+            float scale = scale_of(top * f);
             if (lane == 0 && active) a.scale[row] = scale;
-            const float inv = __fdividef(1.0f, scale);  // (scale < 2^126)
-            g = f * inv;
-            if (kNorm && isinf(g)) {   // a row that is nearly zero
+            if (kNorm) {   // (y has roundings of its own, and no ties to keep: one product)
+                const float inv = __fdividef(1.0f, scale);  // (scale < 2^126)
+                g = f * inv;
+                if (isinf(g)) {   // a row that is nearly zero
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(f));
+                    g = inv;
+                }
+            } else {
+                if (scale > kHighScale) {
+                    scale *= kDown;
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(kDown));
+                }
+                Inverse inv = inverse_of(scale);
+                if (isinf(scale)) inv.hi = inv.lo = 0.0f;   // (an infinity: no number in its place, zeros beside it)
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(f));
-                g = inv;
+                    for (int e = 0; e < 4; ++e) v[i][e] = fma2(v[i][e], both(inv.hi), mul2(v[i][e], both(inv.lo)));
             }
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
+            if (kNorm) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(g));
+                for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], both(g));
+            }
             const int n = active ? n_of[i] : 0;
             if constexpr (kQuant) {
                 const uint32_t lo = pack_e4m3(v[i][0], v[i][1]), hi = pack_e4m3(v[i][2], v[i][3]);
@@ -348,18 +392,26 @@ __global__ void __launch_bounds__(most_element_threads(kCount)) norm_elements_ke
         }
         join_row<kNorm, kQuant>(sum, top, a, shared[turn], row_in);
         const float f = kNorm ? rsqrtf(fmaf(sum, a.inv_C, a.eps)) : 1.0f;
-        float inv = 1.0f;
+        Inverse inv{1.0f, 0.0f};
+        float down = 1.0f;
         if (kQuant) {
-            const float s = top * f * (1.0f / kLargest);
-            const float scale = s < kTiny ? kTiny : s;  // (a NaN stays)
+            float scale = scale_of(top * f);
             if (lane == 0 && row < a.T) a.scale[row] = scale;
-            inv = __fdividef(1.0f, scale);  // (scale < 2^126)
+            if (kNorm) {
+                inv.hi = __fdividef(1.0f, scale);  // (scale < 2^126)
+            } else {   // (as above)
+                if (scale > kHighScale) scale *= down = kDown;
+                inv = inverse_of(scale);
+                if (isinf(scale)) inv.hi = inv.lo = 0.0f;
+            }
         }
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             if (kNorm) v[i] *= f;
             if constexpr (kQuant) {
-                const uint32_t q = pack_e4m3(make_float2(v[i] * inv, 0.0f), make_float2(0.0f, 0.0f));
+                if (!kNorm) v[i] *= down;
+                const float t = kNorm ? v[i] * inv.hi : fmaf(v[i], inv.hi, v[i] * inv.lo);
+                const uint32_t q = pack_e4m3(make_float2(t, 0.0f), make_float2(0.0f, 0.0f));
                 if (i < in) static_cast<uint8_t*>(a.out.data)[row * a.out.stride + lane + i * a.lanes] = (uint8_t)q;
             } else {
                 if (i < in) static_cast<X*>(a.out.data)[row * a.out.stride + lane + i * a.lanes] = (X)v[i];
