@@ -286,7 +286,8 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         if (p.splits > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         // with one block the stages are overwritten: the loads have landed, as the products that wait for them are done
         ok = __all_sync(0xffffffffu, ok && !*(volatile uint32_t*)&b->dead);
-        if (ok) {
+        // In a cluster each block sends all of its sums whatever ran out (NaN then), so that the others' barriers end.
+        if (ok || p.splits > 1) {
             int to = 0, in = 0;   // the block that finishes token t, and t's place there
             const uint32_t mine = sums + (rank * p.share * kFeatures + warp * 32 + lane) * 4, here = smem_u32(&b->here);
             uint32_t row = mine, bar = here;
@@ -298,7 +299,10 @@ __global__ void __launch_bounds__(kTileThreads, 2)
             for (int t = 0; t < kMostTokens; t += 16)
                 if (t < p.tokens) {
                     uint32_t r[16];
-                    if (!kParts) {
+                    if (!ok) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) r[i] = 0x7fffffffu;
+                    } else if (!kParts) {
                         tmem_ld16(at + t, r);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                         asm volatile("" : GEOCACHE_PIN16(r));
@@ -350,8 +354,9 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         if (p.splits == 1) return;
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        if (!ok)   // sums on their way to a block that did not wait for all of them
-            for (const unsigned long long t0 = globaltimer(); globaltimer() - t0 < 20000;) {}
+        // sums on their way to a block that gave up waiting land before it ends
+        const unsigned long long t0 = globaltimer();
+        while (tile_tokens && !mbar_try(&b->here, 0) && globaltimer() - t0 < kDrainLimitNs) {}
     };
     if (!ok) {
         leave();
