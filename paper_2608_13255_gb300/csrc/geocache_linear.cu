@@ -52,7 +52,7 @@ __device__ __forceinline__ void load_epilogue(Epilogue& e, const LinearArgs& a, 
         }
 }
 // v: the sums, and then the results
-template <bool kGated>
+template <typename Out, bool kGated>
 __device__ __forceinline__ void finish(float2* v, float2* gate, const Epilogue& e, float xs, bool scaled, int act) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -62,7 +62,7 @@ __device__ __forceinline__ void finish(float2* v, float2* gate, const Epilogue& 
             const float2 bias = make_float2(e.bias[g][2 * i], e.bias[g][2 * i + 1]);
             z = scaled ? fma2(mul2(z, both(xs)), make_float2(e.scale[g][2 * i], e.scale[g][2 * i + 1]), bias) : add2(z, bias);
         }
-    activate<2>(kGated ? gate : v, act);
+    activate<Out, 2>(kGated ? gate : v, act);
     if (kGated) {
         v[0] = mul2(v[0], gate[0]);
         v[1] = mul2(v[1], gate[1]);
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
                 w[0] = add2(w[0], make_float2(s.x, s.y));
                 w[1] = add2(w[1], make_float2(s.z, s.w));
             }
-        finish<kGated>(v, gate, e, xs, p.a.x_scale != nullptr, p.a.act);
+        finish<Out, kGated>(v, gate, e, xs, p.a.x_scale != nullptr, p.a.act);
         const float y[4] = {v[0].x + res[0], v[0].y + res[1], v[1].x + res[2], v[1].y + res[3]};
         store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + n, p.out_wide, n_in, y);
     }
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
                      : "=f"(s.x), "=f"(s.y), "=f"(s.z), "=f"(s.w)
                      : "r"(smem + (t * (p.features + 4) + unit_f) * 4));
         float2 v[2] = {make_float2(s.x, s.y), make_float2(s.z, s.w)};
-        finish<false>(v, v, e, 1.0f, p.a.x_scale != nullptr, p.a.act);   // (the token's scale is in the sum)
+        finish<Out, false>(v, v, e, 1.0f, p.a.x_scale != nullptr, p.a.act);   // (the token's scale is in the sum)
         const float y[4] = {v[0].x + res[0], v[0].y + res[1], v[1].x + res[2], v[1].y + res[3]};
         store4(static_cast<Out*>(p.a.out.data) + token * p.a.out.stride + unit_f, p.out_wide, n_in, y);
     }

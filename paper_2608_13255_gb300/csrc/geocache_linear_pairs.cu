@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                 }
-                activate<kBlock / 2>(kGated ? g : v, p.a.act);
+                activate<Out, kBlock / 2>(kGated ? g : v, p.a.act);
                 if (kGated) {
 #pragma unroll
                     for (int i = 0; i < kBlock / 2; ++i) v[i] = mul2(v[i], g[i]);
