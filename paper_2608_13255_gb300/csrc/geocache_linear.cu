@@ -355,8 +355,8 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         // sums on their way to a block that gave up waiting land before it ends
-        const unsigned long long t0 = globaltimer();
-        while (tile_tokens && !mbar_try(&b->here, 0) && globaltimer() - t0 < kDrainLimitNs) {}
+        if (!ok && tile_tokens)
+            for (const unsigned long long t0 = globaltimer(); !mbar_try(&b->here, 0) && globaltimer() - t0 < kDrainLimitNs;) {}
     };
     if (!ok) {
         leave();
