@@ -99,14 +99,12 @@ __device__ __forceinline__ void store4(Out* p, bool wide, int n, const float* v)
 }
 
 // ---------------------------------------------------------------- tiles --
-// A tile of 128 rows of weights (the lanes of tensor memory) x up to 128 tokens (its columns), the summed axis cut over
+// A tile of 128 rows of weights (the lanes of tensor memory) x 16, 32 or 64 tokens (its columns), the summed axis cut over
 // the blocks of a cluster.  The blocks' sums meet in shared memory: each sends every other one the sums of the tokens
 // that the other finishes, which adds them in the order of the blocks (no atomics: every call gives the same bits).
-// kParts: f32 results, whose sums leave tensor memory every kPartChunks chunks and are added up in registers, rounded to
-// nearest; the tensor cores' own additions cut off (a chain of 128 was 2.1e-6 from the definition, with parts 2.4e-7).
+// kParts: f32 results, and 16-bit ones of a long summed axis, whose sums leave tensor memory in parts.
 constexpr int kTileWarps = 8, kTileThreads = 32 * kTileWarps, kTileLoadWarp = 4, kTileMmaWarp = 5;
-constexpr int kTileStages = 12;
-constexpr int kPartChunks = 4;
+constexpr int kTileStages = 12, kMostTokens = 64;
 
 struct TileBarriers {
     uint64_t full[kTileStages], empty[kTileStages], sums[2], taken[2], done, here;
@@ -124,11 +122,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 
-template <typename Out, bool kEight, bool kGated>
+template <typename Out, bool kEight, bool kGated, bool kParts>
 __global__ void __launch_bounds__(kTileThreads, 2)
     linear_tile_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm) {
-    constexpr bool kParts = std::is_same<Out, float>::value;
-    constexpr int kMostTokens = kParts ? 64 : 128;
+    constexpr int kLength = std::is_same<Out, float>::value ? kPartChunks : kChainChunks;   // of a part, in chunks
     constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;   // elements of a chunk
     extern __shared__ uint8_t raw[];
     __shared__ TileBarriers bars;
@@ -229,7 +226,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
         for (int c = c0, part = 0; ok && c < c1; ++part) {
             if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead);
             tc_after();   // (what was read from tensor memory)
-            const int end = kParts ? min(c + kPartChunks, c1) : c1;
+            const int end = kParts ? min(c + kLength, c1) : c1;
             uint32_t accumulate = 0;
             for (; ok && c < end; c += p.deep) {
                 ok = wait_warp(&b->full[stage], phase, limit, &b->dead);
@@ -257,7 +254,7 @@ __global__ void __launch_bounds__(kTileThreads, 2)
     } else if (warp < 4) {
         const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
         float acc[kParts ? kMostTokens : 1];
-        const int parts = kParts ? (c1 - c0 + kPartChunks - 1) / kPartChunks : 1;
+        const int parts = kParts ? (c1 - c0 + kLength - 1) / kLength : 1;
         bool ok = true;
         if (kParts) {
 #pragma unroll
@@ -405,10 +402,10 @@ struct NarrowBarriers {
     uint32_t tmem, dead;
 };
 
-template <typename Out, bool kEight>
+template <typename Out, bool kEight, bool kParts>
 __global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
     linear_narrow_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm) {
-    constexpr bool kParts = std::is_same<Out, float>::value;
+    constexpr int kLength = std::is_same<Out, float>::value ? kPartChunks : kChainChunks;   // of a part, in chunks
     constexpr int kStep = kEight ? kRowBytes : kRowBytes / 2;   // elements of a chunk
     constexpr uint32_t x_bytes = kNarrowTokens * kRowBytes;
     extern __shared__ uint8_t raw[];
@@ -482,7 +479,7 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
         for (int c = 0, part = 0; ok && c < p.chunks; ++part) {
             if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead);
             tc_after();   // (what was read from tensor memory)
-            const int end = kParts ? min(c + kPartChunks, p.chunks) : p.chunks;
+            const int end = kParts ? min(c + kLength, p.chunks) : p.chunks;
             uint32_t accumulate = 0;
             for (; ok && c < end; ++c) {
                 ok = wait_warp(&b->full[stage], phase, limit, &b->dead);
@@ -509,7 +506,7 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
         float acc[kNarrowFeatures] = {};
         const long long token = first_token + threadIdx.x;
         const float xs = p.a.x_scale && token < p.a.T ? __ldca(p.a.x_scale + token) : 1.0f;
-        const int parts = kParts ? (p.chunks + kPartChunks - 1) / kPartChunks : 1;
+        const int parts = kParts ? (p.chunks + kLength - 1) / kLength : 1;
         bool ok = true;
         for (int part = 0; ok && part < parts; ++part) {
             ok = wait_warp(&b->sums[part & 1], part >> 1 & 1, limit, &b->dead);
@@ -572,9 +569,9 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowBlocks)
 // ----------------------------------------------------------------- host --
 constexpr int kTileSmem = 112 * 1024;   // two blocks an SM
 
-template <typename Out, bool kEight, bool kGated>
+template <typename Out, bool kEight, bool kGated, bool kParts>
 cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
-    auto kern = linear_tile_kernel<Out, kEight, kGated>;
+    auto kern = linear_tile_kernel<Out, kEight, kGated, kParts>;
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem);
     if (ready != cudaSuccess) return ready;
     CUtensorMap wm, xm;
@@ -593,7 +590,7 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
     int bytes = p.stages * stage + beside;
     if (bytes < sums) bytes = sums;
     p.columns = 32;
-    const int used = p.tokens * (std::is_same<Out, float>::value ? 2 : 1);
+    const int used = p.tokens * (kParts ? 2 : 1);
     while ((int)p.columns < used) p.columns *= 2;
     const long long columns = (p.a.T + p.tokens - 1) / p.tokens * p.splits;
     if (columns > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
@@ -602,9 +599,9 @@ cudaError_t launch_tiles(Params p, int sms, cudaStream_t s) {
 }
 
 constexpr int kNarrowSmem = 227 * 1024;   // of an SM, with 1 KB beside each block's
-template <typename Out, bool kEight>
+template <typename Out, bool kEight, bool kParts>
 cudaError_t launch_narrow(Params p, int sms, cudaStream_t s) {
-    auto kern = linear_narrow_kernel<Out, kEight>;
+    auto kern = linear_narrow_kernel<Out, kEight, kParts>;
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowSmem - 1024);
     if (ready != cudaSuccess) return ready;
     CUtensorMap wm, xm;
@@ -621,16 +618,23 @@ cudaError_t launch_narrow(Params p, int sms, cudaStream_t s) {
     if (p.stages > p.chunks) p.stages = p.chunks;
     const int bytes = p.stages * stage < sums ? sums : p.stages * stage;
     p.columns = 32;
-    while ((int)p.columns < p.features * (std::is_same<Out, float>::value ? 2 : 1)) p.columns *= 2;
+    while ((int)p.columns < p.features * (kParts ? 2 : 1)) p.columns *= 2;
     p.few = 2 * blocks <= sms;
     return launch_cluster(kern, dim3((unsigned)blocks), kNarrowThreads, bytes + 1024, 1, s, p, wm, xm);
 }
 
+template <typename Out, bool kEight, bool kParts>
+cudaError_t launch_parts(const Params& p, int sms, cudaStream_t s) {
+    if (p.features) return launch_narrow<Out, kEight, kParts>(p, sms, s);
+    return p.a.gated ? launch_tiles<Out, kEight, true, kParts>(p, sms, s) : launch_tiles<Out, kEight, false, kParts>(p, sms, s);
+}
+
 template <typename Out>
 cudaError_t launch_out(const Params& p, int sms, cudaStream_t s) {
-    if (p.features) return p.a.in_dtype == GEOCACHE_E4M3 ? launch_narrow<Out, true>(p, sms, s) : launch_narrow<Out, false>(p, sms, s);
-    if (p.a.in_dtype == GEOCACHE_E4M3) return p.a.gated ? launch_tiles<Out, true, true>(p, sms, s) : launch_tiles<Out, true, false>(p, sms, s);
-    return p.a.gated ? launch_tiles<Out, false, true>(p, sms, s) : launch_tiles<Out, false, false>(p, sms, s);
+    const bool eight = p.a.in_dtype == GEOCACHE_E4M3;
+    if constexpr (!std::is_same<Out, float>::value)
+        if (p.chunks <= kChainChunks) return eight ? launch_parts<Out, true, false>(p, sms, s) : launch_parts<Out, false, false>(p, sms, s);
+    return eight ? launch_parts<Out, true, true>(p, sms, s) : launch_parts<Out, false, true>(p, sms, s);
 }
 
 // Which kernel and tile a product takes: the least estimate in us.  The terms were fitted to sweeps over tokens 1 to 24576,
@@ -654,10 +658,10 @@ Choice choose(const LinearArgs& a, int sms) {
             c = to;
         }
     };
-    for (int tokens = 16; tokens <= (f32 ? 64 : 128); tokens *= 2) {
+    for (int tokens = 16; tokens <= kMostTokens; tokens *= 2) {
         if (tokens > 16 && tokens / 2 >= a.T) break;
         for (int splits = 1; splits <= 8; ++splits) {
-            if (splits > 1 && (tokens > 64 || splits > chunks)) break;
+            if (splits > chunks) break;
             // blocks an SM, of which two run beside each other: the second adds 0.58 of the first's time
             const double r = tiles(a.T, tokens) * tiles(a.N, a.gated ? kFeatures / 2 : kFeatures) * splits / sms;
             const double rounds = r <= 1 ? 1 : r <= 2 ? 1 + 0.58 * (r - 1) : 0.79 * r;

@@ -24,7 +24,6 @@ constexpr int kTokens = 256;               // of a tile: 128 of each block
 constexpr int kFinishWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 32 * 10;
 constexpr int kMostStages = 6;
 constexpr int kRing = 6 * 32 * 1024;       // bytes of the stages
-constexpr int kPartChunks = 4;             // as in the tile kernel: f32 results leave tensor memory in parts
 constexpr int kTurnBytes = 32 * 64;        // of a finishing warp's buffer: 64 bytes of 32 tokens, in swizzled words of 16
 
 struct PairParams {
@@ -141,11 +140,12 @@ __device__ __forceinline__ void turn_in(uint32_t buffer, const char* rows, long 
     }
 }
 
-template <typename Out, bool kEight, bool kGated, int kN>
+// kParts: f32 results, and 16-bit ones of a long summed axis, whose sums leave tensor memory in parts
+template <typename Out, bool kEight, bool kGated, int kN, bool kParts>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_pair_kernel(const __grid_constant__ PairParams p, const __grid_constant__ CUtensorMap wm, const __grid_constant__ CUtensorMap xm,
                        const __grid_constant__ CUtensorMap om) {
-    constexpr bool kParts = std::is_same<Out, float>::value;
+    constexpr int kLength = std::is_same<Out, float>::value ? kPartChunks : kChainChunks;   // of a part, in chunks
     constexpr int kOut = kGated ? kN / 2 : kN;          // output features of a tile
     constexpr int kCols = kOut / 2;                     // of them, those of a finishing warp
     // A turn of the loop that issues the products takes some 400 cycles, a chunk's products 512, or 256 with 128 rows of
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; ok && c < p.chunks; ++part) {
                     if (part >= 2) ok = wait_warp(&b->taken[part & 1], (part >> 1 & 1) ^ 1, limit, &b->dead, error);
                     tc_after();   // (what was read from tensor memory)
-                    const int end = kParts ? min(c + kPartChunks, p.chunks) : p.chunks;
+                    const int end = kParts ? min(c + kLength, p.chunks) : p.chunks;
                     uint32_t accumulate = 0;
                     for (; ok && c < end; c += kDeep) {
                         ok = wait_warp(&b->full[stage], phase, limit, &b->dead, error);
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float* bias = consts[warp][0];
         float* scale = consts[warp][1];
         const uint32_t turn = smem + kStages * kStage + warp * kTurnBytes;
-        const int parts = kParts ? (p.chunks + kPartChunks - 1) / kPartChunks : 1;
+        const int parts = kParts ? (p.chunks + kLength - 1) / kLength : 1;
         const bool scaled = p.a.x_scale != nullptr;
         uint32_t part = 0;
         bool ok = true;
@@ -404,9 +404,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();   // the buffer has been read
             };
 
-            float acc[kParts ? kG * kCols : 1];
+            // (f32 results: in registers; 16-bit ones in local memory, whose addresses are no constants)
+            constexpr int kUnroll = std::is_same<Out, float>::value ? kG * kCols : 1;
+            __align__(16) float acc[kParts ? kG * kCols : 1];
             if (kParts) {
-#pragma unroll
+#pragma unroll kUnroll
                 for (int i = 0; i < kG * kCols; ++i) acc[kParts ? i : 0] = 0.0f;
             }
             for (int q = 0; ok && q < parts; ++q, ++part) {
@@ -415,9 +417,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_after();
                 const uint32_t from = at + (part & 1) * kN;
                 if (kParts) {
-#pragma unroll
+#pragma unroll kUnroll
                     for (int g = 0; g < kG; ++g)
-#pragma unroll
+#pragma unroll kUnroll
                         for (int j = 0; j < kCols; j += 16) {
                             uint32_t r[16];
                             tmem_ld16(from + g * (kN / 2) + j, r);
@@ -433,9 +435,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                         continue;
                     }
                     // the whole sums take the last part's place, where the loop below finds them (its columns are no constants)
-#pragma unroll
+#pragma unroll kUnroll
                     for (int g = 0; g < kG; ++g)
-#pragma unroll
+#pragma unroll kUnroll
                         for (int j = 0; j < kCols; j += 16)
                             tmem_st16(from + g * (kN / 2) + j, reinterpret_cast<uint32_t*>(acc) + (kParts ? g * kCols + j : 0));
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -503,9 +505,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
 }
 
-template <typename Out, bool kEight, bool kGated, int kN>
+template <typename Out, bool kEight, bool kGated, int kN, bool kParts>
 cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
-    auto kern = linear_pair_kernel<Out, kEight, kGated, kN>;
+    auto kern = linear_pair_kernel<Out, kEight, kGated, kN, kParts>;
     constexpr int kBytes = kRing + kFinishWarps * kTurnBytes + 1024;
     static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (ready != cudaSuccess) return ready;
@@ -527,19 +529,26 @@ cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
     return launch_cluster(kern, dim3((unsigned)(2 * pairs)), kThreads, kBytes, 2, s, p, wm, xm, om);
 }
 
-// f32 results: tiles of 128 rows of weights only, whose sums in registers need no spills
-template <typename Out, bool kEight, bool kGated>
+// f32 results: tiles of 128 rows of weights only, whose sums the registers hold
+template <typename Out, bool kEight, bool kGated, bool kParts>
 cudaError_t launch_n(const PairParams& p, int features, int pairs, cudaStream_t s) {
     if constexpr (!std::is_same<Out, float>::value)
-        if (features == 256) return launch<Out, kEight, kGated, 256>(p, pairs, s);
-    return launch<Out, kEight, kGated, 128>(p, pairs, s);
+        if (features == 256) return launch<Out, kEight, kGated, 256, kParts>(p, pairs, s);
+    return launch<Out, kEight, kGated, 128, kParts>(p, pairs, s);
+}
+
+template <typename Out, bool kParts>
+cudaError_t launch_parts(const PairParams& p, int features, int pairs, cudaStream_t s) {
+    if (p.a.in_dtype == GEOCACHE_E4M3)
+        return p.a.gated ? launch_n<Out, true, true, kParts>(p, features, pairs, s) : launch_n<Out, true, false, kParts>(p, features, pairs, s);
+    return p.a.gated ? launch_n<Out, false, true, kParts>(p, features, pairs, s) : launch_n<Out, false, false, kParts>(p, features, pairs, s);
 }
 
 template <typename Out>
 cudaError_t launch_out(const PairParams& p, int features, int pairs, cudaStream_t s) {
-    if (p.a.in_dtype == GEOCACHE_E4M3)
-        return p.a.gated ? launch_n<Out, true, true>(p, features, pairs, s) : launch_n<Out, true, false>(p, features, pairs, s);
-    return p.a.gated ? launch_n<Out, false, true>(p, features, pairs, s) : launch_n<Out, false, false>(p, features, pairs, s);
+    if constexpr (!std::is_same<Out, float>::value)
+        if (p.chunks <= kChainChunks) return launch_parts<Out, false>(p, features, pairs, s);
+    return launch_parts<Out, true>(p, features, pairs, s);
 }
 
 }  // namespace
