@@ -630,9 +630,9 @@ typedef enum {
  * with the sums and the epilogue in binary32, rounded once to out_dtype (GELU's
  * second term, |z| erfc(|z| / sqrt 2) / 2, is within 2.2e-6 + 9e-8 z^2 of itself,
  * for BF16 results within 2.1e-7).  The tensor cores cut their additions off: the
- * sums of 16-bit results are within 2^-12 of sum |x w| at any K (2^-16 is met),
+ * sums of 16-bit results are within 2^-12 of sum |x w| at any K (2^-13.3 is met),
  * those of F32 results, which leave them every 256 (8-bit 512) elements, within
- * 2^-17 up to K = 8192 (2^-21 is met).  Every
+ * 2^-17 up to K = 8192 (2^-19.7 is met).  Every
  * call gives the same bits for the same arguments.
  *   x             [T, K] of in_dtype: BF16, F16, or E4M3 with both scales.
  *   weight        [N, K] of in_dtype; gated [2 N, K], the values' rows first.
@@ -718,6 +718,25 @@ int geocache_device_status(void* stream);
  * Process-wide, not thread safe.  Returns GEOCACHE_OK.
  * ------------------------------------------------------------------------ */
 int geocache_debug_set_wait(uint64_t limit_ns, int drop_first_copy);
+
+/* --------------------------------------------------------------------------
+ * geocache_debug_set_linear, geocache_debug_last_linear -- test hooks of
+ * geocache_linear (the paper has no counterpart): which of its kernels later
+ * calls take, instead of the least estimate, and which one the calling
+ * thread's last call took.
+ *   kernel   0: by the estimate (the default).
+ *            1: tiles of 128 rows of weights x `size` (16, 32, 64) tokens, the
+ *               summed axis cut over `splits` (1 to 8) blocks.
+ *            2: tiles of 256 tokens x `size` (128, or 256 for results of 16 bits)
+ *               rows of weights on pairs of SMs.
+ *            3: at most 64 features, not gated, with the tokens as lanes.
+ * A call that the kernel cannot take (256 rows for F32 results, more than 64
+ * features, more blocks than 128-byte pieces of a row of x) is refused with EINVAL.
+ * Process-wide; as for geocache_debug_set_wait, not thread safe.  Returns
+ * GEOCACHE_OK, EINVAL.
+ * ------------------------------------------------------------------------ */
+int geocache_debug_set_linear(int kernel, int size, int splits);
+int geocache_debug_last_linear(int* kernel, int* size, int* splits);
 
 /* --------------------------------------------------------------------------
  * geocache_transport_step_noalloc -- geocache_transport_step for callers that

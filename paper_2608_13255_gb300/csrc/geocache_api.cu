@@ -338,6 +338,21 @@ int geocache_debug_set_wait(uint64_t limit_ns, int drop_first_copy) {
     return ok();
 }
 
+int geocache_debug_set_linear(int kernel, int size, int splits) {
+    const bool tiles = kernel == 1 && (size == 16 || size == 32 || size == 64) && splits >= 1 && splits <= 8;
+    if (kernel != 0 && !tiles && !(kernel == 2 && (size == 128 || size == 256)) && kernel != 3)
+        return fail(GEOCACHE_EINVAL, "geocache_debug_set_linear: kernel %d with size %d and splits %d", kernel, size, splits);
+    geocache::set_debug_linear({kernel, kernel == 1 || kernel == 2 ? size : 0, kernel == 1 ? splits : 0});
+    return ok();
+}
+
+int geocache_debug_last_linear(int* kernel, int* size, int* splits) {
+    if (!kernel || !size || !splits) return fail(GEOCACHE_EINVAL, "geocache_debug_last_linear: an output is NULL");
+    const geocache::LinearKernel k = geocache::last_linear();
+    *kernel = k.kernel; *size = k.size; *splits = k.splits;
+    return ok();
+}
+
 int geocache_build_corr(geocache_corr* c, void* stream) {
     g_launches = 0;
     const int st = check_build(c);
@@ -889,6 +904,7 @@ int geocache_linear(const geocache_rows* x, const geocache_rows* weight, const g
     a.T = T; a.K = K; a.N = N;
     a.in_dtype = in_dtype; a.out_dtype = out_dtype; a.act = act; a.gated = gated != 0;
     a.bias = bias; a.x_scale = x_scale; a.w_scale = weight_scale;
+    if (!geocache::debug_linear_fits(a)) return fail(GEOCACHE_EINVAL, "%s: the kernel that is set cannot take this product", fn);
     a.wait_limit_ns = geocache::debug_wait_limit_ns();
     a.drop_first_copy = geocache::take_drop_first_copy();
     cudaError_t e = geocache::launch_linear(a, (cudaStream_t)stream);

@@ -197,6 +197,14 @@ struct LinearArgs {
     unsigned int* error;   // status word, set by the launch
 };
 cudaError_t launch_linear(const LinearArgs& a, cudaStream_t s);
+// the kernel that products are to take or took (geocache_debug_set_linear); kernel 0: none
+struct LinearKernel {
+    int kernel, size, splits;
+};
+void set_debug_linear(const LinearKernel& k);
+LinearKernel last_linear();
+// whether the kernel that is set can take the product
+bool debug_linear_fits(const LinearArgs& a);
 // the kernel for many tokens, with tiles of 256 or 128 rows of weights
 cudaError_t launch_linear_pairs(const LinearArgs& a, int features, int sms, cudaStream_t s);
 // the limit of bounded waits, and the test hook's pending request (consumed)

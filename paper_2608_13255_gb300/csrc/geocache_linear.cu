@@ -644,9 +644,12 @@ struct Choice {
     int pair_features;   // of a tile of the pairs' kernel, 0: the tile kernel
     int tokens, splits;  // of its tiles and clusters; no tokens: the kernel for few features
 };
+int chunks_of(const LinearArgs& a) {
+    return (int)(((long long)a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) + kRowBytes - 1) / kRowBytes);
+}
 Choice choose(const LinearArgs& a, int sms) {
     const bool f32 = a.out_dtype == GEOCACHE_F32;
-    const int chunks = (int)(((long long)a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) + kRowBytes - 1) / kRowBytes);
+    const int chunks = chunks_of(a);
     auto tiles = [](long long n, int per) { return (double)((n + per - 1) / per); };
     // operands in MB, of which the first wait for memory
     const double mb = 1e-6 * a.K * (a.in_dtype == GEOCACHE_E4M3 ? 1 : 2) * (double)(a.T + (long long)a.N * (a.gated ? 2 : 1));
@@ -687,7 +690,17 @@ Choice choose(const LinearArgs& a, int sms) {
     return c;
 }
 
+LinearKernel g_set{};                 // by a test (0: the estimate)
+thread_local LinearKernel g_taken{};
+
 }  // namespace
+
+void set_debug_linear(const LinearKernel& k) { g_set = k; }
+LinearKernel last_linear() { return g_taken; }
+bool debug_linear_fits(const LinearArgs& a) {
+    return !(g_set.kernel == 1 && g_set.splits > chunks_of(a)) && !(g_set.kernel == 2 && g_set.size == 256 && a.out_dtype == GEOCACHE_F32) &&
+           !(g_set.kernel == 3 && (a.N > kNarrowFeatures || a.gated));
+}
 
 cudaError_t launch_linear(const LinearArgs& given, cudaStream_t s) {
     LinearArgs a = given;
@@ -701,12 +714,14 @@ cudaError_t launch_linear(const LinearArgs& given, cudaStream_t s) {
     }();
     if (ready != cudaSuccess) return ready;
     a.error = word;
-    const Choice c = choose(a, sms);
+    Choice c = choose(a, sms);
+    if (g_set.kernel) c = {g_set.kernel == 2 ? g_set.size : 0, g_set.kernel == 1 ? g_set.size : 0, g_set.splits};
+    g_taken = c.pair_features ? LinearKernel{2, c.pair_features, 0} : c.tokens ? LinearKernel{1, c.tokens, c.splits} : LinearKernel{3, 0, 0};
     if (c.pair_features) return launch_linear_pairs(a, c.pair_features, sms, s);
     Params p{};
     p.a = a;
-    const int eb = a.in_dtype == GEOCACHE_E4M3 ? 1 : 2, ob = a.out_dtype == GEOCACHE_F32 ? 4 : 2;
-    p.chunks = (int)(((long long)a.K * eb + kRowBytes - 1) / kRowBytes);
+    const int ob = a.out_dtype == GEOCACHE_F32 ? 4 : 2;
+    p.chunks = chunks_of(a);
     const int part = a.gated ? kFeatures / 2 : kFeatures;
     p.feature_tiles = (a.N + part - 1) / part;
     p.tokens = c.tokens;

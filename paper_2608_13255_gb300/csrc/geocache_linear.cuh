@@ -15,9 +15,10 @@ namespace geocache {
 constexpr int kRowBytes = 128;   // of an operand's row in a stage: 64 16-bit elements or 128 of 8 bits (one swizzle row)
 
 // The sums leave tensor memory after so many chunks and are added up in registers, rounded to nearest: the tensor cores' own
-// additions, four a chunk, cut off at most 2^-23 of the sum so far, always to one side.  f32 results: a chain of 128 additions
-// was 2.1e-6 from the definition, parts of 16 2.4e-7.  16-bit results: one chain up to kChainChunks, 1,024 additions (at most
-// 6.1e-5 where all products have one sign, f16's half step is 2.4e-4), beyond them parts of that length.
+// additions, four a chunk, cut off up to 2^-22 of the sum so far, always to one side.  Where all products have one sign, a chain
+// of 512 is 2.4e-5 (bf16) or 4.7e-5 (f16) off, with parts of 16 it is 1.1e-6; of normal numbers a chain of 128
+// was 2.1e-6 of the norm off, in parts 2.4e-7.  16-bit results have one chain up to kChainChunks, 1,024 additions (at most
+// 1.2e-4, half of f16's half step; 65,536 were 6.2e-3 off), beyond them parts of that length.
 constexpr int kPartChunks = 4, kChainChunks = 256;
 
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {

@@ -100,7 +100,8 @@ EXPORTS = ("geocache_build_corr", "geocache_transport_step", "geocache_reconstru
            "geocache_rotate_anchors", "geocache_device_status", "geocache_corr_record_count",
            "geocache_transport_workspace", "geocache_transport_step_noalloc", "geocache_pack_anchors",
            "geocache_unpack_anchors", "geocache_transport_step_update", "geocache_permute_records",
-           "geocache_raster_posmaps", "geocache_debug_set_wait", "geocache_raster_posmaps_supersampled",
+           "geocache_raster_posmaps", "geocache_debug_set_wait", "geocache_debug_set_linear",
+           "geocache_debug_last_linear", "geocache_raster_posmaps_supersampled",
            "geocache_pool_posmaps", "geocache_fill_records", "geocache_last_launches",
            "geocache_rope_table", "geocache_qk_norm_rope", "geocache_plan_attention", "geocache_attention",
            "geocache_add_rms_norm", "geocache_quantize_rows", "geocache_linear",
@@ -167,6 +168,10 @@ def load():
         L.geocache_device_status.argtypes = [P]
         L.geocache_debug_set_wait.argtypes = [ctypes.c_uint64, i]
         L.geocache_debug_set_wait.restype = ctypes.c_int
+        L.geocache_debug_set_linear.argtypes = [i, i, i]
+        L.geocache_debug_set_linear.restype = ctypes.c_int
+        L.geocache_debug_last_linear.argtypes = [P, P, P]
+        L.geocache_debug_last_linear.restype = ctypes.c_int
         L.geocache_last_error.restype = ctypes.c_char_p
         L.geocache_last_error.argtypes = []
         L.geocache_abi_version.argtypes = []
@@ -880,6 +885,23 @@ def debug_set_wait(limit_ns: int = 0, drop_first_copy: bool = False):
     (0 = default), and whether the next staged transport call leaves its first
     unit's copies unissued so that its wait runs out."""
     _check(load().geocache_debug_set_wait(int(limit_ns), 1 if drop_first_copy else 0))
+
+
+LINEAR_BY_ESTIMATE, LINEAR_TILES, LINEAR_PAIRS, LINEAR_FEW_FEATURES = 0, 1, 2, 3
+
+
+def debug_set_linear(kernel: int = LINEAR_BY_ESTIMATE, size: int = 0, splits: int = 0):
+    """geocache_debug_set_linear (test hook): the kernel that later calls of linear
+    take; without arguments again the one with the least estimate."""
+    _check(load().geocache_debug_set_linear(int(kernel), int(size), int(splits)))
+
+
+def debug_last_linear():
+    """geocache_debug_last_linear (test hook): (kernel, size, splits) of the calling
+    thread's last linear."""
+    k, n, s = ctypes.c_int(0), ctypes.c_int(0), ctypes.c_int(0)
+    _check(load().geocache_debug_last_linear(ctypes.byref(k), ctypes.byref(n), ctypes.byref(s)))
+    return k.value, n.value, s.value
 
 
 def abi_version() -> int:
