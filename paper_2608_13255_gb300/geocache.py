@@ -741,12 +741,6 @@ _ACTIVATIONS = {None: ACT_NONE, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "s
 _ROWS = None
 
 
-def _activation(name):
-    if isinstance(name, (str, type(None))) and name in _ACTIVATIONS:
-        return _ACTIVATIONS[name]
-    raise ValueError('activation must be None, "gelu", "gelu_tanh" or "silu" (got %r)' % (name,))
-
-
 def _rows_binding():
     """The module that checks and marshals the tensors of the calls on rows
     (csrc/geocache_rows_binding.cpp)."""
@@ -828,7 +822,11 @@ def linear(x, weight, bias=None, activation=None, gated=False, residual=None, x_
         out = _empty((_tensor(x, "x").shape[0], N // 2 if gated else N), out_dtype, x.device, stream)
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise TypeError("out must be %s (got %s)" % (out_dtype, out.dtype))
-    _check((_ROWS or _rows_binding()).linear(x, weight, bias, _activation(activation), gated, residual, x_scale,
+    try:
+        act = _ACTIVATIONS[activation]
+    except (KeyError, TypeError):
+        raise ValueError('activation must be None, "gelu", "gelu_tanh" or "silu" (got %r)' % (activation,)) from None
+    _check((_ROWS or _rows_binding()).linear(x, weight, bias, act, gated, residual, x_scale,
                                              weight_scale, out, None if stream is None else _handle(stream)))
     return out
 
