@@ -3,8 +3,10 @@
 The library is compiled from ``csrc/*.cu`` with one ``-gencode`` for sm_103a,
 each translation unit in parallel, and linked with the static CUDA runtime so
 that the shared object only needs the driver at run time.  Beside it stands
-``geocache_rows_binding.so``, a module of the running interpreter (g++, torch's
-headers) through which Python calls the operators on rows.
+``geocache_rows_binding.so``, a module of the running interpreter (g++, its
+headers and those of a CUDA torch) through which Python calls the operators on
+rows.  The library does not need it: where one of these is missing the library is
+built alone, and the calls on rows say why they have no module.
 """
 from __future__ import annotations
 
@@ -22,6 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libgeocache.so")
 BINDING = os.path.join(LIBDIR, "geocache_rows_binding.so")
+BINDING_FOR = os.path.join(LIBDIR, "geocache_rows_binding.for")  # the interpreter and the torch it was built for
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2", "--expt-relaxed-constexpr"]
@@ -61,11 +64,58 @@ def source_hash() -> str:
     return h.hexdigest()[:16]
 
 
-def is_stale() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
+def _torch_dir() -> str:
+    import importlib.util
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else ""
+
+
+def binding_for() -> str:
+    """The interpreter and the torch that a module built now would be for."""
+    import importlib.metadata
+    try:
+        torch_version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        torch_version = "none"
+    return "%s, torch %s in %s" % (sysconfig.get_config_var("SOABI"), torch_version, _torch_dir())
+
+
+def binding_needs() -> str:
+    """What the module's build lacks here ("" if nothing)."""
+    torch_dir = _torch_dir()
+    for what, there in (("g++", shutil.which("g++")), ("Python.h", os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))),
+                        ("torch", torch_dir), ("a CUDA torch", os.path.exists(os.path.join(torch_dir, "lib", "libc10_cuda.so")))):
+        if not there:
+            return what
+    return ""
+
+
+def binding_was_for() -> str:
+    """The interpreter and the torch that the module was built for."""
+    try:
+        with open(BINDING_FOR) as f:
+            return f.read()
+    except OSError:
+        return "another build"
+
+
+def binding_is_stale() -> bool:
+    """Whether the module is missing or older than its sources, or was built for another interpreter or torch."""
+    if not os.path.exists(BINDING) or binding_was_for() != binding_for():
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
+    t = os.path.getmtime(BINDING)
     return any(os.path.getmtime(d) > t for d in _deps())
+
+
+def library_is_stale() -> bool:
+    if not os.path.exists(LIB):
+        return True
+    t = os.path.getmtime(LIB)
+    return any(os.path.getmtime(d) > t for d in _deps() if d != _binding_source())
+
+
+def is_stale() -> bool:
+    return library_is_stale() or (binding_is_stale() and not binding_needs())
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
@@ -80,18 +130,15 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         fcntl.flock(lock, fcntl.LOCK_EX)
         if not force and not is_stale():  # another process built it meanwhile
             return LIB
-        return _build_locked(verbose, extra_flags)
+        return _build_locked(verbose, extra_flags, force)
 
 
-def _torch_dir() -> str:
-    import importlib.util
-    return os.path.dirname(importlib.util.find_spec("torch").origin)
-
-
-def _build_locked(verbose, extra_flags) -> str:
+def _build_locked(verbose, extra_flags, force) -> str:
     cc = nvcc()
+    library, lacks = force or library_is_stale(), binding_needs()
+    binding = not lacks and (force or binding_is_stale())
     objs, procs = [], []
-    for src in _sources():
+    for src in _sources() if library else []:
         obj = os.path.join(LIBDIR, os.path.basename(src)[:-3] + ".o")
         cmd = [cc, *ARCH, *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj]
         if verbose:
@@ -100,11 +147,12 @@ def _build_locked(verbose, extra_flags) -> str:
         objs.append(obj)
     torch_dir = _torch_dir()
     binding_obj = os.path.join(LIBDIR, "geocache_rows_binding.o")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE, "-I", os.path.join(torch_dir, "include"),
-           "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
-           "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(cc))), "include"),
-           "-I", sysconfig.get_paths()["include"], "-c", _binding_source(), "-o", binding_obj]
-    procs.append((_binding_source(), subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    if binding:
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE, "-I", os.path.join(torch_dir, "include"),
+               "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+               "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(cc))), "include"),
+               "-I", sysconfig.get_paths()["include"], "-c", _binding_source(), "-o", binding_obj]
+        procs.append((_binding_source(), subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -112,15 +160,21 @@ def _build_locked(verbose, extra_flags) -> str:
             sys.stderr.write(out.decode(errors="replace"))
         if p.returncode:
             failed.append(src)
+    if library and not any(src != _binding_source() for src in failed):
+        tmp = LIB + ".tmp%d" % os.getpid()
+        subprocess.check_call([cc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs])
+        os.replace(tmp, LIB)
     if failed:
         raise RuntimeError("compiling failed on: " + ", ".join(failed))
-    tmp = LIB + ".tmp%d" % os.getpid()
-    subprocess.check_call([cc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs])
-    os.replace(tmp, LIB)
-    tmp = BINDING + ".tmp%d" % os.getpid()
-    subprocess.check_call(["g++", "-shared", "-o", tmp, binding_obj, "-L", LIBDIR, "-lgeocache", "-Wl,-rpath,$ORIGIN",
-                           "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
-    os.replace(tmp, BINDING)
+    if binding:
+        tmp = BINDING + ".tmp%d" % os.getpid()
+        subprocess.check_call(["g++", "-shared", "-o", tmp, binding_obj, "-L", LIBDIR, "-lgeocache", "-Wl,-rpath,$ORIGIN",
+                               "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
+        os.replace(tmp, BINDING)
+        with open(BINDING_FOR, "w") as f:
+            f.write(binding_for())
+    elif lacks:
+        sys.stderr.write("geocache_rows_binding.so is not built: it needs %s\n" % lacks)
     return LIB
 
 

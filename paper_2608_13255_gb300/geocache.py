@@ -748,7 +748,12 @@ def _rows_binding():
     if _ROWS is None:
         load()
         if not os.path.exists(_build.BINDING):
-            raise RuntimeError("%s is not built; run __graft_entry__.build()" % _build.BINDING)
+            lacks = _build.binding_needs()
+            raise RuntimeError("%s is not built%s; run __graft_entry__.build()" %
+                               (_build.BINDING, " (its build needs %s)" % lacks if lacks else ""))
+        if _build.binding_was_for() != _build.binding_for():
+            raise RuntimeError("%s was built for %s, this is %s; run __graft_entry__.build()" %
+                               (_build.BINDING, _build.binding_was_for(), _build.binding_for()))
         loader = importlib.machinery.ExtensionFileLoader("geocache_rows_binding", _build.BINDING)
         spec = importlib.util.spec_from_file_location("geocache_rows_binding", _build.BINDING, loader=loader)
         _ROWS = importlib.util.module_from_spec(spec)
