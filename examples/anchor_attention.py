@@ -3,9 +3,10 @@
 Full steps run the block on all views; cached steps run it on the anchors alone (Sec. 3.2, batch-sliced anchor forward):
 their rows are packed, keep the rotary slots of the N-view layout, and attend to each other inside their asset; the
 library transports their change to the other views.  Background tokens take no part, so each asset is a packed sequence
-of its own length.  The projections of the latents are torch products (their few channels are no whole 16-byte words);
-the norms with the rotation, the attention, the packing, the transport and the reconstruction are the library's.  With
---ff a gated feed-forward stands behind the attention: the library's norm and products, with --eight-bit on 8-bit rows.
+of its own length.  The projections of the latents are torch products (those into the heads have rows of few channels, no whole
+16-byte words); the norms with the rotation, the attention, the packing, the transport and the reconstruction are the library's.
+With --ff a gated feed-forward stands behind the attention: the library's norm and products, with --eight-bit on 8-bit rows, and
+its product back to the latents, into f32.
 
     python examples/anchor_attention.py [--workload hunyuan64] [--assets 2] [--heads 8] [--dim 64] [--steps 10]
                                         [--ff 2048 [--eight-bit]]
@@ -56,6 +57,7 @@ class Block:
             self.norm_weight = 1 + 0.1 * r(M)
             self.up = (r(2 * ff, M) / M ** 0.5).to(torch.bfloat16)       # values, then gates
             self.down = (r(M, ff) / ff ** 0.5).to(torch.bfloat16)
+            self.back_rows = self.back.T.contiguous()                    # [C, M]: features are rows
             self.up_scale = self.down_scale = None
             if eight_bit:
                 self.up, self.up_scale = gc.quantize_rows(self.up)
@@ -105,10 +107,11 @@ class Block:
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
         gc.qk_norm_rope(q, k, self.table, slots, self.q_weight, self.k_weight, q_out=q, k_out=k)  # in place
         out = gc.attention(plan, q, k, v).reshape(len(place), -1)
-        if self.ff:
-            out = self.feed_forward(out)
         x0 = torch.zeros((w.B * len(views) * w.H * w.W, w.C), device="cuda")
-        x0[place] = (out @ self.back).float()
+        if self.ff:
+            x0[place] = gc.linear(self.feed_forward(out), self.back_rows, out_dtype=torch.float32)
+        else:
+            x0[place] = (out @ self.back).float()
         return x0.view(w.B, len(views), w.H, w.W, w.C).permute(0, 1, 4, 2, 3).contiguous()
 
 
