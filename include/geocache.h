@@ -608,8 +608,9 @@ int geocache_add_rms_norm(const geocache_rows* x, const geocache_rows* residual,
  * geocache_quantize_rows -- 8-bit rows of what follows no norm (the
  * attention's output, a feed-forward's hidden rows, weights):
  *     scale = max(max_c |x_c| / 448, 2^-126),  out = e4m3(x / scale),
- * the scale rounded to nearest; from 16-bit rows so are the quotients (binary32,
- * then e4m3), from F32 rows they are within 2^-43 of that before the rounding.
+ * in binary32: the scale is the rounded product with the number nearest to 1 / 448;
+ * from 16-bit rows the quotients are rounded to nearest (and then to e4m3), from
+ * F32 rows they are within 2^-43 of that before the rounding.
  * x [T, C] of `dtype` (F32, BF16 or F16), out [T, C] E4M3, scale device [T] f32.
  * Sizes, alignment and statuses as geocache_add_rms_norm; no buffers overlap.
  * ------------------------------------------------------------------------ */

@@ -2,8 +2,10 @@
 //
 //     h = x + residual (rounded to the residual's type, as it is stored),  r = 1 / sqrt(mean(h^2) + eps),
 //     y = h w r,  scale = max(max |y| / 448, 2^-126),  q = e4m3(y / scale).
-// One pass: a row stays in the registers of the threads that read it, and its two statistics, sum h^2 and max |h w|, are
-// taken in one round: max |y| = r max |h w|, since r does not depend on the element.  Sums are binary32.
+// One pass: a row stays with the threads that read it, and its two statistics, sum h^2 and max |h w|, are taken in one round:
+// max |y| = r max |h w|, since r does not depend on the element.  Sums are binary32.  Up to 16,384 elements a row is held in
+// registers (but for up to 12 bytes a thread of some kernels for single elements); beyond that most of it lies in local memory
+// (128 to 4,360 bytes a thread): 2048 x 16384 bf16 with residual into 8 bits 51 us, x 32768 308 (with its bytes at the copy rate 69).
 //
 // Bound by memory on paper (bf16 with residual into 8 bits: 7 bytes an element), and by the instructions in a first form
 // with 40 an element: 24576 rows of 2048 in bf16 with residual into 8 bits took 95 us, with half as many 59 (5.9 TB/s).
@@ -57,13 +59,10 @@ __device__ __forceinline__ uint32_t pack_e4m3(float2 a, float2 b) {
     return r;
 }
 
-// max / 448: an inverse of two terms, the first of which is rounded down.  Rounded correctly, as no quotient by 7 is within
-// 2^-27 of half a step, where no term is subnormal.
+// max / 448, as a product with the nearest binary32 number to 1 / 448 (what a division of a tensor by a number is elsewhere too,
+// so that rows made there have the same scales)
 __device__ __forceinline__ float scale_of(float top) {
-    constexpr float kHigh = 0x1.249248p-9f, kLow = (float)(1.0 / 448.0 - (double)kHigh);
-    static_assert(kLow > 0.0f, "rounded down");
-    float s = fmaf(top, kHigh, top * kLow);
-    if (top < 0x1p-60f) s = __fdiv_rn(top, kLargest);
+    const float s = top * (1.0f / kLargest);
     return s < kTiny ? kTiny : s;  // (a NaN stays)
 }
 // 1 / scale as the sum of two terms: x hi + x lo is within 2^-43 of x / scale before it is rounded.  With one term a value at
@@ -507,7 +506,7 @@ cudaError_t launch_norm_rows(const NormRowsArgs& given, cudaStream_t s) {
     int pieces = n <= 32 ? 1 : n <= 2 * most_threads(2) ? 2 : n <= 4 * most_threads(4) ? 4 : 8;
     // Norms of many rows are bound by instructions, of which four pieces have fewer (44943 x 2048 bf16 with residual into 8
     // bits 110 -> 103 us, 11772 x 1808 without 21.3 -> 18.6); few rows leave SMs idle (1569 x 592 3.2 -> 3.5), and 8-bit
-    // rows without a norm are bound by memory (8192 x 2048 10.1 -> 11.1).
+    // rows without a norm are bound by memory (8192 x 2048 11.2 -> 12.2, 24576 x 1280 23.2 -> 29.4; buffers in turn).
     if (pieces == 2 && n > 64 && a.norm && a.T >= 3000 && four_ahead(eb, !a.residual.data ? kNone : eb == 2 && !a.residual_f32 ? kSame : kF32))
         pieces = 4;
     int lanes = 1;

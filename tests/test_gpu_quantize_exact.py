@@ -1,6 +1,6 @@
-"""8-bit rows bit for bit: geocache_quantize_rows defines scale = max(max |x| / 448, 2^-126) and out = e4m3(x / scale), each
-operation rounded to nearest in binary32.  torch's division of two binary32 tensors and its conversion to float8_e4m3fn are
-these operations, so scales and elements have to be equal, also at the ties of e4m3."""
+"""8-bit rows bit for bit: geocache_quantize_rows defines scale = max(max |x| r, 2^-126) with r = 1 / 448 rounded to binary32, and
+out = e4m3(x / scale), each operation rounded to nearest in binary32.  torch's product, its division of two binary32 tensors and
+its conversion to float8_e4m3fn are these operations, so scales and elements have to be equal, also at the ties of e4m3."""
 import pytest
 import torch
 
@@ -25,7 +25,7 @@ def gc():
 def _equal(gc, x):
     q, scale = gc.quantize_rows(x)
     y = x.float()
-    want = torch.div(y.abs().amax(-1), torch.full((), 448.0, device=DEV)).clamp(min=TINY)
+    want = (y.abs().amax(-1) * torch.full((), 1.0 / 448.0, device=DEV)).clamp(min=TINY)
     assert torch.equal(scale, want)
     assert torch.equal(q.view(torch.uint8), (y / want[:, None]).to(E4M3).view(torch.uint8))
 
