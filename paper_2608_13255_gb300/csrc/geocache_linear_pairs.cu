@@ -529,7 +529,8 @@ cudaError_t launch(PairParams p, int pairs, cudaStream_t s) {
     return launch_cluster(kern, dim3((unsigned)(2 * pairs)), kThreads, kBytes, 2, s, p, wm, xm, om);
 }
 
-// f32 results: tiles of 128 rows of weights only, whose sums the registers hold
+// f32 results: tiles of 128 rows of weights only, whose sums fit beside the rest of the 168 registers (the gated kernels move 52
+// bytes a thread to local memory, those of 16-bit results with 256 rows 152)
 template <typename Out, bool kEight, bool kGated, bool kParts>
 cudaError_t launch_n(const PairParams& p, int features, int pairs, cudaStream_t s) {
     if constexpr (!std::is_same<Out, float>::value)

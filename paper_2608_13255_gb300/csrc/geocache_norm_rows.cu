@@ -4,8 +4,8 @@
 //     y = h w r,  scale = max(max |y| / 448, 2^-126),  q = e4m3(y / scale).
 // One pass: a row stays with the threads that read it, and its two statistics, sum h^2 and max |h w|, are taken in one round:
 // max |y| = r max |h w|, since r does not depend on the element.  Sums are binary32.  Up to 16,384 elements a row is held in
-// registers (but for up to 12 bytes a thread of some kernels for single elements); beyond that most of it lies in local memory
-// (128 to 4,360 bytes a thread): 2048 x 16384 bf16 with residual into 8 bits 51 us, x 32768 308 (with its bytes at the copy rate 69).
+// registers (but for up to 8 bytes a thread in a few kernels); beyond that most of it lies in local memory (140 to 4,344 bytes
+// a thread): 2048 x 16384 bf16 with residual into 8 bits 51 us, x 32768 308 (with its bytes at the copy rate 69).
 //
 // Bound by memory on paper (bf16 with residual into 8 bits: 7 bytes an element), and by the instructions in a first form
 // with 40 an element: 24576 rows of 2048 in bf16 with residual into 8 bits took 95 us, with half as many 59 (5.9 TB/s).
@@ -67,7 +67,7 @@ __device__ __forceinline__ float scale_of(float top) {
 }
 // 1 / scale as the sum of two terms: x hi + x lo is within 2^-43 of x / scale before it is rounded.  With one term a value at
 // the middle of two numbers of e4m3, which 16-bit rows meet often, went either way (0.05% of the elements of 20001 x 8192
-// f16 were a step from e4m3(x / scale); one more instruction a pair: 81.5 -> 82.9 us, 8192 x 2048 bf16 9.1 -> 9.8).  lo is
+// f16 were a step from e4m3(x / scale); one more instruction a pair: 81.5 -> 82.8 us, 8192 x 2048 bf16 9.2 -> 9.9).  lo is
 // positive, so that a zero keeps its sign.
 struct Inverse {
     float hi, lo;
