@@ -77,7 +77,7 @@ def binding_for() -> str:
         torch_version = importlib.metadata.version("torch")
     except importlib.metadata.PackageNotFoundError:
         torch_version = "none"
-    return "%s, torch %s in %s" % (sysconfig.get_config_var("SOABI"), torch_version, _torch_dir())
+    return "%s, torch %s" % (sysconfig.get_config_var("SOABI"), torch_version)
 
 
 def binding_needs() -> str:

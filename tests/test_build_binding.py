@@ -29,7 +29,7 @@ def _elsewhere(monkeypatch, tmp_path):
 def test_a_module_of_another_torch_is_stale(gc, monkeypatch, tmp_path):
     assert not gbuild.is_stale() and gbuild.binding_was_for() == gbuild.binding_for()
     monkeypatch.setattr(gbuild, "BINDING_FOR", str(tmp_path / "for"))
-    for text in (None, "cpython-39, torch 1.0 in /nowhere"):
+    for text in (None, "cpython-39, torch 1.0"):
         if text:
             (tmp_path / "for").write_text(text)
         assert gbuild.binding_is_stale() and gbuild.is_stale() and not gbuild.library_is_stale()
